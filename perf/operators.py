@@ -291,7 +291,7 @@ def _plain_adamw(s, coef):
         m, v = s["M"], s["V"]
     # (each product rounded by itself: an 8-bit code next to a border does not depend on a fused multiply-add)
     m.mul_(h["beta1"]).add_(g * (1 - h["beta1"]))
-    v.mul_(h["beta2"]).add_(g.square_().mul_(1 - h["beta2"]))
+    v.mul_(h["beta2"]).add_(g.square().mul_(1 - h["beta2"]))
     root = v.sqrt()
     if "Ms" in s:
         x, s["Ms"][:] = _code(m)

@@ -11,6 +11,7 @@
 #include <mutex>
 #include <utility>
 
+#include "abi.h"
 #include "internal.h"
 #include "resbm.h"
 #include "tc.h"
@@ -20,17 +21,37 @@ using namespace resbm;
 namespace resbm {
 static std::atomic<uint64_t> g_launches{0};
 void count_launches(uint64_t n) { g_launches.fetch_add(n, std::memory_order_relaxed); }
-}  // namespace resbm
 
-namespace {
-
-thread_local int g_last_cuda_error = 0;
+static thread_local int g_last_cuda_error = 0;
 
 resbm_status cuda_fail(cudaError_t e)
 {
     g_last_cuda_error = (int)e;
     return RESBM_ERR_CUDA;
 }
+
+static constexpr int kMaxDevices = 64;
+static std::atomic<int> g_sm_count[kMaxDevices];
+
+resbm_status make_ctx(void *stream, Ctx *c)
+{
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return cuda_fail(e);
+    int sms = (dev >= 0 && dev < kMaxDevices) ? g_sm_count[dev].load(std::memory_order_relaxed) : 0;
+    if (sms <= 0) {
+        e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+        if (e != cudaSuccess) return cuda_fail(e);
+        if (dev >= 0 && dev < kMaxDevices) g_sm_count[dev].store(sms, std::memory_order_relaxed);
+    }
+    c->stream = static_cast<cudaStream_t>(stream);
+    c->device = dev;
+    c->sm_count = sms;
+    return RESBM_OK;
+}
+}  // namespace resbm
+
+namespace {
 
 // The first columns of a row-major matrix between host and device when the host side is pinned
 // and mapped: rows x w16 16-byte units, both sides rows pitch16 units apart, one unit per thread
@@ -98,26 +119,6 @@ cudaError_t side_streams(cudaStream_t caller, SideStreams **out)
     return cudaSuccess;
 }
 
-constexpr int kMaxDevices = 64;
-std::atomic<int> g_sm_count[kMaxDevices];
-
-resbm_status make_ctx(void *stream, Ctx *c)
-{
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return cuda_fail(e);
-    int sms = (dev >= 0 && dev < kMaxDevices) ? g_sm_count[dev].load(std::memory_order_relaxed) : 0;
-    if (sms <= 0) {
-        e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-        if (e != cudaSuccess) return cuda_fail(e);
-        if (dev >= 0 && dev < kMaxDevices) g_sm_count[dev].store(sms, std::memory_order_relaxed);
-    }
-    c->stream = static_cast<cudaStream_t>(stream);
-    c->device = dev;
-    c->sm_count = sms;
-    return RESBM_OK;
-}
-
 // SM count that sizes the scratch memory: the current device's, or kDefaultSms when no device
 // can be queried (the tensor-core backward kernels keep one partial slot per CTA).
 constexpr int kDefaultSms = 160;
@@ -140,8 +141,6 @@ int sizing_sms()
 
 size_t elem_size(const resbm_desc &d) { return d.dtype == RESBM_BF16 ? 2 : 4; }
 
-bool mul_ok(int64_t a, int64_t b) { return a >= 0 && b >= 0 && (a == 0 || b <= INT64_MAX / a); }
-
 resbm_status check_desc(const resbm_desc *d)
 {
     if (!d) return RESBM_ERR_INVALID_ARG;
@@ -158,37 +157,6 @@ resbm_status check_desc(const resbm_desc *d)
         !mul_ok(d->d, d->m) || d->d * d->m > big || !mul_ok(d->m, d->r) || d->m * d->r > big)
         return RESBM_ERR_INVALID_ARG;
     return RESBM_OK;
-}
-
-// A tensor argument: required non-null when it has elements, aligned to its element size.
-bool ptr_ok(const void *p, size_t align, bool required)
-{
-    if (!p) return !required;
-    return (reinterpret_cast<uintptr_t>(p) % align) == 0;
-}
-
-struct Range {
-    uintptr_t lo, hi;
-};
-Range rng(const void *p, int64_t n, size_t es)
-{
-    uintptr_t a = reinterpret_cast<uintptr_t>(p);
-    return Range{a, a + (uintptr_t)n * es};
-}
-bool overlaps(Range a, Range b)
-{
-    if (!a.lo || !b.lo || a.lo == a.hi || b.lo == b.hi) return false;
-    return a.lo < b.hi && b.lo < a.hi;
-}
-template <size_t N> bool any_overlap(const Range (&outs)[N], const Range *ins, size_t nin)
-{
-    for (size_t i = 0; i < N; ++i) {
-        for (size_t j = 0; j < nin; ++j)
-            if (overlaps(outs[i], ins[j])) return true;
-        for (size_t j = i + 1; j < N; ++j)
-            if (overlaps(outs[i], outs[j])) return true;
-    }
-    return false;
 }
 
 // Which kernels run an op: the fused tensor-core kernels where they take the shape and are the faster
@@ -296,8 +264,6 @@ resbm_status zero_f32(float *p, int64_t n, cudaStream_t s)
     cudaError_t e = cudaMemsetAsync(p, 0, (size_t)n * sizeof(float), s);
     return e == cudaSuccess ? RESBM_OK : cuda_fail(e);
 }
-
-resbm_status finish(cudaError_t e) { return e == cudaSuccess ? RESBM_OK : cuda_fail(e); }
 
 // ---- per-op validation (no GPU work) ---------------------------------------------------------
 resbm_status validate_encode_fwd(const resbm_desc &d, const void *X, const void *F,

@@ -1,4 +1,4 @@
-"""Python binding of the C ABI in include/resbm.h (libresbm.so).
+"""Python binding of the C ABI in include/resbm.h and include/resbm_train.h (libresbm.so).
 
 Argument marshalling only: every function here has the C function's name, takes torch tensors
 (device memory owned by the caller) or None, passes their data pointers and the current CUDA
@@ -45,6 +45,11 @@ EXPORTS = ("resbm_version", "resbm_status_string", "resbm_last_cuda_error", "res
            "resbm_newton_schulz", "resbm_effective_rank", "resbm_ffn_down_encode_workspace_bytes",
            "resbm_ffn_down_encode_fwd", "resbm_decode_fwd_rmsnorm", "resbm_rmsnorm_bwd",
            "resbm_measure_hbm_form")
+# the functions of include/resbm_train.h
+TRAIN_EXPORTS = ("resbm_add_rmsnorm_fwd", "resbm_adamw_plan_bytes", "resbm_adamw_plan", "resbm_adamw_step",
+                 "resbm_grad_norm_workspace_bytes", "resbm_grad_norm")
+RESBM_STATE_NONE, RESBM_STATE_E4M3, RESBM_STATE_F32 = 0, 8, 32
+RESBM_STATE_BLOCK = 256
 
 
 class resbm_desc(ctypes.Structure):
@@ -57,6 +62,26 @@ class resbm_step_args(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in
                 ("X", "F", "dY", "We1", "We2", "Wd1", "Wd2", "B", "P", "Y", "dB", "dF", "dX",
                  "dWe1", "dWe2", "dWd1", "dWd2", "wait_before_inputs", "inputs_done")]
+
+
+class resbm_add_norm_desc(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64), ("d", ctypes.c_int64), ("ldx", ctypes.c_int64), ("lda", ctypes.c_int64),
+                ("ldh", ctypes.c_int64), ("ldn", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("q_group", ctypes.c_int32), ("eps", ctypes.c_float), ("flags", ctypes.c_uint32)]
+
+
+class resbm_adamw_desc(ctypes.Structure):
+    _fields_ = [("w_dtype", ctypes.c_int32), ("g_dtype", ctypes.c_int32), ("state", ctypes.c_int32),
+                ("flags", ctypes.c_uint32)]
+
+
+class resbm_adamw_tensor(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("w", "g", "m", "v", "m_scale", "v_scale", "master")] + [("n", ctypes.c_int64)]
+
+
+class resbm_adamw_hyper(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay")] + \
+               [("step", ctypes.c_int64)] + [(n, ctypes.c_void_p) for n in ("lr_dev", "step_dev", "grad_scale")]
 
 
 class ResbmError(RuntimeError):
@@ -129,6 +154,18 @@ def load(path: str | None = None) -> ctypes.CDLL:
     lib.resbm_ffn_down_encode_fwd.argtypes = [D, i64] + [vp] * 8 + [vp, sz, vp]
     lib.resbm_measure_hbm_form.restype = i32
     lib.resbm_measure_hbm_form.argtypes = [i32, vp, vp, i64, vp]
+    lib.resbm_add_rmsnorm_fwd.restype = i32
+    lib.resbm_add_rmsnorm_fwd.argtypes = [ctypes.POINTER(resbm_add_norm_desc)] + [vp] * 8
+    lib.resbm_adamw_plan_bytes.restype = i32
+    lib.resbm_adamw_plan_bytes.argtypes = [i64, ctypes.POINTER(sz)]
+    lib.resbm_adamw_plan.restype = i32
+    lib.resbm_adamw_plan.argtypes = [ctypes.POINTER(resbm_adamw_desc), ctypes.POINTER(resbm_adamw_tensor), i64, vp, sz]
+    lib.resbm_adamw_step.restype = i32
+    lib.resbm_adamw_step.argtypes = [vp, ctypes.POINTER(resbm_adamw_hyper), vp]
+    lib.resbm_grad_norm_workspace_bytes.restype = i32
+    lib.resbm_grad_norm_workspace_bytes.argtypes = [ctypes.POINTER(vp), i64, ctypes.POINTER(sz)]
+    lib.resbm_grad_norm.restype = i32
+    lib.resbm_grad_norm.argtypes = [ctypes.POINTER(vp), i64, ctypes.c_float, vp, vp, sz, vp]
     if path is None:
         _lib = lib
     return lib
@@ -363,3 +400,179 @@ def resbm_ffn_down_encode_fwd(desc, H, W2, X, We1, We2, B, P_save, F_out, ws, st
     st = load().resbm_ffn_down_encode_fwd(ctypes.byref(desc), int(f), _p(H), _p(W2), _p(X), _p(We1), _p(We2),
                                           _p(B), _p(P_save), _p(F_out), _p(ws), _nbytes(ws), _stream(stream))
     _check("resbm_ffn_down_encode_fwd", st)
+
+
+# ---- the training step's operators around the boundary (include/resbm_train.h) ----------------
+_DT = {torch.float32: RESBM_F32, torch.bfloat16: RESBM_BF16}
+
+
+def _want(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _here(t, device, what):
+    """t is on the current device (where the library enqueues)"""
+    if not t.is_cuda or t.get_device() != device:
+        raise ValueError("%s must be on the current CUDA device (%d): got %s" % (what, device, t.device))
+
+
+def resbm_add_rmsnorm_fwd(X, A, gamma, eps, H=None, N=None, Q=None, S=None, q_group=0, stream=None):
+    """H = X + A (A None: H = X), N = RMSNorm(H) * gamma, Q and S the same in e4m3 with scales. X, A, H, N: (T, d) of one
+    type, unit stride along d, any row stride (A and X: also 0, an expanded row); gamma (d,); Q (T, d) dense, one byte an
+    element (float8_e4m3fn or uint8), with S (T, ceil(d / q_group)) fp32, or (T, 1) for q_group = 0."""
+    if X.dim() != 2 or X.dtype not in _DT:
+        raise ValueError("X must be (T, d), fp32 or bf16")
+    shape, dtype = X.shape, X.dtype
+    T, d = shape
+    device = torch.cuda.current_device()
+    ld = []
+    for name, t in (("X", X), ("A", A), ("H", H), ("N", N)):
+        if t is None:
+            ld.append(0)
+            continue
+        if t.shape != shape or t.dtype != dtype or (t.stride(1) != 1 and d > 1):
+            raise ValueError("%s must be %s, %s, with unit stride along the columns" % (name, tuple(shape), dtype))
+        _here(t, device, name)
+        ld.append(t.stride(0))
+    if gamma.shape != shape[1:] or gamma.dtype != dtype or not gamma.is_contiguous():
+        raise ValueError("gamma must be (%d,), %s" % (d, dtype))
+    _here(gamma, device, "gamma")
+    if (Q is None) != (S is None):
+        raise ValueError("Q and S come together")
+    if Q is not None:
+        groups = -(-d // q_group) if q_group > 0 else 1
+        if Q.shape != shape or Q.element_size() != 1 or not Q.is_contiguous():
+            raise ValueError("Q must be %s, dense, one byte an element" % (tuple(shape),))
+        if tuple(S.shape) != (T, groups) or S.dtype != torch.float32 or not S.is_contiguous():
+            raise ValueError("S must be (%d, %d), fp32, dense" % (T, groups))
+        _here(Q, device, "Q")
+        _here(S, device, "S")
+    desc = resbm_add_norm_desc(T, d, ld[0], ld[1], ld[2], ld[3], _DT[dtype], q_group, eps, 0)
+    st = load().resbm_add_rmsnorm_fwd(ctypes.byref(desc), X.data_ptr(), _p(A), gamma.data_ptr(), _p(H), _p(N), _p(Q), _p(S),
+                                      _stream(stream))
+    if st != RESBM_OK:
+        _check("resbm_add_rmsnorm_fwd", st)
+
+
+class AdamWPlan:
+    """The tensors of resbm_adamw_step and resbm_grad_norm (resbm_adamw_plan in host memory). Lists of dense CUDA tensors
+    of the same lengths, one entry per parameter: weights (fp32 or bf16), gradients (fp32 or bf16), states m and v (fp32,
+    or e4m3 codes of m and of sqrt(v): float8_e4m3fn or uint8, with m_scale and v_scale of ceil(n / 256) fp32), optionally
+    fp32 master copies of bf16 weights. With gradients alone (params None) the plan serves resbm_grad_norm. The plan
+    keeps the tensors alive; gradients that moved are given with set_grads."""
+
+    def __init__(self, params, grads, m=None, v=None, m_scale=None, v_scale=None, master=None):
+        self._fields = {"w": params, "g": grads, "m": m, "v": v, "m_scale": m_scale, "v_scale": v_scale, "master": master}
+        self._fields = {k: list(x) for k, x in self._fields.items() if x is not None}
+        grads = self._fields["g"]
+        self.device = torch.cuda.current_device()
+        self.count = len(grads)
+        state = RESBM_STATE_NONE
+        if params is not None:
+            _want(m is not None and v is not None, "weights come with their states m and v")
+            coded = self.count > 0 and self._fields["m"][0].element_size() == 1
+            state = RESBM_STATE_E4M3 if coded else RESBM_STATE_F32
+            _want((m_scale is not None) == coded and (v_scale is not None) == coded, "8-bit states, and only they, have scales")
+            _want(master is None or self.count == 0 or self._fields["w"][0].dtype == torch.bfloat16, "master copies are of bf16 weights")
+        else:
+            _want(set(self._fields) == {"g"}, "states and master copies belong to weights")
+        for k, x in self._fields.items():
+            _want(len(x) == self.count, "%s: %d tensors, and %d gradients" % (k, len(x), self.count))
+        for k in ("w", "g"):
+            x = self._fields.get(k)
+            _want(not x or (x[0].dtype in _DT and all(t.dtype == x[0].dtype for t in x)), "%s: fp32 or bf16, one type in a plan" % k)
+        for k, x in self._fields.items():
+            if k == "g":
+                continue
+            for t, g in zip(x, grads):
+                n = -(-g.numel() // RESBM_STATE_BLOCK) if k.endswith("_scale") else g.numel()
+                _want(t.is_contiguous() and t.numel() == n, "%s: dense tensors of the gradients' sizes" % k)
+                if k in ("m", "v"):
+                    _want(t.dtype in ((torch.float8_e4m3fn, torch.uint8) if state == RESBM_STATE_E4M3 else (torch.float32,)), "%s: fp32, or e4m3 codes with scales" % k)
+                elif k != "w":
+                    _want(t.dtype == torch.float32, "%s: fp32" % k)
+                _here(t, self.device, k)
+        dt = lambda k: _DT[self._fields[k][0].dtype] if self._fields.get(k) else RESBM_F32
+        self._desc = resbm_adamw_desc(dt("w"), dt("g"), state, 0)
+        self._tensors = (resbm_adamw_tensor * self.count)()
+        for k, x in self._fields.items():
+            for e, t in zip(self._tensors, x):
+                setattr(e, k, t.data_ptr())
+        for e, g in zip(self._tensors, grads):
+            e.n = g.numel()
+        size = ctypes.c_size_t(0)
+        _check("resbm_adamw_plan_bytes", load().resbm_adamw_plan_bytes(self.count, ctypes.byref(size)))
+        self._plan = (ctypes.c_uint64 * (-(-size.value // 8)))()
+        self._address = ctypes.addressof(self._plan)
+        self._check_grads(grads)
+        self._build()
+
+    def _check_grads(self, grads):
+        _want(len(grads) == self.count, "%d gradients for %d tensors" % (len(grads), self.count))
+        for g, o, e in zip(grads, self._fields["g"], self._tensors):
+            _want(g.is_contiguous() and g.numel() == e.n and g.dtype == o.dtype, "gradients: dense tensors of the same sizes and type")
+            _here(g, self.device, "a gradient")
+
+    def _build(self):
+        _check("resbm_adamw_plan", load().resbm_adamw_plan(ctypes.byref(self._desc), self._tensors, self.count, self._address,
+                                                           ctypes.sizeof(self._plan)))
+
+    def set_grads(self, grads):
+        """The gradients of the next steps: same sizes, types and order. (If they are refused, the plan is as before, or,
+        where they overlap what the step writes, refuses steps until it has others.)"""
+        grads = list(grads)
+        self._check_grads(grads)
+        self._fields["g"] = grads
+        for e, g in zip(self._tensors, grads):
+            e.g = g.data_ptr()
+        self._build()
+
+
+def resbm_adamw_step(plan, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, step=1, lr_dev=None, step_dev=None,
+                     grad_scale=None, stream=None):
+    """One AdamW step over the plan's tensors, in place. step counts from 1. lr_dev (fp32), step_dev (int64) and grad_scale
+    (fp32): one-element device tensors that the kernel reads instead of lr and step, and as the gradients' factor."""
+    for name, t, dt in (("lr_dev", lr_dev, torch.float32), ("step_dev", step_dev, torch.int64), ("grad_scale", grad_scale, torch.float32)):
+        if t is not None:
+            if t.dtype != dt or t.numel() != 1:
+                raise ValueError("%s must be one %s" % (name, dt))
+            _here(t, plan.device, name)
+    if torch.cuda.current_device() != plan.device:
+        raise ValueError("the plan's tensors are on device %d, not the current one" % plan.device)
+    hyper = resbm_adamw_hyper(lr, beta1, beta2, eps, weight_decay, step, _p(lr_dev), _p(step_dev), _p(grad_scale))
+    st = load().resbm_adamw_step(plan._address, ctypes.byref(hyper), _stream(stream))
+    if st != RESBM_OK:
+        _check("resbm_adamw_step", st)
+
+
+def _plans(plans):
+    plans = [plans] if isinstance(plans, AdamWPlan) else list(plans)
+    return (ctypes.c_void_p * len(plans))(*[p._address for p in plans]), plans
+
+
+def resbm_grad_norm_workspace_bytes(plans) -> int:
+    out = ctypes.c_size_t(0)
+    array, plans = _plans(plans)
+    _check("resbm_grad_norm_workspace_bytes", load().resbm_grad_norm_workspace_bytes(array, len(plans), ctypes.byref(out)))
+    return int(out.value)
+
+
+def grad_norm_workspace(plans, device="cuda") -> torch.Tensor:
+    return torch.empty(max(resbm_grad_norm_workspace_bytes(plans), 1), dtype=torch.uint8, device=device)
+
+
+def resbm_grad_norm(plans, max_norm, out, ws, stream=None):
+    """out (2 fp32): the norm of the gradients of a plan (or of several together), and the coefficient that clips it to
+    max_norm (0: none), which resbm_adamw_step takes as grad_scale = out[1:]."""
+    array, plans = _plans(plans)
+    device = torch.cuda.current_device()
+    if out.dtype != torch.float32 or out.numel() != 2 or not out.is_contiguous():
+        raise ValueError("out must be 2 fp32")
+    _here(out, device, "out")
+    _here(ws, device, "ws")
+    if any(p.device != device for p in plans):
+        raise ValueError("a plan's tensors are not on the current device")
+    st = load().resbm_grad_norm(array, len(plans), max_norm, out.data_ptr(), ws.data_ptr(), _nbytes(ws), _stream(stream))
+    if st != RESBM_OK:
+        _check("resbm_grad_norm", st)

@@ -14,18 +14,27 @@
 #include "abi.h"
 #include "common.cuh"
 #include "fp8.cuh"
+#include "pair.cuh"
 #include "resbm_train.h"
 
+#ifndef MINB
+#define MINB 8
+#endif
 namespace resbm {
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kThreads = 128, kWarps = kThreads / 32;
 constexpr int kBlock = RESBM_STATE_BLOCK;             // elements a warp takes at a time: one block of 8-bit states
+// Blocks that a warp has in flight where its accesses are vectors, by the states' bits
+__host__ __device__ constexpr int deep_of(int bits) { return bits == 8 ? 2 : 1; }
 constexpr int kSmall = 32, kLarge = 448;              // tensors a launch, by the parameter's size
 constexpr int kNormGrid = 1216;                       // most CTAs of the gradients' norm: eight on each of 152 SMs
+constexpr float kLeastRoot = 0x1p-63f;                // sqrt(2^-126)
+constexpr int kRound = 16384;                          // gradients that a CTA of the norm has in flight
 constexpr uint64_t kMagic = 0x7265736264616d77ull;
 
-// The tensors of one launch. A unit is what one CTA takes: kWarps * passes blocks of one tensor.
+// The tensors of one launch, of one kind: those whose accesses are vectors (everything of a tensor aligned to eight
+// elements) and the others. A unit is what one CTA takes: kWarps * deep blocks of one tensor.
 template <int CAP> struct Table {
     void *w[CAP];
     const void *g[CAP];
@@ -34,8 +43,9 @@ template <int CAP> struct Table {
     float *master[CAP];
     int64_t n[CAP];
     uint32_t first[CAP + 1];      // a tensor's first unit; first[count]: all units
-    uint32_t vec[(CAP + 31) / 32];   // whether everything of a tensor is aligned to four elements
-    int32_t count, passes;
+    int32_t count, vec, deep, pad;
+
+    __host__ __device__ int64_t unit() const { return (int64_t)kWarps * kBlock * deep; }   // elements
 };
 static_assert(sizeof(Table<kLarge>) <= 32000, "the launch's parameters are at most 32764 bytes");
 
@@ -51,158 +61,189 @@ struct Step {
     float step_size;              // lr / (1 - beta1^t)
     float root;                   // 1 / sqrt(1 - beta2^t)
     float eps, decay;             // decay: 1 - lr weight_decay
+    float least;                  // the smallest denominator: of v = 2^-126, with eps
     float lr, wd, lnb1, lnb2, t;  // for the values that the device gives
     const float *lr_dev;
     const int64_t *step_dev;
     const float *grad_scale;
 };
 
-// Eight elements of a warp's block: with VEC lane l has 4 l .. 4 l + 3 of either half (whole sectors for every
-// element size), else l, l + 32, ... below `rem`.
-template <bool VEC> __device__ __forceinline__ int elem(int lane, int j)
+// Eight elements of a warp's block: lane l has the neighbours 8 l .. 8 l + 7 in one access of 8, 16 or 32 bytes (kVec), or
+// l, l + 32, ... one by one (kSingle), below `rem` (kPart).
+enum Mode { kVec, kSingle, kPart };
+template <Mode MODE> __device__ __forceinline__ void load8(const float *p, int lane, int rem, float (&x)[8])
 {
-    return VEC ? (j >> 2) * 128 + lane * 4 + (j & 3) : j * 32 + lane;
-}
-template <bool VEC> __device__ __forceinline__ void load8(const float *p, int lane, int rem, float (&x)[8])
-{
-    if (VEC) {
+    if (MODE == kVec) {
+        asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7])
+                     : "l"(p + lane * 8));
+    } else {
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const float4 u = *reinterpret_cast<const float4 *>(p + k * 128 + lane * 4);
-            x[4 * k] = u.x; x[4 * k + 1] = u.y; x[4 * k + 2] = u.z; x[4 * k + 3] = u.w;
+        for (int j = 0; j < 8; ++j) x[j] = MODE == kSingle || j * 32 + lane < rem ? p[j * 32 + lane] : 0.0f;
+    }
+}
+template <Mode MODE> __device__ __forceinline__ void load8(const __nv_bfloat16 *p, int lane, int rem, float (&x)[8])
+{
+    if (MODE == kVec) {
+        const uint4 u = *reinterpret_cast<const uint4 *>(p + lane * 8);
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = j * 32 + lane < rem ? p[j * 32 + lane] : 0.0f;
+        for (int j = 0; j < 8; ++j) x[j] = MODE == kSingle || j * 32 + lane < rem ? to_f32(p[j * 32 + lane]) : 0.0f;
     }
 }
-template <bool VEC> __device__ __forceinline__ void load8(const __nv_bfloat16 *p, int lane, int rem, float (&x)[8])
+template <Mode MODE> __device__ __forceinline__ void load8(const uint8_t *p, int lane, int rem, float (&x)[8])
 {
-    if (VEC) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const uint2 u = *reinterpret_cast<const uint2 *>(p + k * 128 + lane * 4);
-            x[4 * k] = __uint_as_float(u.x << 16);
-            x[4 * k + 1] = __uint_as_float(u.x & 0xFFFF0000u);
-            x[4 * k + 2] = __uint_as_float(u.y << 16);
-            x[4 * k + 3] = __uint_as_float(u.y & 0xFFFF0000u);
-        }
+    if (MODE == kVec) {
+        const uint2 u = *reinterpret_cast<const uint2 *>(p + lane * 8);
+        const float4 a = from_e4m3x4(u.x), b = from_e4m3x4(u.y);
+        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+        x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = j * 32 + lane < rem ? to_f32(p[j * 32 + lane]) : 0.0f;
+        for (int j = 0; j < 8; ++j) x[j] = MODE == kSingle || j * 32 + lane < rem ? from_e4m3(p[j * 32 + lane]) : 0.0f;
     }
 }
-template <bool VEC> __device__ __forceinline__ void load8(const uint8_t *p, int lane, int rem, float (&x)[8])
+template <Mode MODE> __device__ __forceinline__ void store8(float *p, int lane, int rem, const float (&x)[8])
 {
-    if (VEC) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const float4 u = from_e4m3x4(*reinterpret_cast<const uint32_t *>(p + k * 128 + lane * 4));
-            x[4 * k] = u.x; x[4 * k + 1] = u.y; x[4 * k + 2] = u.z; x[4 * k + 3] = u.w;
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = j * 32 + lane < rem ? from_e4m3(p[j * 32 + lane]) : 0.0f;
-    }
-}
-template <bool VEC> __device__ __forceinline__ void store8(float *p, int lane, int rem, const float (&x)[8])
-{
-    if (VEC) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-            *reinterpret_cast<float4 *>(p + k * 128 + lane * 4) = make_float4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
+    if (MODE == kVec) {
+        asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p + lane * 8), "f"(x[0]), "f"(x[1]), "f"(x[2]),
+                     "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7])
+                     : "memory");
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            if (j * 32 + lane < rem) p[j * 32 + lane] = x[j];
+            if (MODE == kSingle || j * 32 + lane < rem) p[j * 32 + lane] = x[j];
     }
 }
-template <bool VEC> __device__ __forceinline__ void store8(__nv_bfloat16 *p, int lane, int rem, const float (&x)[8])
+template <Mode MODE> __device__ __forceinline__ void store8(__nv_bfloat16 *p, int lane, int rem, const float (&x)[8])
 {
-    if (VEC) {
+    if (MODE == kVec) {
+        uint32_t w[4];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const __nv_bfloat162 a = __floats2bfloat162_rn(x[4 * k], x[4 * k + 1]), b = __floats2bfloat162_rn(x[4 * k + 2], x[4 * k + 3]);
-            *reinterpret_cast<uint2 *>(p + k * 128 + lane * 4) =
-                make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+            w[i] = *reinterpret_cast<const uint32_t *>(&h);
         }
+        *reinterpret_cast<uint4 *>(p + lane * 8) = make_uint4(w[0], w[1], w[2], w[3]);
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            if (j * 32 + lane < rem) p[j * 32 + lane] = from_f32<__nv_bfloat16>(x[j]);
+            if (MODE == kSingle || j * 32 + lane < rem) p[j * 32 + lane] = from_f32<__nv_bfloat16>(x[j]);
     }
 }
 // (values in units of their scale)
-template <bool VEC> __device__ __forceinline__ void store8(uint8_t *p, int lane, int rem, const float (&x)[8])
+template <Mode MODE> __device__ __forceinline__ void store8(uint8_t *p, int lane, int rem, const float (&x)[8])
 {
-    if (VEC) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-            *reinterpret_cast<uint32_t *>(p + k * 128 + lane * 4) = e4m3x4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
+    if (MODE == kVec) {
+        *reinterpret_cast<uint2 *>(p + lane * 8) = make_uint2(e4m3x4(x[0], x[1], x[2], x[3]), e4m3x4(x[4], x[5], x[6], x[7]));
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            if (j * 32 + lane < rem) p[j * 32 + lane] = e4m3x1(x[j]);
+            if (MODE == kSingle || j * 32 + lane < rem) p[j * 32 + lane] = e4m3x1(x[j]);
     }
 }
 
-// One block of 256 elements (or the last `rem` of a tensor) by one warp. The products of the running means are
-// rounded one by one: a fused multiply-add would move values next to a rounding border of e4m3 across it, and
-// the same step would then depend on the compiler's contractions.
-template <typename W, typename G, bool MASTER, int BITS, bool VEC>
-__device__ __forceinline__ void adamw_block(W *w, const G *g, void *mp, void *vp, float *ms, float *vs, float *master,
-                                            int lane, int rem, const Step &h, float c)
+// Root and reciprocal by the approximate instructions (errors under 2^-22), which take normal numbers only
+__device__ __forceinline__ float approx_sqrt(float v)
+{
+    float r;
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float approx_rcp(float v)
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+
+// K blocks of 256 elements by one warp, kWarps blocks apart (or one, the last `rem` of a tensor). The products of the
+// running means are rounded one by one: a fused multiply-add would move values next to a rounding border of e4m3 across
+// it, and the same step would then depend on the compiler's contractions. The root and the quotient m / (sqrt(v) ..) are
+// approximate, far below what the update is to the weight. A v below 2^-126 (gradients below 1e-17) counts as that for
+// the weight (`least` is its denominator), as zero for the 8-bit state.
+// The 8-bit form is bound by instructions as much as by memory (10 bytes an element): with IEEE roots and quotients, one
+// value an instruction and one block a warp 75 of them an element, 868 us for 308 M elements; with pairs and approximate
+// ones 52 and 597.
+template <typename W, typename G, bool MASTER, int BITS, Mode MODE, int K>
+__device__ __forceinline__ void adamw_blocks(W *w, const G *g, void *mp, void *vp, float *ms, float *vs, float *master,
+                                             int lane, int rem, const Step &h, float c)
 {
     using S = typename std::conditional<BITS == 8, uint8_t, float>::type;
+    constexpr int kNext = kWarps * kBlock;
     S *const m8 = static_cast<S *>(mp), *const v8 = static_cast<S *>(vp);
-    float x[8], dg[8], m[8], v[8];
-    if (MASTER) load8<VEC>(static_cast<const float *>(master), lane, rem, x);
-    else load8<VEC>(static_cast<const W *>(w), lane, rem, x);
-    load8<VEC>(g, lane, rem, dg);
-    load8<VEC>(static_cast<const S *>(m8), lane, rem, m);
-    load8<VEC>(static_cast<const S *>(v8), lane, rem, v);
-    float sm = 1.0f, sv = 1.0f;
-    if (BITS == 8) {
-        sm = *ms;
-        sv = *vs;
-    }
-    uint32_t am = 0, av = 0;   // the largest |m| and sqrt(v), as bits
+    float x[K][8], dg[K][8], m[K][8], v[K][8];
+    float sm[K], sv[K];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const float gj = __fmul_rn(dg[j], c);
+    for (int k = 0; k < K; ++k) {
         if (BITS == 8) {
-            m[j] = __fmul_rn(m[j], sm);
-            v[j] = __fmul_rn(v[j], sv);
-            v[j] = __fmul_rn(v[j], v[j]);
+            sm[k] = ms[k * kWarps];
+            sv[k] = vs[k * kWarps];
         }
-        m[j] = __fadd_rn(__fmul_rn(m[j], h.b1), __fmul_rn(gj, h.omb1));
-        v[j] = __fadd_rn(__fmul_rn(v[j], h.b2), __fmul_rn(__fmul_rn(gj, gj), h.omb2));
-        const float r = __fsqrt_rn(v[j]);
-        x[j] = fmaf(-h.step_size, m[j] / fmaf(r, h.root, h.eps), x[j] * h.decay);
-        if (BITS == 8) {
-            v[j] = r;
-            am = max(am, abs_bits(m[j]));
-            av = max(av, abs_bits(r));
-        }
+        load8<MODE>(static_cast<const S *>(m8 + k * kNext), lane, rem, m[k]);
+        load8<MODE>(static_cast<const S *>(v8 + k * kNext), lane, rem, v[k]);
+        load8<MODE>(g + k * kNext, lane, rem, dg[k]);
+        if (MASTER) load8<MODE>(static_cast<const float *>(master + k * kNext), lane, rem, x[k]);
+        else load8<MODE>(static_cast<const W *>(w + k * kNext), lane, rem, x[k]);
     }
-    if (MASTER) store8<VEC>(master, lane, rem, x);
-    store8<VEC>(w, lane, rem, x);
-    if (BITS == 8) {
-        const E4m3Scale a = e4m3_scale(__reduce_max_sync(0xffffffffu, am)), b = e4m3_scale(__reduce_max_sync(0xffffffffu, av));
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            m[j] = __fmul_rn(m[j], a.inv);
-            // a sqrt(v) above zero keeps a code above zero (and a NaN stays one)
-            const float r = __fmul_rn(v[j], b.inv);
-            v[j] = v[j] > 0.0f && r < kE4m3Least ? kE4m3Least : r;
+    for (int k = 0; k < K; ++k) {
+        float am = 0.0f, av = 0.0f;   // the largest |m| and sqrt(v)
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+            const Pair g2 = pair(dg[k][j], dg[k][j + 1]) * both(c);
+            Pair m2 = pair(m[k][j], m[k][j + 1]), v2 = pair(v[k][j], v[k][j + 1]);
+            if (BITS == 8) {
+                m2 = m2 * both(sm[k]);
+                v2 = v2 * both(sv[k]);
+                v2 = v2 * v2;
+            }
+            m2 = m2 * both(h.b1) + g2 * both(h.omb1);
+            v2 = v2 * both(h.b2) + (g2 * g2) * both(h.omb2);
+            float m0, m1, v0, v1, d0, d1;
+            split(m2, m0, m1);
+            split(v2, v0, v1);
+            const float r0 = approx_sqrt(v0), r1 = approx_sqrt(v1);
+            split(fma(pair(r0, r1), both(h.root), both(h.eps)), d0, d1);
+            const Pair q = m2 * pair(approx_rcp(max_nan(d0, h.least)), approx_rcp(max_nan(d1, h.least)));
+            split(fma(q, both(-h.step_size), pair(x[k][j], x[k][j + 1]) * both(h.decay)), x[k][j], x[k][j + 1]);
+            m[k][j] = m0;
+            m[k][j + 1] = m1;
+            v[k][j] = BITS == 8 ? r0 : v0;
+            v[k][j + 1] = BITS == 8 ? r1 : v1;
+            if (BITS == 8) {
+                am = max_nan(am, max_nan(fabsf(m0), fabsf(m1)));
+                av = max_nan(av, max_nan(r0, r1));
+            }
         }
-        if (lane == 0) {
-            *ms = a.scale;
-            *vs = b.scale;
+        if (MASTER) store8<MODE>(master + k * kNext, lane, rem, x[k]);
+        store8<MODE>(w + k * kNext, lane, rem, x[k]);
+        if (BITS == 8) {
+            const E4m3Scale a = e4m3_scale(__reduce_max_sync(0xffffffffu, abs_bits(am))), b = e4m3_scale(__reduce_max_sync(0xffffffffu, abs_bits(av)));
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) {
+                // a sqrt(v) above zero (at least 2^-63 then) keeps a code above zero
+                float l0, l1;
+                split(pair(v[k][j], v[k][j + 1]) * both(0x1p60f), l0, l1);
+                split(pair(m[k][j], m[k][j + 1]) * both(a.inv), m[k][j], m[k][j + 1]);
+                split(pair(v[k][j], v[k][j + 1]) * both(b.inv), v[k][j], v[k][j + 1]);
+                v[k][j] = max_nan(v[k][j], fminf(l0, kE4m3Least));
+                v[k][j + 1] = max_nan(v[k][j + 1], fminf(l1, kE4m3Least));
+            }
+            if (lane == 0) {
+                ms[k * kWarps] = a.scale;
+                vs[k * kWarps] = b.scale;
+            }
         }
+        store8<MODE>(m8 + k * kNext, lane, rem, m[k]);
+        store8<MODE>(v8 + k * kNext, lane, rem, v[k]);
     }
-    store8<VEC>(m8, lane, rem, m);
-    store8<VEC>(v8, lane, rem, v);
 }
 
 // The tensor that unit `u` belongs to
@@ -217,15 +258,14 @@ template <int CAP> __device__ __forceinline__ int tensor_of(const Table<CAP> &ta
     return lo;
 }
 
-template <typename W, typename G, bool MASTER, int BITS, int CAP>
-__global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ Table<CAP> tab, const __grid_constant__ Step given)
+template <typename W, typename G, bool MASTER, int BITS, bool VEC, int CAP>
+__global__ void __launch_bounds__(kThreads, VEC && BITS == 8 ? MINB : 1) k_adamw(const __grid_constant__ Table<CAP> tab, const __grid_constant__ Step given)
 {
     Step h = given;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int i = tensor_of(tab, blockIdx.x);
     const int64_t n = tab.n[i];
-    int64_t b = (int64_t)(blockIdx.x - tab.first[i]) * tab.passes * kWarps + warp;
-    const bool vec = (tab.vec[i >> 5] >> (i & 31)) & 1u;
+    int64_t b = (int64_t)(blockIdx.x - tab.first[i]) * tab.deep * kWarps + warp;
     griddep_wait();
     griddep_launch_dependents();
     float c = 1.0f;
@@ -239,23 +279,89 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ Tabl
         h.step_size = lr / -expm1f(t * h.lnb1);
         h.root = 1.0f / sqrtf(-expm1f(t * h.lnb2));
         h.decay = 1.0f - lr * h.wd;
+        h.least = fmaf(h.root, kLeastRoot, h.eps);
     }
-    for (int p = 0; p < tab.passes; ++p, b += kWarps) {
+    W *const w = static_cast<W *>(tab.w[i]);
+    const G *const g = static_cast<const G *>(tab.g[i]);
+    char *const m = static_cast<char *>(tab.m[i]), *const v = static_cast<char *>(tab.v[i]);
+    float *const ms = tab.ms[i], *const vs = tab.vs[i], *const master = tab.master[i];
+    constexpr int ss = BITS / 8, K = VEC ? deep_of(BITS) : 1;
+    auto run = [&](auto mode, auto deep, int rem) {
         const int64_t at = b * kBlock;
-        if (at >= n) return;
-        const int rem = n - at < kBlock ? (int)(n - at) : kBlock;
-        W *const w = static_cast<W *>(tab.w[i]) + at;
-        const G *const g = static_cast<const G *>(tab.g[i]) + at;
-        char *const m = static_cast<char *>(tab.m[i]) + at * (BITS / 8), *const v = static_cast<char *>(tab.v[i]) + at * (BITS / 8);
-        float *const ms = BITS == 8 ? tab.ms[i] + b : nullptr, *const vs = BITS == 8 ? tab.vs[i] + b : nullptr;
-        float *const master = MASTER ? tab.master[i] + at : nullptr;
-        if (vec && rem == kBlock) adamw_block<W, G, MASTER, BITS, true>(w, g, m, v, ms, vs, master, lane, rem, h, c);
-        else adamw_block<W, G, MASTER, BITS, false>(w, g, m, v, ms, vs, master, lane, rem, h, c);
+        adamw_blocks<W, G, MASTER, BITS, (Mode)decltype(mode)::value, decltype(deep)::value>(
+            w + at, g + at, m + at * ss, v + at * ss, ms + b, vs + b, master + at, lane, rem, h, c);
+    };
+    using std::integral_constant;
+    if (b * kBlock + ((K - 1) * kWarps + 1) * kBlock <= n) {
+        run(integral_constant<int, VEC ? kVec : kSingle>(), integral_constant<int, K>(), kBlock);
+        return;
+    }
+    for (int k = 0; k < K; ++k, b += kWarps) {   // the end of a tensor
+        const int64_t rem = n - b * kBlock;
+        if (rem <= 0) return;
+        if (VEC && rem >= kBlock) run(integral_constant<int, kVec>(), integral_constant<int, 1>(), kBlock);
+        else run(integral_constant<int, kPart>(), integral_constant<int, 1>(), (int)min(rem, (int64_t)kBlock));
     }
 }
 
-// The sum of squares of the gradients of a CTA's share of the units (an even run of them), in 64 bits from a thread's
-// share of one unit on.
+// Sum of squares of g[from .. to) by a CTA, this thread's share: 16-byte loads, eight in flight, from the first element on
+// whose address is a multiple of 16; in 64 bits from one round of loads on.
+template <typename G> __device__ __forceinline__ double squares(const G *g, int64_t from, int64_t to)
+{
+    constexpr int V = 16 / (int)sizeof(G), kDeep = 8;
+    double sum = 0.0;
+    const int64_t head = min(to, from + (int64_t)((16 - reinterpret_cast<uintptr_t>(g + from) % 16) % 16 / sizeof(G)));
+    const int64_t vectors = (to - head) / V;
+    const uint4 *const p = reinterpret_cast<const uint4 *>(g + head);
+    auto add = [](uint4 u, float &s) {
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (sizeof(G) == 2) {
+                const float a = __uint_as_float(w[i] << 16), b = __uint_as_float(w[i] & 0xFFFF0000u);
+                s = fmaf(a, a, s);
+                s = fmaf(b, b, s);
+            } else {
+                const float a = __uint_as_float(w[i]);
+                s = fmaf(a, a, s);
+            }
+        }
+    };
+    int64_t k = threadIdx.x;
+    for (; k + (kDeep - 1) * kThreads < vectors; k += kDeep * kThreads) {
+        uint4 u[kDeep];
+        float s[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < kDeep; ++j) u[j] = p[k + j * kThreads];
+#pragma unroll
+        for (int j = 0; j < kDeep; ++j) add(u[j], s[j & 1]);
+        sum += (double)(s[0] + s[1]);
+    }
+    float s = 0.0f;
+    if (k < vectors) {
+        uint4 u[kDeep];
+        float a[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < kDeep; ++j) u[j] = k + j * kThreads < vectors ? p[k + j * kThreads] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int j = 0; j < kDeep; ++j) add(u[j], a[j & 1]);
+        sum += (double)(a[0] + a[1]);
+    }
+    // the elements before the first vector and behind the last
+    if (from + threadIdx.x < head) {
+        const float a = to_f32(g[from + threadIdx.x]);
+        s = fmaf(a, a, s);
+    }
+    const int64_t tail = head + vectors * V + threadIdx.x;
+    if (tail < to) {
+        const float a = to_f32(g[tail]);
+        s = fmaf(a, a, s);
+    }
+    return sum + (double)s;
+}
+
+// The sum of squares of the gradients of a CTA's share of the units, an even run of them: what it has of each tensor is
+// one contiguous piece.
 template <typename G, int CAP>
 __global__ void __launch_bounds__(kThreads) k_grad_squares(const __grid_constant__ Table<CAP> tab, double *__restrict__ part)
 {
@@ -266,26 +372,12 @@ __global__ void __launch_bounds__(kThreads) k_grad_squares(const __grid_constant
     const uint64_t units = tab.first[tab.count];
     uint32_t u = (uint32_t)(units * blockIdx.x / gridDim.x);
     const uint32_t end = (uint32_t)(units * (blockIdx.x + 1) / gridDim.x);
+    const int64_t per = tab.unit();
     double sum = 0.0;
-    int i = tensor_of(tab, u);
-    for (; u < end; ++u) {
-        while (u >= tab.first[i + 1]) ++i;
-        const int64_t n = tab.n[i];
-        const bool vec = (tab.vec[i >> 5] >> (i & 31)) & 1u;
-        const G *const g = static_cast<const G *>(tab.g[i]);
-        int64_t b = (int64_t)(u - tab.first[i]) * tab.passes * kWarps + warp;
-        float s = 0.0f;
-        for (int p = 0; p < tab.passes; ++p, b += kWarps) {
-            const int64_t at = b * kBlock;
-            if (at >= n) break;
-            const int rem = n - at < kBlock ? (int)(n - at) : kBlock;
-            float x[8];
-            if (vec && rem == kBlock) load8<true>(g + at, lane, rem, x);
-            else load8<false>(g + at, lane, rem, x);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) s = fmaf(x[j], x[j], s);
-        }
-        sum += (double)s;
+    for (int i = tensor_of(tab, u); u < end; ++i) {
+        const uint32_t stop = min(end, tab.first[i + 1]);
+        sum += squares(static_cast<const G *>(tab.g[i]), (int64_t)(u - tab.first[i]) * per, min((int64_t)(stop - tab.first[i]) * per, tab.n[i]));
+        u = stop;
     }
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if (lane == 0) sums[warp] = sum;
@@ -296,18 +388,19 @@ __global__ void __launch_bounds__(kThreads) k_grad_squares(const __grid_constant
     }
 }
 
-__global__ void __launch_bounds__(kThreads) k_grad_norm(const double *__restrict__ part, int64_t parts, float max_norm, float *__restrict__ out)
+constexpr int kNormThreads = 1024;
+__global__ void __launch_bounds__(kNormThreads) k_grad_norm(const double *__restrict__ part, int64_t parts, float max_norm, float *__restrict__ out)
 {
-    __shared__ double sums[kWarps];
+    __shared__ double sums[kNormThreads / 32];
     griddep_wait();
     griddep_launch_dependents();
     double sum = 0.0;
-    for (int64_t k = threadIdx.x; k < parts; k += kThreads) sum += part[k];
+    for (int64_t k = threadIdx.x; k < parts; k += kNormThreads) sum += part[k];
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = sum;
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int k = 1; k < kWarps; ++k) sum += sums[k];
+        for (int k = 1; k < kNormThreads / 32; ++k) sum += sums[k];
         const float norm = (float)sqrt(sum);
         out[0] = norm;
         out[1] = !isfinite(norm) ? __int_as_float(0x7fffffff) : max_norm > 0.0f ? fminf(1.0f, max_norm / (norm + 1e-6f)) : 1.0f;
@@ -326,59 +419,69 @@ const void *table_at(const Plan &p, int64_t k)
 {
     return reinterpret_cast<const char *>(&p + 1) + (size_t)k * table_bytes(p);
 }
-template <int CAP> uint32_t units_of(const void *t)
+struct Extent {
+    uint32_t units;
+    int64_t unit;   // elements
+    bool vec;
+};
+template <int CAP> Extent extent_of(const void *t)
 {
     const Table<CAP> &tab = *static_cast<const Table<CAP> *>(t);
-    return tab.first[tab.count];
+    return {tab.first[tab.count], tab.unit(), tab.vec != 0};
 }
-uint32_t units_at(const Plan &p, int64_t k)
+Extent extent_at(const Plan &p, int64_t k)
 {
-    return p.small ? units_of<kSmall>(table_at(p, k)) : units_of<kLarge>(table_at(p, k));
+    return p.small ? extent_of<kSmall>(table_at(p, k)) : extent_of<kLarge>(table_at(p, k));
 }
 
 struct Span {
     uintptr_t lo, hi;
     bool out;
 };
-int64_t tables_for(int64_t count) { return (count + kLarge - 1) / kLarge; }
+// (either kind of tensors may end in a table that is not full)
 size_t plan_size(int64_t count)
 {
-    const size_t tables = count <= kSmall ? sizeof(Table<kSmall>) : (size_t)tables_for(count) * sizeof(Table<kLarge>);
+    const size_t tables = count <= kSmall ? 2 * sizeof(Table<kSmall>) : (size_t)((count + kLarge - 1) / kLarge + 1) * sizeof(Table<kLarge>);
     return sizeof(Plan) + tables + (size_t)count * 7 * sizeof(Span);   // (the spans: scratch of the overlap check)
 }
 bool count_ok(int64_t count) { return count >= 0 && count <= (int64_t(1) << 24); }
 
-// Fills the tables with the tensors that have elements. passes: the blocks that a warp takes one after the other.
-template <int CAP> int64_t lay_out(const resbm_adamw_desc &d, const resbm_adamw_tensor *tensors, int64_t count, int passes, Table<CAP> *tabs)
+// Whether everything of a tensor is aligned to eight elements
+bool is_vec(const resbm_adamw_desc &d, const resbm_adamw_tensor &x)
 {
-    const size_t ws = d.w_dtype == RESBM_BF16 ? 2 : 4, gs = d.g_dtype == RESBM_BF16 ? 2 : 4;
-    const size_t ss = d.state == RESBM_STATE_E4M3 ? 1 : 4;
-    Table<CAP> *t = nullptr;
+    const size_t ws = d.w_dtype == RESBM_BF16 ? 16 : 32, gs = d.g_dtype == RESBM_BF16 ? 16 : 32, ss = d.state == RESBM_STATE_E4M3 ? 8 : 32;
+    if (!ptr_ok(x.g, gs, true)) return false;
+    return d.state == RESBM_STATE_NONE || (ptr_ok(x.w, ws, true) && ptr_ok(x.m, ss, true) && ptr_ok(x.v, ss, true) && ptr_ok(x.master, 32, false));
+}
+
+// Fills the tables with the tensors that have elements, one kind after the other.
+template <int CAP> int64_t lay_out(const resbm_adamw_desc &d, const resbm_adamw_tensor *tensors, int64_t count, Table<CAP> *tabs)
+{
     int64_t tables = 0;
-    for (int64_t i = 0; i < count; ++i) {
-        const resbm_adamw_tensor &x = tensors[i];
-        if (x.n == 0) continue;
-        if (!t || t->count == CAP) {
-            t = tabs + tables++;
-            memset(t, 0, sizeof *t);
-            t->passes = passes;
+    for (int vec = 1; vec >= 0; --vec) {
+        Table<CAP> *t = nullptr;
+        for (int64_t i = 0; i < count; ++i) {
+            const resbm_adamw_tensor &x = tensors[i];
+            if (x.n == 0 || is_vec(d, x) != (vec != 0)) continue;
+            if (!t || t->count == CAP) {
+                t = tabs + tables++;
+                memset(t, 0, sizeof *t);
+                t->vec = vec;
+                t->deep = vec && d.state != RESBM_STATE_NONE ? deep_of(d.state) : 1;
+            }
+            const int k = t->count++;
+            t->g[k] = x.g;
+            t->n[k] = x.n;
+            if (d.state != RESBM_STATE_NONE) {
+                t->w[k] = x.w;
+                t->m[k] = x.m;
+                t->v[k] = x.v;
+                t->ms[k] = x.m_scale;
+                t->vs[k] = x.v_scale;
+                t->master[k] = x.master;
+            }
+            t->first[k + 1] = t->first[k] + (uint32_t)((x.n + t->unit() - 1) / t->unit());
         }
-        const int k = t->count++;
-        t->g[k] = x.g;
-        t->n[k] = x.n;
-        bool vec = ptr_ok(x.g, 4 * gs, true);
-        if (d.state != RESBM_STATE_NONE) {
-            t->w[k] = x.w;
-            t->m[k] = x.m;
-            t->v[k] = x.v;
-            t->ms[k] = x.m_scale;
-            t->vs[k] = x.v_scale;
-            t->master[k] = x.master;
-            vec = vec && ptr_ok(x.w, 4 * ws, true) && ptr_ok(x.m, 4 * ss, true) && ptr_ok(x.v, 4 * ss, true) && ptr_ok(x.master, 16, false);
-        }
-        if (vec) t->vec[k >> 5] |= 1u << (k & 31);
-        const int64_t per = (int64_t)passes * kWarps * kBlock;
-        t->first[k + 1] = t->first[k] + (uint32_t)((x.n + per - 1) / per);
     }
     return tables;
 }
@@ -404,16 +507,21 @@ resbm_status launch_table(const void *kernel, const Plan &p, int64_t k, unsigned
     return RESBM_OK;
 }
 
-template <typename W, typename G, bool MASTER> const void *adamw_kernel(const Plan &p)
+template <typename W, typename G, bool MASTER, int BITS> const void *adamw_kernel(const Plan &p, bool vec)
 {
-    if (p.state == RESBM_STATE_E4M3)
-        return p.small ? (const void *)k_adamw<W, G, MASTER, 8, kSmall> : (const void *)k_adamw<W, G, MASTER, 8, kLarge>;
-    return p.small ? (const void *)k_adamw<W, G, MASTER, 32, kSmall> : (const void *)k_adamw<W, G, MASTER, 32, kLarge>;
+    if (vec) return p.small ? (const void *)k_adamw<W, G, MASTER, BITS, true, kSmall> : (const void *)k_adamw<W, G, MASTER, BITS, true, kLarge>;
+    return p.small ? (const void *)k_adamw<W, G, MASTER, BITS, false, kSmall> : (const void *)k_adamw<W, G, MASTER, BITS, false, kLarge>;
 }
-template <typename G> const void *adamw_kernel(const Plan &p)
+template <typename W, typename G, bool MASTER> const void *adamw_kernel(const Plan &p, bool vec)
+{
+    return p.state == RESBM_STATE_E4M3 ? adamw_kernel<W, G, MASTER, 8>(p, vec) : adamw_kernel<W, G, MASTER, 32>(p, vec);
+}
+template <typename G> const void *adamw_kernel(const Plan &p, bool vec)
 {
     using bf = __nv_bfloat16;
-    return p.w_dtype == RESBM_F32 ? adamw_kernel<float, G, false>(p) : p.master ? adamw_kernel<bf, G, true>(p) : adamw_kernel<bf, G, false>(p);
+    return p.w_dtype == RESBM_F32 ? adamw_kernel<float, G, false>(p, vec)
+           : p.master             ? adamw_kernel<bf, G, true>(p, vec)
+                                  : adamw_kernel<bf, G, false>(p, vec);
 }
 template <typename G> const void *squares_kernel(const Plan &p)
 {
@@ -423,7 +531,12 @@ template <typename G> const void *squares_kernel(const Plan &p)
 bool dtype_ok(int32_t t) { return t == RESBM_F32 || t == RESBM_BF16; }
 bool finite_nonneg(double x) { return x >= 0.0 && x < HUGE_VAL; }
 
-unsigned norm_grid(const Plan &p, int64_t k) { return std::min<unsigned>(units_at(p, k), kNormGrid); }
+// CTAs of the gradients' norm: a round of loads for each, up to kNormGrid
+unsigned norm_grid(const Plan &p, int64_t k)
+{
+    const Extent x = extent_at(p, k);
+    return (unsigned)std::min<int64_t>((x.units * x.unit + kRound - 1) / kRound, kNormGrid);
+}
 // The partial sums of `count` plans, or -1 where one of them is none
 int64_t norm_parts(const void *const *plans, int64_t count)
 {
@@ -509,9 +622,8 @@ resbm_status resbm_adamw_plan(const resbm_adamw_desc *desc, const resbm_adamw_te
     out->state = d.state;
     out->master = masters > 0;
     out->pad = 0;
-    const int passes = 1;
-    out->tables = out->small ? lay_out(d, tensors, count, passes, reinterpret_cast<Table<kSmall> *>(out + 1))
-                             : lay_out(d, tensors, count, passes, reinterpret_cast<Table<kLarge> *>(out + 1));
+    out->tables = out->small ? lay_out(d, tensors, count, reinterpret_cast<Table<kSmall> *>(out + 1))
+                             : lay_out(d, tensors, count, reinterpret_cast<Table<kLarge> *>(out + 1));
     out->magic = kMagic;
     return RESBM_OK;
 }
@@ -539,14 +651,17 @@ resbm_status resbm_adamw_step(const void *plan, const resbm_adamw_hyper *hyper, 
     h.root = (float)(1.0 / sqrt(-expm1(t * log(a.beta2))));
     h.eps = (float)a.eps;
     h.decay = (float)(1.0 - a.lr * a.weight_decay);
+    h.least = h.root * kLeastRoot + h.eps;
     h.lr = (float)a.lr;
     h.wd = (float)a.weight_decay;
     h.t = (float)t;
     h.lr_dev = a.lr_dev;
     h.step_dev = a.step_dev;
     h.grad_scale = a.grad_scale;
-    const void *kernel = p->g_dtype == RESBM_F32 ? adamw_kernel<float>(*p) : adamw_kernel<__nv_bfloat16>(*p);
-    for (int64_t k = 0; s == RESBM_OK && k < p->tables; ++k) s = launch_table(kernel, *p, k, units_at(*p, k), &h, c);
+    for (int64_t k = 0; s == RESBM_OK && k < p->tables; ++k) {
+        const Extent x = extent_at(*p, k);
+        s = launch_table(p->g_dtype == RESBM_F32 ? adamw_kernel<float>(*p, x.vec) : adamw_kernel<__nv_bfloat16>(*p, x.vec), *p, k, x.units, &h, c);
+    }
     return s;
 }
 
@@ -579,7 +694,7 @@ resbm_status resbm_grad_norm(const void *const *plans, int64_t count, float max_
         }
     }
     if (s != RESBM_OK) return s;
-    const cudaError_t e = launch_pdl(k_grad_norm, dim3(1), dim3(kThreads), 0, c, static_cast<const double *>(ws), parts, max_norm, out);
+    const cudaError_t e = launch_pdl(k_grad_norm, dim3(1), dim3(kNormThreads), 0, c, static_cast<const double *>(ws), parts, max_norm, out);
     if (e == cudaSuccess) count_launches(1);
     return finish(e);
 }

@@ -10,6 +10,7 @@
 #include "abi.h"
 #include "common.cuh"
 #include "fp8.cuh"
+#include "pair.cuh"
 #include "resbm_train.h"
 
 namespace resbm {
@@ -21,60 +22,89 @@ struct NormArgs {
     uint8_t *Q;
     float *S;
     int64_t T, ldx, lda, ldh, ldn, groups;
-    int d, group;                 // group: columns behind a scale, a power of two >= 32, or > d for the whole row
+    int d, group_log;             // columns behind a scale, as a power of two >= 32; 30 (over every d) for the whole row
     float eps, inv_d;
 };
 
+template <int V> __device__ __forceinline__ void scale_by(float (&f)[V], float c)
+{
+    if constexpr (V > 1) {
+#pragma unroll
+        for (int i = 0; i < V; i += 2) split(pair(f[i], f[i + 1]) * both(c), f[i], f[i + 1]);
+    } else {
+        f[0] *= c;
+    }
+}
+
 // V neighbouring elements, as loaded
-template <typename E, int V> struct Vec;
-template <> struct Vec<__nv_bfloat16, 8> {
-    uint4 u;
-    __device__ __forceinline__ void load(const __nv_bfloat16 *p) { u = *reinterpret_cast<const uint4 *>(p); }
-    __device__ __forceinline__ void zero() { u = make_uint4(0u, 0u, 0u, 0u); }
-    __device__ __forceinline__ void get(float (&f)[8]) const
+template <typename E, int V> struct Vec {
+    static constexpr int kWords = V * (int)sizeof(E) / 4;   // 4
+    uint32_t w[kWords];
+
+    __device__ __forceinline__ void load(const E *p)
     {
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            f[2 * i] = __uint_as_float(w[i] << 16);
-            f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-        }
+        const uint4 u = *reinterpret_cast<const uint4 *>(p);
+        w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
     }
-    __device__ __forceinline__ void put(const float (&f)[8])
+    __device__ __forceinline__ void zero() { w[0] = w[1] = w[2] = w[3] = 0u; }
+    __device__ __forceinline__ void store(E *p) const { *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]); }
+    // elements 2 i and 2 i + 1
+    __device__ __forceinline__ Pair get(int i) const
     {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+        if constexpr (sizeof(E) == 2) return pair(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
+        else return pair(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+    }
+    __device__ __forceinline__ void set(int i, Pair f)
+    {
+        float a, b;
+        split(f, a, b);
+        if constexpr (sizeof(E) == 2) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
             w[i] = *reinterpret_cast<const uint32_t *>(&h);
+        } else {
+            w[2 * i] = __float_as_uint(a);
+            w[2 * i + 1] = __float_as_uint(b);
         }
-        u = make_uint4(w[0], w[1], w[2], w[3]);
     }
-    __device__ __forceinline__ void store(__nv_bfloat16 *p) const { *reinterpret_cast<uint4 *>(p) = u; }
-    static __device__ __forceinline__ void codes(uint8_t *q, const float (&f)[8])
+    __device__ __forceinline__ void add(const Vec &o)
     {
-        *reinterpret_cast<uint2 *>(q) = make_uint2(e4m3x4(f[0], f[1], f[2], f[3]), e4m3x4(f[4], f[5], f[6], f[7]));
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) set(i, get(i) + o.get(i));
     }
-};
-template <> struct Vec<float, 4> {
-    float4 u;
-    __device__ __forceinline__ void load(const float *p) { u = *reinterpret_cast<const float4 *>(p); }
-    __device__ __forceinline__ void zero() { u = make_float4(0.0f, 0.0f, 0.0f, 0.0f); }
-    __device__ __forceinline__ void get(float (&f)[4]) const { f[0] = u.x; f[1] = u.y; f[2] = u.z; f[3] = u.w; }
-    __device__ __forceinline__ void put(const float (&f)[4]) { u = make_float4(f[0], f[1], f[2], f[3]); }
-    __device__ __forceinline__ void store(float *p) const { *reinterpret_cast<float4 *>(p) = u; }
-    static __device__ __forceinline__ void codes(uint8_t *q, const float (&f)[4])
+    __device__ __forceinline__ float squares() const
     {
-        *reinterpret_cast<uint32_t *>(q) = e4m3x4(f[0], f[1], f[2], f[3]);
+        Pair s = both(0.0f);
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) s = fma(get(i), get(i), s);
+        float a, b;
+        split(s, a, b);
+        return a + b;
+    }
+    __device__ __forceinline__ void scaled(float c, const Vec &g, float (&f)[V]) const
+    {
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) split(get(i) * both(c) * g.get(i), f[2 * i], f[2 * i + 1]);
+    }
+    __device__ __forceinline__ void put(const float (&f)[V])
+    {
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) set(i, pair(f[2 * i], f[2 * i + 1]));
+    }
+    static __device__ __forceinline__ void codes(uint8_t *q, const float (&f)[V])
+    {
+        if constexpr (V == 8) *reinterpret_cast<uint2 *>(q) = make_uint2(e4m3x4(f[0], f[1], f[2], f[3]), e4m3x4(f[4], f[5], f[6], f[7]));
+        else *reinterpret_cast<uint32_t *>(q) = e4m3x4(f[0], f[1], f[2], f[3]);
     }
 };
 template <typename E> struct Vec<E, 1> {
     E u;
     __device__ __forceinline__ void load(const E *p) { u = *p; }
     __device__ __forceinline__ void zero() { u = from_f32<E>(0.0f); }
-    __device__ __forceinline__ void get(float (&f)[1]) const { f[0] = to_f32(u); }
-    __device__ __forceinline__ void put(const float (&f)[1]) { u = from_f32<E>(f[0]); }
     __device__ __forceinline__ void store(E *p) const { *p = u; }
+    __device__ __forceinline__ void add(const Vec &o) { u = from_f32<E>(to_f32(u) + to_f32(o.u)); }
+    __device__ __forceinline__ float squares() const { return to_f32(u) * to_f32(u); }
+    __device__ __forceinline__ void scaled(float c, const Vec &g, float (&f)[1]) const { f[0] = to_f32(u) * c * to_f32(g.u); }
+    __device__ __forceinline__ void put(const float (&f)[1]) { u = from_f32<E>(f[0]); }
     static __device__ __forceinline__ void codes(uint8_t *q, const float (&f)[1]) { *q = e4m3x1(f[0]); }
 };
 
@@ -102,6 +132,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) k_add_norm(const __grid
             if (q < nv) h[k].load(x + q * V);
             else h[k].zero();
         }
+        float s = 0.0f;
         if (p.A) {
             const E *const a = static_cast<const E *>(p.A) + t * p.lda;
 #pragma unroll
@@ -110,22 +141,11 @@ __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) k_add_norm(const __grid
                 if (q < nv) b[k].load(a + q * V);
                 else b[k].zero();
             }
+#pragma unroll
+            for (int k = 0; k < KV; ++k) h[k].add(b[k]);
         }
-        float s = 0.0f;
 #pragma unroll
-        for (int k = 0; k < KV; ++k) {
-            float f[V], g[V];
-            h[k].get(f);
-            if (p.A) {
-                b[k].get(g);
-#pragma unroll
-                for (int i = 0; i < V; ++i) f[i] += g[i];
-                h[k].put(f);
-                h[k].get(f);   // (the norm is taken of h as stored)
-            }
-#pragma unroll
-            for (int i = 0; i < V; ++i) s = fmaf(f[i], f[i], s);
-        }
+        for (int k = 0; k < KV; ++k) s += h[k].squares();   // (of h as stored)
         if (p.H) {
             E *const o = static_cast<E *>(p.H) + t * p.ldh;
 #pragma unroll
@@ -152,13 +172,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) k_add_norm(const __grid
         const float rstd = 1.0f / sqrtf(s + p.eps);
         float n[KV][V];
 #pragma unroll
-        for (int k = 0; k < KV; ++k) {
-            float f[V], g[V];
-            h[k].get(f);
-            b[k].get(g);
-#pragma unroll
-            for (int i = 0; i < V; ++i) n[k][i] = f[i] * rstd * g[i];
-        }
+        for (int k = 0; k < KV; ++k) h[k].scaled(rstd, b[k], n[k]);
         if (p.N) {
             E *const o = static_cast<E *>(p.N) + t * p.ldn;
 #pragma unroll
@@ -172,19 +186,20 @@ __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) k_add_norm(const __grid
         if (p.Q) {
             // the largest |n| of a group: over the lanes that share it, then, where a group has more than a warp's
             // vectors, over the 32-vector pieces that the warps left in shared memory (a warp's own in registers)
-            const int lanes = p.group / V;   // (>= 32 for the whole row)
+            const int lanes_log = p.group_log - (V == 8 ? 3 : V == 4 ? 2 : 0);
             uint32_t am[KV];
 #pragma unroll
             for (int k = 0; k < KV; ++k) {
-                am[k] = 0;
+                float m = fabsf(n[k][0]);
 #pragma unroll
-                for (int i = 0; i < V; ++i) am[k] = max(am[k], abs_bits(n[k][i]));
+                for (int i = 1; i < V; ++i) m = max_nan(m, fabsf(n[k][i]));
+                am[k] = __float_as_uint(m) & 0x7FFFFFFFu;
             }
-            if (lanes >= 32) {
+            if (lanes_log >= 5) {
 #pragma unroll
                 for (int k = 0; k < KV; ++k) am[k] = __reduce_max_sync(0xffffffffu, am[k]);
-                const int pieces = lanes >> 5;
-                if (pieces > 1) {
+                const int pieces_log = lanes_log - 5;
+                if (pieces_log > 0) {
                     if (kW > 1) {
                         if (lane == 0)
 #pragma unroll
@@ -192,7 +207,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) k_add_norm(const __grid
                         __syncthreads();
 #pragma unroll
                         for (int k = 0; k < KV; ++k) {
-                            const int c0 = (k * kW + warp) / pieces * pieces, c1 = min(c0 + pieces, KV * kW);
+                            const int c0 = (k * kW + warp) >> pieces_log << pieces_log, c1 = min(c0 + (1 << pieces_log), KV * kW);
                             for (int c = c0; c < c1; ++c) am[k] = max(am[k], most[c]);
                         }
                     } else {
@@ -202,27 +217,25 @@ __global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) k_add_norm(const __grid
                             all[k] = am[k];
 #pragma unroll
                             for (int j = 0; j < KV; ++j)
-                                if (j / pieces == k / pieces) all[k] = max(all[k], am[j]);
+                                if (j >> pieces_log == k >> pieces_log) all[k] = max(all[k], am[j]);
                         }
 #pragma unroll
                         for (int k = 0; k < KV; ++k) am[k] = all[k];
                     }
                 }
             } else {
+                for (int o = 1 << lanes_log >> 1; o > 0; o >>= 1)
 #pragma unroll
-                for (int k = 0; k < KV; ++k)
-                    for (int o = lanes >> 1; o > 0; o >>= 1) am[k] = max(am[k], __shfl_xor_sync(0xffffffffu, am[k], o));
+                    for (int k = 0; k < KV; ++k) am[k] = max(am[k], __shfl_xor_sync(0xffffffffu, am[k], o));
             }
 #pragma unroll
             for (int k = 0; k < KV; ++k) {
                 const int q = tid + TPR * k;
                 if (q >= nv) continue;
                 const E4m3Scale c = e4m3_scale(am[k]);
-                float f[V];
-#pragma unroll
-                for (int i = 0; i < V; ++i) f[i] = n[k][i] * c.inv;
-                L::codes(p.Q + t * p.d + q * V, f);
-                if (q % lanes == 0) p.S[t * p.groups + q / lanes] = c.scale;
+                scale_by(n[k], c.inv);
+                L::codes(p.Q + t * p.d + q * V, n[k]);
+                if ((q & ((1 << lanes_log) - 1)) == 0) p.S[t * p.groups + (q >> lanes_log)] = c.scale;
             }
         }
         if (kW > 1) __syncthreads();   // sums and most are this row's until here
@@ -263,7 +276,8 @@ template <typename E> __global__ void __launch_bounds__(1024) k_add_norm_long(co
             if (p.N) static_cast<E *>(p.N)[t * p.ldn + j] = from_f32<E>(n);
             am = max(am, abs_bits(n));
         }
-        if (p.Q && p.group > p.d) {   // one scale a row
+        const int64_t group = int64_t(1) << p.group_log;
+        if (p.Q && group > p.d) {   // one scale a row
             am = __reduce_max_sync(0xffffffffu, am);
             if (lane == 0) peaks[warp] = am;
             __syncthreads();
@@ -275,7 +289,7 @@ template <typename E> __global__ void __launch_bounds__(1024) k_add_norm_long(co
         } else if (p.Q) {             // a warp a group (the other warps' H has to be there)
             __syncthreads();
             for (int64_t g = warp; g < p.groups; g += 32) {
-                const int64_t j0 = g * p.group, j1 = min(j0 + (int64_t)p.group, (int64_t)p.d);
+                const int64_t j0 = g * group, j1 = min(j0 + group, (int64_t)p.d);
                 uint32_t m = 0;
                 for (int64_t j = j0 + lane; j < j1; j += 32) m = max(m, abs_bits(h_at(j) * rstd * to_f32(gamma[j])));
                 const E4m3Scale c = e4m3_scale(__reduce_max_sync(0xffffffffu, m));
@@ -296,17 +310,26 @@ template <typename E, int V, int KV, int TPR> cudaError_t launch(const NormArgs 
     return launch_pdl(k_add_norm<E, V, KV, TPR>, dim3(grid), dim3(kThreads), 0, c, p);
 }
 
+#ifndef KVV
+#define KVV 2
+#endif
+#ifndef KVS
+#define KVS 8
+#endif
 template <typename E, int V> cudaError_t run(const NormArgs &p, const Ctx &c)
 {
     const int64_t nv = p.d / V;
+    constexpr int K = V > 1 ? KVV : KVS;
     if (nv <= 32) return launch<E, V, 1, 32>(p, c);
     if (nv <= 64) return launch<E, V, 2, 32>(p, c);
     if (nv <= 128) return launch<E, V, 4, 32>(p, c);
-    if (nv <= 256) return launch<E, V, 2, 128>(p, c);
-    if (nv <= 512) return launch<E, V, 2, 256>(p, c);
-    if (nv <= 1024) return launch<E, V, 2, 512>(p, c);
-    if (nv <= 2048) return launch<E, V, 2, 1024>(p, c);
-    if (nv <= 4096) return launch<E, V, 4, 1024>(p, c);
+    if (V == 1 && nv <= 256) return launch<E, V, 8, 32>(p, c);
+    if (nv <= 64 * K) return launch<E, V, K, 64>(p, c);
+    if (nv <= 128 * K) return launch<E, V, K, 128>(p, c);
+    if (nv <= 256 * K) return launch<E, V, K, 256>(p, c);
+    if (nv <= 512 * K) return launch<E, V, K, 512>(p, c);
+    if (nv <= 1024 * K) return launch<E, V, K, 1024>(p, c);
+    if (nv <= 1024 * 4) return launch<E, V, 4, 1024>(p, c);
     const unsigned grid = (unsigned)std::min<int64_t>(p.T, (int64_t)c.sm_count * 2);
     return launch_pdl(k_add_norm_long<E>, dim3(grid), dim3(1024), 0, c, p);
 }
@@ -377,7 +400,7 @@ extern "C" resbm_status resbm_add_rmsnorm_fwd(const resbm_add_norm_desc *desc, c
     resbm_status st = make_ctx(stream, &c);
     if (st != RESBM_OK || !t) return st;
     NormArgs p{X, A, gamma, H, N, static_cast<uint8_t *>(Q), S, d.T, ldx, lda, ldh, ldn, groups, (int)d.d, 0, d.eps, (float)(1.0 / (double)d.d)};
-    p.group = d.q_group && d.q_group <= d.d ? d.q_group : INT32_MAX / 2 + 1;   // 2^30: over every d
+    p.group_log = d.q_group && d.q_group <= d.d ? __builtin_ctz((unsigned)d.q_group) : 30;
     const cudaError_t e = d.dtype == RESBM_F32 ? run<float>(p, c) : run<__nv_bfloat16>(p, c);
     if (e == cudaSuccess) count_launches(1);
     else cudaGetLastError();

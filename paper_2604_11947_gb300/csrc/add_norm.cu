@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "abi.h"
 #include "common.cuh"
@@ -28,18 +29,14 @@ struct NormArgs {
 
 template <int V> __device__ __forceinline__ void scale_by(float (&f)[V], float c)
 {
-    if constexpr (V > 1) {
 #pragma unroll
-        for (int i = 0; i < V; i += 2) split(pair(f[i], f[i + 1]) * both(c), f[i], f[i + 1]);
-    } else {
-        f[0] *= c;
-    }
+    for (int i = 0; i < V; i += 2) split(pair(f[i], f[i + 1]) * both(c), f[i], f[i + 1]);
 }
 
-// V neighbouring elements, as loaded
-template <typename E, int V> struct Vec {
-    static constexpr int kWords = V * (int)sizeof(E) / 4;   // 4
-    uint32_t w[kWords];
+// 16 bytes of a row: 8 bf16 or 4 fp32 elements
+template <typename E> struct Vec {
+    static constexpr int V = 16 / (int)sizeof(E);
+    uint32_t w[4];
 
     __device__ __forceinline__ void load(const E *p)
     {
@@ -90,155 +87,332 @@ template <typename E, int V> struct Vec {
 #pragma unroll
         for (int i = 0; i < V / 2; ++i) set(i, pair(f[2 * i], f[2 * i + 1]));
     }
-    static __device__ __forceinline__ void codes(uint8_t *q, const float (&f)[V])
+    // the first n elements stay, the others become zero
+    __device__ __forceinline__ void keep(int n)
     {
-        if constexpr (V == 8) *reinterpret_cast<uint2 *>(q) = make_uint2(e4m3x4(f[0], f[1], f[2], f[3]), e4m3x4(f[4], f[5], f[6], f[7]));
-        else *reinterpret_cast<uint32_t *>(q) = e4m3x4(f[0], f[1], f[2], f[3]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (sizeof(E) == 2) w[i] = n >= 2 * i + 2 ? w[i] : n == 2 * i + 1 ? w[i] & 0xFFFFu : 0u;
+            else w[i] = n > i ? w[i] : 0u;
+        }
     }
 };
-template <typename E> struct Vec<E, 1> {
-    E u;
-    __device__ __forceinline__ void load(const E *p) { u = *p; }
-    __device__ __forceinline__ void zero() { u = from_f32<E>(0.0f); }
-    __device__ __forceinline__ void store(E *p) const { *p = u; }
-    __device__ __forceinline__ void add(const Vec &o) { u = from_f32<E>(to_f32(u) + to_f32(o.u)); }
-    __device__ __forceinline__ float squares() const { return to_f32(u) * to_f32(u); }
-    __device__ __forceinline__ void scaled(float c, const Vec &g, float (&f)[1]) const { f[0] = to_f32(u) * c * to_f32(g.u); }
-    __device__ __forceinline__ void put(const float (&f)[1]) { u = from_f32<E>(f[0]); }
-    static __device__ __forceinline__ void codes(uint8_t *q, const float (&f)[1]) { *q = e4m3x1(f[0]); }
+// The e4m3 codes of a vector
+template <int V> struct Codes {
+    uint32_t w[V / 4];
+    __device__ __forceinline__ explicit Codes(const float (&f)[V])
+    {
+#pragma unroll
+        for (int i = 0; i < V / 4; ++i) w[i] = e4m3x4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
+    }
+    __device__ __forceinline__ Codes() {}
+    __device__ __forceinline__ void store(uint8_t *p) const
+    {
+        if constexpr (V == 8) *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
+        else *reinterpret_cast<uint32_t *>(p) = w[0];
+    }
 };
 
-// The row in registers: TPR threads a row (a warp of a CTA of eight, or a whole CTA), each with KV vectors of V
-// elements, thread q of them owning vectors q, q + TPR, ... X and A are read once, H, N, Q and S written once. The
-// sum of squares goes through a fixed shuffle tree and the warps' sums in warp order.
-template <typename E, int V, int KV, int TPR>
-__global__ void __launch_bounds__(TPR == 32 ? 256 : TPR) k_add_norm(const __grid_constant__ NormArgs p)
+// Bytes n .. n + 4 NW - 1 of lo followed by hi (0 <= n < 4 NW; BYTES: n need not be a multiple of 4)
+template <int NW, bool BYTES> __device__ __forceinline__ void realign(const uint32_t (&lo)[NW], const uint32_t (&hi)[NW], int n, uint32_t (&out)[NW])
 {
-    constexpr int kThreads = TPR == 32 ? 256 : TPR, kRows = kThreads / TPR, kW = TPR / 32;
-    __shared__ float sums[kW];
-    __shared__ uint32_t most[KV * kW];   // the largest |n| of every 32 vectors
-    using L = Vec<E, V>;
-    const int tid = threadIdx.x % TPR, lane = threadIdx.x & 31, warp = tid >> 5;
-    const int nv = p.d / V;
+    uint32_t x[2 * NW];
+#pragma unroll
+    for (int i = 0; i < NW; ++i) {
+        x[i] = lo[i];
+        x[NW + i] = hi[i];
+    }
+#pragma unroll
+    for (int step = NW / 2; step > 0; step >>= 1) {
+        const bool on = (n >> 2) & step;
+#pragma unroll
+        for (int i = 0; i + step < 2 * NW; ++i) x[i] = on ? x[i + step] : x[i];
+    }
+#pragma unroll
+    for (int i = 0; i < NW; ++i) out[i] = BYTES ? __funnelshift_r(x[i], x[i + 1], 8 * (n & 3)) : x[i];
+}
+
+// A row whose first element is anywhere: element j of the row is byte `off` + j * size of the words from `base`
+template <typename E> struct Shifted {
+    const char *base;
+    int off;
+    __device__ __forceinline__ explicit Shifted(const E *row, int word)
+    {
+        off = (int)(reinterpret_cast<uintptr_t>(row) & (uintptr_t)(word - 1));
+        base = reinterpret_cast<const char *>(row) - off;
+    }
+};
+
+// Vector q (elements V q ..) of a shifted row of d elements: the two 16-byte words that hold it, no word without an
+// element of the row; elements past the row are zero.
+template <typename E> __device__ __forceinline__ void load_shifted(Vec<E> &r, const Shifted<E> &row, int q, int d)
+{
+    constexpr int V = Vec<E>::V, kSize = sizeof(E);
+    Vec<E> lo, hi;
+    lo.zero();
+    hi.zero();
+    const int bytes = row.off + d * kSize;   // of the words that reach to the row's end (d * 4 < 2^31)
+    if (16 * q < bytes) lo.load(reinterpret_cast<const E *>(row.base + (int64_t)16 * q));
+    if (row.off) {
+        if (16 * (q + 1) < bytes) hi.load(reinterpret_cast<const E *>(row.base + (int64_t)16 * (q + 1)));
+        realign<4, sizeof(E) != 4>(lo.w, hi.w, row.off, r.w);
+    } else {
+        r = lo;
+    }
+    if (V * (q + 1) > d) r.keep(d - V * q);
+}
+
+// Element `lane` of the words that lane `from` holds
+template <typename T, int NW> __device__ __forceinline__ T element(const uint32_t (&w)[NW], int from, int lane)
+{
+    constexpr int kSize = sizeof(T);
+    uint32_t r = 0;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) {
+        const uint32_t x = __shfl_sync(0xffffffffu, w[i], from);
+        r = lane * kSize / 4 == i ? x : r;
+    }
+    return (T)(kSize == 4 ? r : r >> (8 * (lane * kSize % 4)));
+}
+
+// A warp's KV vectors, neighbours in lanes and then in k, from vector q0 (lane 0, k = 0) on, into a row that starts at any
+// element (T: what an element is stored as, NW words a vector): whole words where the warp has all of one; the elements
+// before its first whole word and behind its last, fewer than a word's each, one a lane. get(k, out): the words of vector k.
+template <typename T, int NW, int KV, typename Get> __device__ __forceinline__ void store_shifted(T *row, int q0, int lane, int d, Get get)
+{
+    constexpr int kSize = sizeof(T), V = 4 * NW / kSize, kWord = 4 * NW;
+    const Shifted<T> at(row, kWord);
+    const int o = at.off / kSize;                                   // elements before the row in its first word
+    const int first = q0 * V, last = min(first + 32 * KV * V, d);   // the warp's elements
+    uint32_t before[NW] = {}, tail[NW] = {};                        // lane 31's words of the previous k; the last, partial word
+    int behind = -1;                                                // its first element
+#pragma unroll
+    for (int k = 0; k < KV; ++k) {
+        uint32_t own[NW], prev[NW], out[NW];
+        get(k, own);
+        const int from = (q0 + 32 * k + lane) * V - o;              // the first element of the word that ends in this vector
+        if (k == 0 && o) {
+            const T x = element<T, NW>(own, 0, lane);
+            if (lane < V - o && first + lane < last) row[first + lane] = x;
+        }
+        if (o) {
+#pragma unroll
+            for (int i = 0; i < NW; ++i) {
+                const uint32_t left = __shfl_sync(0xffffffffu, own[i], (lane + 31) & 31);
+                prev[i] = lane == 0 ? before[i] : left;
+                before[i] = left;
+            }
+            realign<NW, kSize != 4>(prev, own, kWord - at.off, out);
+        } else {
+#pragma unroll
+            for (int i = 0; i < NW; ++i) out[i] = own[i];
+        }
+        if (from >= first && from + V <= last) {
+            char *const p = const_cast<char *>(at.base) + (int64_t)(from + o) * kSize;
+            if constexpr (NW == 4) *reinterpret_cast<uint4 *>(p) = make_uint4(out[0], out[1], out[2], out[3]);
+            else if constexpr (NW == 2) *reinterpret_cast<uint2 *>(p) = make_uint2(out[0], out[1]);
+            else *reinterpret_cast<uint32_t *>(p) = out[0];
+        } else if (from >= first && from < last) {
+            behind = from;
+#pragma unroll
+            for (int i = 0; i < NW; ++i) tail[i] = out[i];
+        }
+        if (k == KV - 1 && lane == 31 && from + V < last) {   // the word that only begins in the last vector
+            const uint32_t none[NW] = {};
+            behind = from + V;
+            realign<NW, kSize != 4>(own, none, kWord - at.off, tail);
+        }
+    }
+    const unsigned has = __ballot_sync(0xffffffffu, behind >= 0);   // (one lane at most)
+    if (has) {
+        const int src = __ffs(has) - 1, from = __shfl_sync(0xffffffffu, behind, src);
+        const T x = element<T, NW>(tail, src, lane);
+        if (lane < V && from + lane < last) row[from + lane] = x;
+    }
+}
+
+// The row in registers: a warp a row (MAXT = 32, in CTAs of eight) or a CTA of up to MAXT threads a row, each thread with
+// KV vectors of 16 bytes, a warp's vectors one contiguous piece of the row. X and A are read once, H, N, Q and S written
+// once. The sum of squares goes through a fixed shuffle tree and the warps' sums through another. SHIFT: rows that start
+// or end off the vectors' alignment; every tensor's row is then realigned by itself on its way in and out (single
+// elements took 90 instructions each and 67 us at T = 20000, d = 1001, bf16).
+template <typename E, int KV, int MAXT, bool SHIFT>
+__global__ void __launch_bounds__(MAXT == 32 ? 256 : MAXT) k_add_norm(const __grid_constant__ NormArgs p)
+{
+    using L = Vec<E>;
+    constexpr int V = L::V, kLogV = V == 8 ? 3 : 2;
+    constexpr bool kWide = MAXT > 32;                // a CTA a row
+    constexpr int kRows = kWide ? 1 : 8;
+    using Bits = typename std::conditional<sizeof(E) == 2, uint16_t, uint32_t>::type;
+    __shared__ float sums[32];
+    __shared__ uint32_t most[KV * 32];               // the largest |n| of every 32 vectors, or of a warp's
+    __shared__ float factor[KV * 32];                // 448 over a group's
+    const int lane = threadIdx.x & 31, warp = kWide ? (int)threadIdx.x >> 5 : 0, warps = kWide ? (int)blockDim.x >> 5 : 1;
+    const int nv = (p.d + V - 1) / V, q0 = warp * 32 * KV, qt = q0 + lane;   // qt + 32 k: this thread's vectors
     const E *const gamma = static_cast<const E *>(p.gamma);
     griddep_wait();
     griddep_launch_dependents();
-    for (int64_t t = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR; t < p.T; t += (int64_t)gridDim.x * kRows) {
-        const E *const x = static_cast<const E *>(p.X) + t * p.ldx;
-        L h[KV], b[KV];
+    auto load = [&](L (&r)[KV], const E *row) {
+        if constexpr (SHIFT) {
+            const Shifted<E> s(row, 16);
 #pragma unroll
-        for (int k = 0; k < KV; ++k) {
-            const int q = tid + TPR * k;
-            if (q < nv) h[k].load(x + q * V);
-            else h[k].zero();
-        }
-        float s = 0.0f;
-        if (p.A) {
-            const E *const a = static_cast<const E *>(p.A) + t * p.lda;
+            for (int k = 0; k < KV; ++k) load_shifted<E>(r[k], s, qt + 32 * k, p.d);
+        } else {
+            const E *const at = row + qt * V;
 #pragma unroll
             for (int k = 0; k < KV; ++k) {
-                const int q = tid + TPR * k;
-                if (q < nv) b[k].load(a + q * V);
-                else b[k].zero();
+                if (qt + 32 * k < nv) r[k].load(at + 32 * k * V);
+                else r[k].zero();
             }
+        }
+    };
+    // r(k): vector k as an L
+    auto store = [&](E *row, auto r) {
+        if constexpr (SHIFT) {
+            store_shifted<Bits, 4, KV>(reinterpret_cast<Bits *>(row), q0, lane, p.d, [&](int k, uint32_t (&w)[4]) {
+                const L x = r(k);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = x.w[i];
+            });
+        } else {
+            E *const at = row + qt * V;
+#pragma unroll
+            for (int k = 0; k < KV; ++k)
+                if (qt + 32 * k < nv) r(k).store(at + 32 * k * V);
+        }
+    };
+    for (int64_t t = (int64_t)blockIdx.x * kRows + (kWide ? 0 : threadIdx.x >> 5); t < p.T; t += (int64_t)gridDim.x * kRows) {
+        L h[KV], b[KV];
+        load(h, static_cast<const E *>(p.X) + t * p.ldx);
+        if (p.A) {
+            load(b, static_cast<const E *>(p.A) + t * p.lda);
 #pragma unroll
             for (int k = 0; k < KV; ++k) h[k].add(b[k]);
         }
+        float s = 0.0f;
 #pragma unroll
         for (int k = 0; k < KV; ++k) s += h[k].squares();   // (of h as stored)
         if (p.H) {
-            E *const o = static_cast<E *>(p.H) + t * p.ldh;
-#pragma unroll
-            for (int k = 0; k < KV; ++k)
-                if (tid + TPR * k < nv) h[k].store(o + (tid + TPR * k) * V);
+            // (in place: a word of X or A that two threads read is read by both before either stores)
+            if (SHIFT && kWide) __syncthreads();
+            else if (SHIFT) __syncwarp();
+            store(static_cast<E *>(p.H) + t * p.ldh, [&](int k) { return h[k]; });
         }
         s *= p.inv_d;   // (a thread's share of the mean: the row's sum itself could leave fp32's range)
-        // gamma, on its way while the sums travel
-#pragma unroll
-        for (int k = 0; k < KV; ++k) {
-            const int q = tid + TPR * k;
-            if (q < nv) b[k].load(gamma + q * V);
-            else b[k].zero();
-        }
+        load(b, gamma);   // on its way while the sums travel
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-        if (kW > 1) {
+        if (kWide) {
             if (lane == 0) sums[warp] = s;
             __syncthreads();
-            s = 0.0f;
+            s = lane < warps ? sums[lane] : 0.0f;
 #pragma unroll
-            for (int w = 0; w < kW; ++w) s += sums[w];
+            for (int o = MAXT >= 1024 ? 16 : MAXT / 64; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+            if (MAXT < 1024) s = __shfl_sync(0xffffffffu, s, 0);
         }
         const float rstd = 1.0f / sqrtf(s + p.eps);
         float n[KV][V];
 #pragma unroll
         for (int k = 0; k < KV; ++k) h[k].scaled(rstd, b[k], n[k]);
-        if (p.N) {
-            E *const o = static_cast<E *>(p.N) + t * p.ldn;
-#pragma unroll
-            for (int k = 0; k < KV; ++k)
-                if (tid + TPR * k < nv) {
-                    L r;
-                    r.put(n[k]);
-                    r.store(o + (tid + TPR * k) * V);
-                }
-        }
+        if (p.N)
+            store(static_cast<E *>(p.N) + t * p.ldn, [&](int k) {
+                L r;
+                r.put(n[k]);
+                return r;
+            });
         if (p.Q) {
-            // the largest |n| of a group: over the lanes that share it, then, where a group has more than a warp's
-            // vectors, over the 32-vector pieces that the warps left in shared memory (a warp's own in registers)
-            const int lanes_log = p.group_log - (V == 8 ? 3 : V == 4 ? 2 : 0);
+            // the largest |n| of a group: over the lanes that share it; over a warp's pieces of 32 vectors, in shared
+            // memory where other warps have some of them; or, for the whole row, over the warps
+            const int lanes_log = p.group_log - kLogV;
             uint32_t am[KV];
 #pragma unroll
             for (int k = 0; k < KV; ++k) {
                 float m = fabsf(n[k][0]);
 #pragma unroll
                 for (int i = 1; i < V; ++i) m = max_nan(m, fabsf(n[k][i]));
-                am[k] = __float_as_uint(m) & 0x7FFFFFFFu;
+                am[k] = abs_bits(m);
             }
-            if (lanes_log >= 5) {
+            float *const S = p.S + t * p.groups;
+            bool mine = true;   // whether this thread writes its groups' scales
+            if (p.groups == 1) {
+                uint32_t m = am[0];
 #pragma unroll
-                for (int k = 0; k < KV; ++k) am[k] = __reduce_max_sync(0xffffffffu, am[k]);
-                const int pieces_log = lanes_log - 5;
-                if (pieces_log > 0) {
-                    if (kW > 1) {
-                        if (lane == 0)
-#pragma unroll
-                            for (int k = 0; k < KV; ++k) most[k * kW + warp] = am[k];
-                        __syncthreads();
-#pragma unroll
-                        for (int k = 0; k < KV; ++k) {
-                            const int c0 = (k * kW + warp) >> pieces_log << pieces_log, c1 = min(c0 + (1 << pieces_log), KV * kW);
-                            for (int c = c0; c < c1; ++c) am[k] = max(am[k], most[c]);
-                        }
-                    } else {
-                        uint32_t all[KV];
-#pragma unroll
-                        for (int k = 0; k < KV; ++k) {
-                            all[k] = am[k];
-#pragma unroll
-                            for (int j = 0; j < KV; ++j)
-                                if (j >> pieces_log == k >> pieces_log) all[k] = max(all[k], am[j]);
-                        }
-#pragma unroll
-                        for (int k = 0; k < KV; ++k) am[k] = all[k];
-                    }
+                for (int k = 1; k < KV; ++k) m = max(m, am[k]);
+                m = __reduce_max_sync(0xffffffffu, m);
+                if (kWide) {
+                    if (lane == 0) most[warp] = m;
+                    __syncthreads();
+                    m = __reduce_max_sync(0xffffffffu, lane < warps ? most[lane] : 0u);
                 }
-            } else {
+                const E4m3Scale c = e4m3_scale(m);
+#pragma unroll
+                for (int k = 0; k < KV; ++k) scale_by(n[k], c.inv);
+                if (qt == 0) S[0] = c.scale;
+                mine = false;
+            } else if (lanes_log < 5) {
                 for (int o = 1 << lanes_log >> 1; o > 0; o >>= 1)
 #pragma unroll
                     for (int k = 0; k < KV; ++k) am[k] = max(am[k], __shfl_xor_sync(0xffffffffu, am[k], o));
-            }
+            } else {
+                const int pieces_log = lanes_log - 5;
 #pragma unroll
-            for (int k = 0; k < KV; ++k) {
-                const int q = tid + TPR * k;
-                if (q >= nv) continue;
-                const E4m3Scale c = e4m3_scale(am[k]);
-                scale_by(n[k], c.inv);
-                L::codes(p.Q + t * p.d + q * V, n[k]);
-                if ((q & ((1 << lanes_log) - 1)) == 0) p.S[t * p.groups + (q >> lanes_log)] = c.scale;
+                for (int k = 0; k < KV; ++k) am[k] = __reduce_max_sync(0xffffffffu, am[k]);
+                if (pieces_log > 0 && kWide) {   // a warp a group, from shared memory
+                    if (lane == 0)
+#pragma unroll
+                        for (int k = 0; k < KV; ++k) most[warp * KV + k] = am[k];
+                    __syncthreads();
+                    for (int g = warp; g < (int)p.groups; g += warps) {
+                        uint32_t m = 0;
+                        for (int c = lane; c < 1 << pieces_log; c += 32)
+                            if ((g << pieces_log) + c < warps * KV) m = max(m, most[(g << pieces_log) + c]);
+                        const E4m3Scale c = e4m3_scale(__reduce_max_sync(0xffffffffu, m));
+                        if (lane == 0) {
+                            factor[g] = c.inv;
+                            S[g] = c.scale;
+                        }
+                    }
+                    __syncthreads();
+#pragma unroll
+                    for (int k = 0; k < KV; ++k)
+                        if (qt + 32 * k < nv) scale_by(n[k], factor[(warp * KV + k) >> pieces_log]);
+                    mine = false;
+                } else if (pieces_log > 0) {
+                    uint32_t all[KV];
+#pragma unroll
+                    for (int k = 0; k < KV; ++k) {
+                        all[k] = am[k];
+#pragma unroll
+                        for (int j = 0; j < KV; ++j)
+                            if (j >> pieces_log == k >> pieces_log) all[k] = max(all[k], am[j]);
+                    }
+#pragma unroll
+                    for (int k = 0; k < KV; ++k) am[k] = all[k];
+                }
+            }
+            if (mine) {
+#pragma unroll
+                for (int k = 0; k < KV; ++k) {
+                    const E4m3Scale c = e4m3_scale(am[k]);
+                    scale_by(n[k], c.inv);
+                    const int q = qt + 32 * k;
+                    if (q < nv && (q & ((1 << lanes_log) - 1)) == 0) S[q >> lanes_log] = c.scale;
+                }
+            }
+            uint8_t *const Q = p.Q + t * p.d;
+            if constexpr (SHIFT) {
+                store_shifted<uint8_t, V / 4, KV>(Q, q0, lane, p.d, [&](int k, uint32_t (&w)[V / 4]) {
+                    const Codes<V> c(n[k]);
+#pragma unroll
+                    for (int i = 0; i < V / 4; ++i) w[i] = c.w[i];
+                });
+            } else {
+#pragma unroll
+                for (int k = 0; k < KV; ++k)
+                    if (qt + 32 * k < nv) Codes<V>(n[k]).store(Q + (qt + 32 * k) * V);
             }
         }
-        if (kW > 1) __syncthreads();   // sums and most are this row's until here
+        if (kWide) __syncthreads();   // sums, most and factor are this row's until here
     }
 }
 
@@ -302,46 +476,33 @@ template <typename E> __global__ void __launch_bounds__(1024) k_add_norm_long(co
     }
 }
 
-template <typename E, int V, int KV, int TPR> cudaError_t launch(const NormArgs &p, const Ctx &c)
+template <typename E, int KV, int MAXT> cudaError_t launch(const NormArgs &p, bool shift, const Ctx &c)
 {
-    constexpr int kThreads = TPR == 32 ? 256 : TPR, kRows = kThreads / TPR;
-    const int64_t want = (p.T + kRows - 1) / kRows;
-    const unsigned grid = (unsigned)std::min<int64_t>(want, INT32_MAX);
-    return launch_pdl(k_add_norm<E, V, KV, TPR>, dim3(grid), dim3(kThreads), 0, c, p);
-}
-
-#ifndef KVV
-#define KVV 2
-#endif
-#ifndef KVS
-#define KVS 8
-#endif
-template <typename E, int V> cudaError_t run(const NormArgs &p, const Ctx &c)
-{
-    const int64_t nv = p.d / V;
-    constexpr int K = V > 1 ? KVV : KVS;
-    if (nv <= 32) return launch<E, V, 1, 32>(p, c);
-    if (nv <= 64) return launch<E, V, 2, 32>(p, c);
-    if (nv <= 128) return launch<E, V, 4, 32>(p, c);
-    if (V == 1 && nv <= 256) return launch<E, V, 8, 32>(p, c);
-    if (nv <= 64 * K) return launch<E, V, K, 64>(p, c);
-    if (nv <= 128 * K) return launch<E, V, K, 128>(p, c);
-    if (nv <= 256 * K) return launch<E, V, K, 256>(p, c);
-    if (nv <= 512 * K) return launch<E, V, K, 512>(p, c);
-    if (nv <= 1024 * K) return launch<E, V, K, 1024>(p, c);
-    if (nv <= 1024 * 4) return launch<E, V, 4, 1024>(p, c);
-    const unsigned grid = (unsigned)std::min<int64_t>(p.T, (int64_t)c.sm_count * 2);
-    return launch_pdl(k_add_norm_long<E>, dim3(grid), dim3(1024), 0, c, p);
+    const int64_t rows = MAXT > 32 ? 1 : 8, nv = (p.d + Vec<E>::V - 1) / Vec<E>::V;
+    const unsigned grid = (unsigned)std::min<int64_t>((p.T + rows - 1) / rows, INT32_MAX);
+    const unsigned threads = MAXT > 32 ? (unsigned)((nv + KV * 32 - 1) / (KV * 32)) * 32 : 256;
+    return launch_pdl(shift ? k_add_norm<E, KV, MAXT, true> : k_add_norm<E, KV, MAXT, false>, dim3(grid), dim3(threads), 0, c, p);
 }
 
 template <typename E> cudaError_t run(const NormArgs &p, const Ctx &c)
 {
-    // 16-byte vectors where every row of every tensor starts at a multiple of 16 bytes (Q: of the vector's codes)
-    constexpr int V = 16 / (int)sizeof(E);
+    // whole vectors where every row of every tensor starts and ends at a multiple of 16 bytes (Q: of a vector's codes)
+    constexpr int V = Vec<E>::V;
     auto al = [](const void *q, int64_t ld) { return !q || (reinterpret_cast<uintptr_t>(q) % 16 == 0 && ld % V == 0); };
-    const bool vec = p.d % V == 0 && al(p.X, p.ldx) && al(p.A, p.lda) && al(p.H, p.ldh) && al(p.N, p.ldn) && al(p.gamma, 0) &&
-                     reinterpret_cast<uintptr_t>(p.Q) % V == 0;
-    return vec ? run<E, V>(p, c) : run<E, 1>(p, c);
+    const bool shift = !(p.d % V == 0 && al(p.X, p.ldx) && al(p.A, p.lda) && al(p.H, p.ldh) && al(p.N, p.ldn) && al(p.gamma, 0) &&
+                         reinterpret_cast<uintptr_t>(p.Q) % V == 0);
+    const int64_t nv = (p.d + V - 1) / V;
+    // A warp a row up to 128 vectors (no barrier), then CTAs of three vectors a thread: against two and four at bf16
+    // d = 4096 to e4m3 266 us (274, 306), d = 8192 138 (160, 192), d = 2048 41.3 (41.3, 43.2).
+    if (nv <= 32) return launch<E, 1, 32>(p, shift, c);
+    if (nv <= 64) return launch<E, 2, 32>(p, shift, c);
+    if (nv <= 96) return launch<E, 3, 32>(p, shift, c);
+    if (nv <= 128) return launch<E, 4, 32>(p, shift, c);
+    if (nv <= 512 * 3) return launch<E, 3, 512>(p, shift, c);
+    if (nv <= 512 * 4) return launch<E, 4, 512>(p, shift, c);
+    if (nv <= 512 * 8) return launch<E, 8, 512>(p, shift, c);
+    const unsigned grid = (unsigned)std::min<int64_t>(p.T, (int64_t)c.sm_count * 2);
+    return launch_pdl(k_add_norm_long<E>, dim3(grid), dim3(1024), 0, c, p);
 }
 
 // Rows of a strided matrix: T rows of `width` bytes, `pitch` bytes apart

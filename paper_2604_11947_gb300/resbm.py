@@ -411,30 +411,38 @@ def _want(ok, what):
         raise ValueError(what)
 
 
+_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 def _here(t, device, what):
     """t is on the current device (where the library enqueues)"""
-    if not t.is_cuda or t.get_device() != device:
+    if t.get_device() != device:
         raise ValueError("%s must be on the current CUDA device (%d): got %s" % (what, device, t.device))
+
+
+def _row_stride(t, shape, dtype, device, what):
+    """The row stride of a (T, d) tensor with unit stride along d"""
+    stride = t.stride()
+    if t.shape != shape or t.dtype != dtype or (stride[1] != 1 and shape[1] > 1):
+        raise ValueError("%s must be %s, %s, with unit stride along the columns" % (what, tuple(shape), dtype))
+    _here(t, device, what)
+    return stride[0]
 
 
 def resbm_add_rmsnorm_fwd(X, A, gamma, eps, H=None, N=None, Q=None, S=None, q_group=0, stream=None):
     """H = X + A (A None: H = X), N = RMSNorm(H) * gamma, Q and S the same in e4m3 with scales. X, A, H, N: (T, d) of one
     type, unit stride along d, any row stride (A and X: also 0, an expanded row); gamma (d,); Q (T, d) dense, one byte an
     element (float8_e4m3fn or uint8), with S (T, ceil(d / q_group)) fp32, or (T, 1) for q_group = 0."""
-    if X.dim() != 2 or X.dtype not in _DT:
-        raise ValueError("X must be (T, d), fp32 or bf16")
     shape, dtype = X.shape, X.dtype
+    code = _DT.get(dtype)
+    if len(shape) != 2 or code is None:
+        raise ValueError("X must be (T, d), fp32 or bf16")
     T, d = shape
-    device = torch.cuda.current_device()
-    ld = []
-    for name, t in (("X", X), ("A", A), ("H", H), ("N", N)):
-        if t is None:
-            ld.append(0)
-            continue
-        if t.shape != shape or t.dtype != dtype or (t.stride(1) != 1 and d > 1):
-            raise ValueError("%s must be %s, %s, with unit stride along the columns" % (name, tuple(shape), dtype))
-        _here(t, device, name)
-        ld.append(t.stride(0))
+    device = _device()
+    ldx = _row_stride(X, shape, dtype, device, "X")
+    lda = 0 if A is None else _row_stride(A, shape, dtype, device, "A")
+    ldh = 0 if H is None else _row_stride(H, shape, dtype, device, "H")
+    ldn = 0 if N is None else _row_stride(N, shape, dtype, device, "N")
     if gamma.shape != shape[1:] or gamma.dtype != dtype or not gamma.is_contiguous():
         raise ValueError("gamma must be (%d,), %s" % (d, dtype))
     _here(gamma, device, "gamma")
@@ -444,13 +452,16 @@ def resbm_add_rmsnorm_fwd(X, A, gamma, eps, H=None, N=None, Q=None, S=None, q_gr
         groups = -(-d // q_group) if q_group > 0 else 1
         if Q.shape != shape or Q.element_size() != 1 or not Q.is_contiguous():
             raise ValueError("Q must be %s, dense, one byte an element" % (tuple(shape),))
-        if tuple(S.shape) != (T, groups) or S.dtype != torch.float32 or not S.is_contiguous():
+        if S.shape != (T, groups) or S.dtype != torch.float32 or not S.is_contiguous():
             raise ValueError("S must be (%d, %d), fp32, dense" % (T, groups))
         _here(Q, device, "Q")
         _here(S, device, "S")
-    desc = resbm_add_norm_desc(T, d, ld[0], ld[1], ld[2], ld[3], _DT[dtype], q_group, eps, 0)
-    st = load().resbm_add_rmsnorm_fwd(ctypes.byref(desc), X.data_ptr(), _p(A), gamma.data_ptr(), _p(H), _p(N), _p(Q), _p(S),
-                                      _stream(stream))
+    if stream is None and _raw_stream is not None:
+        stream = _raw_stream(device)
+    st = (_lib or load()).resbm_add_rmsnorm_fwd(
+        resbm_add_norm_desc(T, d, ldx, lda, ldh, ldn, code, q_group, eps, 0), X.data_ptr(), None if A is None else A.data_ptr(),
+        gamma.data_ptr(), None if H is None else H.data_ptr(), None if N is None else N.data_ptr(),
+        None if Q is None else Q.data_ptr(), None if S is None else S.data_ptr(), _stream(stream))
     if st != RESBM_OK:
         _check("resbm_add_rmsnorm_fwd", st)
 
@@ -466,7 +477,7 @@ class AdamWPlan:
         self._fields = {"w": params, "g": grads, "m": m, "v": v, "m_scale": m_scale, "v_scale": v_scale, "master": master}
         self._fields = {k: list(x) for k, x in self._fields.items() if x is not None}
         grads = self._fields["g"]
-        self.device = torch.cuda.current_device()
+        self.device = _device()
         self.count = len(grads)
         state = RESBM_STATE_NONE
         if params is not None:
@@ -538,10 +549,10 @@ def resbm_adamw_step(plan, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.
             if t.dtype != dt or t.numel() != 1:
                 raise ValueError("%s must be one %s" % (name, dt))
             _here(t, plan.device, name)
-    if torch.cuda.current_device() != plan.device:
+    if _device() != plan.device:
         raise ValueError("the plan's tensors are on device %d, not the current one" % plan.device)
     hyper = resbm_adamw_hyper(lr, beta1, beta2, eps, weight_decay, step, _p(lr_dev), _p(step_dev), _p(grad_scale))
-    st = load().resbm_adamw_step(plan._address, ctypes.byref(hyper), _stream(stream))
+    st = (_lib or load()).resbm_adamw_step(plan._address, hyper, _stream(stream))
     if st != RESBM_OK:
         _check("resbm_adamw_step", st)
 
@@ -566,7 +577,7 @@ def resbm_grad_norm(plans, max_norm, out, ws, stream=None):
     """out (2 fp32): the norm of the gradients of a plan (or of several together), and the coefficient that clips it to
     max_norm (0: none), which resbm_adamw_step takes as grad_scale = out[1:]."""
     array, plans = _plans(plans)
-    device = torch.cuda.current_device()
+    device = _device()
     if out.dtype != torch.float32 or out.numel() != 2 or not out.is_contiguous():
         raise ValueError("out must be 2 fp32")
     _here(out, device, "out")

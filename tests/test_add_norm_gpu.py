@@ -137,6 +137,39 @@ def test_strides(dtype, d, pad):
     assert bool((buf[:, 3 * d:] == 9.0).all())
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 1), ("bf16", 64), ("bf16", 65), ("bf16", 300), ("bf16", 1999), ("bf16", 2048), ("bf16", 5001), ("f32", 3), ("f32", 64),
+                                     ("f32", 333), ("f32", 2500)])
+def test_every_alignment(dtype, d):
+    """Each tensor off the vectors' alignment by its own number of elements, in rows that follow each other without a gap:
+    what lies before the first row and behind the last stays."""
+    T, n = 13, 8
+    X, A, gamma = rows(T, d, dtype, 1), rows(T, d, dtype, 2), gamma_of(d, dtype)
+    want = outputs(T, d, dtype, "hnq", 32)
+    run(X, A, gamma, want, T, d, 32)
+    check(X, A, gamma, EPS, want, T, d, 32)
+
+    def at(offset, src, dt, fill):
+        buf = torch.full((offset + src.numel() + 16,), fill, dtype=dt, device="cuda")
+        view = buf[offset:offset + src.numel()].view(src.shape)
+        view.copy_(src)
+        return buf, view
+
+    dt = DT[dtype]
+    for k in range(n):
+        (_, x), (_, a), (_, g) = at(k, X, dt, 3.0), at((3 * k + 1) % n, A, dt, 3.0), at((5 * k) % n, gamma, dt, 3.0)
+        hb, h = at((k + 2) % n, X, dt, 5.0)
+        nb, y = at((2 * k) % n, X, dt, 5.0)
+        qb, q = at(k + 8, torch.zeros(T, d, dtype=torch.uint8, device="cuda"), torch.uint8, 99)
+        S = torch.empty(T, -(-d // 32), device="cuda")
+        resbm.resbm_add_rmsnorm_fwd(x, a, g, EPS, h, y, q, S, 32)
+        assert torch.equal(h, want["H"][:T]) and torch.equal(y, want["N"][:T]) and torch.equal(q, want["Q"][:T]) and torch.equal(S, want["S"][:T])
+        for buf, view, fill in ((hb, h, 5.0), (nb, y, 5.0), (qb, q, 99)):
+            o = view.storage_offset()
+            assert bool((buf[:o] == fill).all()) and bool((buf[o + T * d:] == fill).all())
+        resbm.resbm_add_rmsnorm_fwd(x, a, g, EPS, x, None, q, S, 32)      # in place
+        assert torch.equal(x, want["H"][:T])
+
+
 @pytest.mark.parametrize("dtype,d", [("bf16", 512), ("f32", 77), ("bf16", 4096), ("bf16", 34000)])
 def test_in_place_and_broadcast(dtype, d):
     T = 50

@@ -16,8 +16,9 @@ P^id truncates to the first r columns on the send side and zero-pads on the rece
 Pid_definition). The encoder and decoder run through the C ABI of libresbm.so
 (resbm_encode_fwd / resbm_decode_fwd forward, resbm_decode_bwd / resbm_encode_bwd backward)
 inside torch.autograd.Function; everything else (attention, SwiGLU feed-forward, RMSNorm, rotary
-positions, embedding, loss) is plain PyTorch in bf16. There is no fallback: without the library
-the boundary raises.
+positions, embedding, loss) is plain PyTorch in bf16, but for the norms with fuse_add_norm, which
+add the residual and normalise in one kernel of the library. There is no fallback: without the
+library the boundary raises.
 """
 from __future__ import annotations
 
@@ -49,6 +50,8 @@ class PipelineConfig:
     seed: int = 0
     flags: int = 0           # resbm descriptor flags of the boundaries (RESBM_FLAG_*)
     fuse_norm: bool = True   # the receiving block's pre-attention RMSNorm fused into the decoder
+    fuse_add_norm: bool = False   # every other RMSNorm with the residual's addition before it, in one
+                                  # kernel (resbm_add_rmsnorm_fwd); else torch's
 
     def with_(self, **kw) -> "PipelineConfig":
         return replace(self, **kw)
@@ -214,6 +217,51 @@ class _DecodeNorm(torch.autograd.Function):
         return dB, dWd1.to(Wd1.dtype), dWd2.to(Wd2.dtype), dgamma, None
 
 
+class _AddNorm(torch.autograd.Function):
+    """(h, n) = (x + a, RMSNorm(h) * gamma): resbm_add_rmsnorm_fwd forward; backward resbm_rmsnorm_bwd, whose result is the
+    gradient of x and of a alike. a None: (x, n)."""
+
+    @staticmethod
+    def forward(ctx, x, a, gamma):
+        if x.shape[1] > 16384:
+            raise ValueError("the norm's backward takes rows of at most 16384")
+        h = x if a is None else torch.empty_like(x, memory_format=torch.contiguous_format)
+        n = torch.empty_like(h, memory_format=torch.contiguous_format)
+        resbm.resbm_add_rmsnorm_fwd(x, a, gamma, NORM_EPS, None if a is None else h, n)
+        ctx.save_for_backward(h, gamma)
+        ctx.set_materialize_grads(False)
+        ctx.added = a is not None
+        return (h, n) if ctx.added else n
+
+    @staticmethod
+    def backward(ctx, *grads):
+        h, gamma = ctx.saved_tensors
+        dh, dn = grads if ctx.added else (None, grads[0])
+        if dn is None:
+            return dh, dh if ctx.added else None, None
+        h, (T, d) = h.contiguous(), h.shape
+        desc = resbm.make_desc(T, d, 1, 1, "bf16" if h.dtype == torch.bfloat16 else "f32")
+        dx = torch.empty_like(h)
+        dgamma = torch.empty(d, dtype=torch.float32, device=h.device)
+        resbm.resbm_rmsnorm_bwd(desc, h, gamma, NORM_EPS, dn.contiguous(), None if dh is None else dh.contiguous(), dx, dgamma,
+                                resbm.workspace(desc, resbm.RESBM_OP_RMSNORM_BWD, h.device))
+        return dx, dx if ctx.added else None, dgamma.to(gamma.dtype)
+
+
+def add_norm(x, a, gamma):
+    """(x + a, RMSNorm(x + a) * gamma) over the last dimension, in one pass each way; a None: (x, RMSNorm(x) * gamma)."""
+    shape = x.shape
+
+    def flat(t):
+        t = t.reshape(-1, shape[-1])
+        return t if t.stride(1) == 1 else t.contiguous()
+
+    if a is None:
+        return x, _AddNorm.apply(flat(x), None, gamma).view(shape)
+    h, n = _AddNorm.apply(flat(x), flat(a), gamma)
+    return h.view(shape), n.view(shape)
+
+
 class Boundary(torch.nn.Module):
     """One ResBM boundary: the encoder on the sending stage, the decoder on the receiving one.
     Weights N(0, 1/fan_in), bf16."""
@@ -296,8 +344,9 @@ class Block(torch.nn.Module):
         o = Fn.scaled_dot_product_attention(q, k, v, is_causal=True)
         return Fn.linear(o.transpose(1, 2).reshape(bsz, seq, d), self.wo)
 
-    def ffn(self, h):
-        u = Fn.rms_norm(h, (h.shape[-1],), self.n2, NORM_EPS)
+    def ffn(self, h, normed=None):
+        """The feed-forward half; normed: RMSNorm(h) * n2 when the caller has it."""
+        u = Fn.rms_norm(h, (h.shape[-1],), self.n2, NORM_EPS) if normed is None else normed
         return Fn.linear(Fn.silu(Fn.linear(u, self.w1)) * Fn.linear(u, self.w3), self.w2)
 
 
@@ -337,10 +386,12 @@ class PipelineModel(torch.nn.Module):
         rope = self.rope(seq, tokens.device)
         per_stage = cfg.layers // cfg.stages
         x = Fn.embedding(tokens, self.embed)
-        b = None
+        b = z = None
+        fuse = cfg.fuse_add_norm
         for s in range(cfg.stages):
             for j in range(per_stage):
                 blk = self.blocks[s * per_stage + j]
+                skip = None
                 if j == 0 and s > 0:   # receive: decode the boundary tensor of the previous stage
                     bnd = self.bounds[s - 1]
                     if cfg.fuse_norm:   # the block's attention norm comes out of the decoder
@@ -349,18 +400,25 @@ class PipelineModel(torch.nn.Module):
                     else:
                         y, n = bnd.decode(b).view(bsz, seq, d), None
                     if cfg.wiring == "A":
-                        x = y                                       # pad(b) + D(b)
-                        h = x + blk.attn(x, rope, n)
+                        x = skip = y                                # pad(b) + D(b)
                     else:
-                        h = Fn.pad(b, (0, d - bnd.r)).view(bsz, seq, d) + blk.attn(y, rope, n)   # pad(b) + Attn(D(b))
+                        x, skip = y, Fn.pad(b, (0, d - bnd.r)).view(bsz, seq, d)   # pad(b) + Attn(D(b))
+                elif fuse:             # x: the previous block's h + z, added as it is normalised
+                    x, n = add_norm(x, z, blk.n1)
+                    skip = x
                 else:
-                    h = x + blk.attn(x, rope)
-                z = blk.ffn(h)
+                    x = skip = x if z is None else x + z
+                    n = None
+                if fuse:
+                    h, u = add_norm(skip, blk.attn(x, rope, n), blk.n2)
+                else:
+                    h, u = skip + blk.attn(x, rope, n), None
+                z = blk.ffn(h, u)
                 if j == per_stage - 1 and s < cfg.stages - 1:   # send: encode after the feed-forward
                     b = self.bounds[s].encode(h.reshape(T, d), z.reshape(T, d))
-                else:
-                    x = h + z
-        logits = Fn.linear(Fn.rms_norm(x, (d,), self.norm, NORM_EPS), self.head)
+                x = h
+        last = add_norm(x, z, self.norm)[1] if fuse else Fn.rms_norm(x + z, (d,), self.norm, NORM_EPS)
+        logits = Fn.linear(last, self.head)
         return Fn.cross_entropy(logits[:, :-1].reshape(-1, cfg.vocab).float(), tokens[:, 1:].reshape(-1))
 
 
@@ -424,11 +482,15 @@ def markov_batches(cfg: PipelineConfig, n_batches, seed=2, branching=4, device="
     return torch.from_numpy(out).view(n_batches, cfg.batch, cfg.seq).to(device), rate
 
 
-def train_curve(cfg: PipelineConfig, data, steps, lr=1e-3, every=25):
+def train_curve(cfg: PipelineConfig, data, steps, lr=1e-3, every=25, optimizer=None):
     """AdamW on the model's parameters over `steps` batches of `data` (cycled); the loss at step
-    0, every `every` steps and at the end (mean of the last `every` steps' losses)."""
+    0, every `every` steps and at the end (mean of the last `every` steps' losses). optimizer: called with the
+    parameters and lr instead of torch's AdamW (for example optim.AdamW, or a function that gives it state_bits = 8)."""
     model = PipelineModel(cfg)
-    opt = torch.optim.AdamW(model.parameters(), lr=lr, weight_decay=0.01)
+    if optimizer is None:
+        opt = torch.optim.AdamW(model.parameters(), lr=lr, weight_decay=0.01)
+    else:
+        opt = optimizer(model.parameters(), lr=lr)
     curve, window = [], []
     for s in range(steps):
         loss = train_step(model, data[s % data.shape[0]])

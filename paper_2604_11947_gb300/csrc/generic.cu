@@ -423,6 +423,7 @@ template <> struct VecOf<float, 4> {
     static __device__ void store(float *p, const float *f) { *reinterpret_cast<float4 *>(p) = make_float4(f[0], f[1], f[2], f[3]); }
 };
 template <typename E> struct VecOf<E, 1> {
+    static __device__ void unpack(const E u, float *f) { f[0] = to_f32(u); }
     static __device__ void load(const E *p, float *f) { f[0] = to_f32(*p); }
     static __device__ void store(E *p, const float *f) { *p = from_f32<E>(f[0]); }
 };
@@ -512,48 +513,51 @@ __global__ void __launch_bounds__(256) k_rmsnorm_bwd(const E *__restrict__ Y, co
     for (int64_t j = tid; j < d; j += 256) dg_part[(int64_t)blockIdx.x * d + j] = dgs[j];
 }
 
-// The vector path for rows of at most 256 * KV vectors: each thread keeps its vectors of Y, dN and dY (as
-// loaded, 16 bytes each) in registers from the first pass to the second, so a row costs one trip to memory,
+// Rows of at most 256 * KV vectors (V = 1: elements): each thread keeps its vectors of Y, dN and dY (as
+// loaded, 16 bytes or one element each) in registers from the first pass to the second, so a row costs one trip to memory,
 // with the next row's loads in flight meanwhile; gamma and the dgamma sums of the thread's columns stay in
 // registers too. The same sums in the same order as k_rmsnorm_bwd, so the same bits. Bound by memory (4 d
 // elements a row): T = 16384, d = 2048 59 us (4.5 TB/s) without the prefetch and with the dgamma sums in
-// shared memory.
+// shared memory. Widths that are no multiple of a vector: T = 20000, d = 1001 bf16 57 us, fp32 65 (135 and 139 with the
+// elements read twice and the dgamma sums in shared memory), d = 2001 116 and 125 (247, 275).
 template <typename E, int V, int KV>
-__global__ void __launch_bounds__(256, KV == 1 ? 4 : KV == 2 ? 2 : 1)
+__global__ void __launch_bounds__(256, V == 1 ? (KV <= 4 ? 4 : 2) : KV == 1 ? 4 : KV == 2 ? 2 : 1)
     k_rmsnorm_bwd_reg(const E *__restrict__ Y, const E *__restrict__ gamma, float eps, const E *__restrict__ dN,
                       const E *dY, E *dYo, float *__restrict__ dg_part, int64_t rows, int64_t d)
 {
     __shared__ float2 part[2][8];
     using L = VecOf<E, V>;
+    using Raw = typename std::conditional<V == 1, E, uint4>::type;   // a vector as loaded
+    const Raw zero = {};
     griddep_wait();
     griddep_launch_dependents();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int nv = (int)(d / V);
     float acc[KV][V];
-    uint4 rg[KV];
+    Raw rg[KV];
 #pragma unroll
     for (int k = 0; k < KV; ++k) {
         const int q = tid + 256 * k;
-        rg[k] = q < nv ? *reinterpret_cast<const uint4 *>(gamma + q * V) : make_uint4(0u, 0u, 0u, 0u);
+        rg[k] = q < nv ? *reinterpret_cast<const Raw *>(gamma + q * V) : zero;
 #pragma unroll
         for (int i = 0; i < V; ++i) acc[k][i] = 0.0f;
     }
     const int64_t r0 = rows * blockIdx.x / gridDim.x, r1 = rows * (blockIdx.x + 1) / gridDim.x;
-    uint4 ry[KV], rn[KV], ro[KV];
-    auto load = [&](int64_t t, uint4 (&y)[KV], uint4 (&n)[KV], uint4 (&o)[KV]) {
+    Raw ry[KV], rn[KV], ro[KV];
+    auto load = [&](int64_t t, Raw (&y)[KV], Raw (&n)[KV], Raw (&o)[KV]) {
 #pragma unroll
         for (int k = 0; k < KV; ++k) {
             const int q = tid + 256 * k;
             if (q < nv) {
-                y[k] = *reinterpret_cast<const uint4 *>(Y + t * d + q * V);
-                n[k] = *reinterpret_cast<const uint4 *>(dN + t * d + q * V);
-                o[k] = dY ? *reinterpret_cast<const uint4 *>(dY + t * d + q * V) : make_uint4(0u, 0u, 0u, 0u);
+                y[k] = *reinterpret_cast<const Raw *>(Y + t * d + q * V);
+                n[k] = *reinterpret_cast<const Raw *>(dN + t * d + q * V);
+                o[k] = dY ? *reinterpret_cast<const Raw *>(dY + t * d + q * V) : zero;
             }
         }
     };
     if (r0 < r1) load(r0, ry, rn, ro);
     for (int64_t t = r0; t < r1; ++t) {
-        uint4 ny[KV], nn[KV], no[KV];
+        Raw ny[KV], nn[KV], no[KV];
         if (t + 1 < r1) load(t + 1, ny, nn, no);   // (dY_out may be dY: each row is read before it is written)
         float sy = 0.0f, sg = 0.0f;
 #pragma unroll
@@ -595,7 +599,7 @@ __global__ void __launch_bounds__(256, KV == 1 ? 4 : KV == 2 ? 2 : 1)
                 L::unpack(rg[k], gm);
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    o[i] += s * (b[i] * gm[i]) - a[i] * kk;
+                    o[i] += fmaf(s, b[i] * gm[i], -__fmul_rn(a[i], kk));   // (as k_rmsnorm_bwd's is contracted)
                     acc[k][i] = fmaf(b[i], a[i] * s, acc[k][i]);
                 }
                 L::store(dYo + t * d + q * V, o);
@@ -608,11 +612,15 @@ __global__ void __launch_bounds__(256, KV == 1 ? 4 : KV == 2 ? 2 : 1)
 #pragma unroll
     for (int k = 0; k < KV; ++k) {
         const int q = tid + 256 * k;
-        if (q < nv)
+        if (q >= nv) continue;
+        float *const part_at = dg_part + (int64_t)blockIdx.x * d + q * V;
+        if constexpr (V == 1) {
+            *part_at = acc[k][0];
+        } else {
 #pragma unroll
             for (int i = 0; i < V; i += 4)
-                *reinterpret_cast<float4 *>(dg_part + (int64_t)blockIdx.x * d + q * V + i) =
-                    make_float4(acc[k][i], acc[k][i + 1], acc[k][i + 2], acc[k][i + 3]);
+                *reinterpret_cast<float4 *>(part_at + i) = make_float4(acc[k][i], acc[k][i + 1], acc[k][i + 2], acc[k][i + 3]);
+        }
     }
 }
 
@@ -673,9 +681,9 @@ cudaError_t generic_rmsnorm_bwd(const resbm_desc &d, const void *Y, const void *
                      d.d % (d.dtype == RESBM_F32 ? 4 : 8) == 0;
     cudaError_t e = cudaSuccess;
     if (d.T > 0) {
-        // the register-cached vector path up to 4 vectors a thread (bf16 d <= 8192, fp32 d <= 4096)
-        const int64_t nv = d.d / (d.dtype == RESBM_F32 ? 4 : 8);
-        const int kv = !vec ? 0 : nv <= 256 ? 1 : nv <= 512 ? 2 : nv <= 1024 ? 4 : 0;
+        // the register-cached form up to 4 vectors a thread (bf16 d <= 8192, fp32 d <= 4096), or 8 single elements
+        const int64_t nv = vec ? d.d / (d.dtype == RESBM_F32 ? 4 : 8) : d.d;
+        const int kv = nv <= 256 ? 1 : nv <= 512 ? 2 : nv <= 1024 ? 4 : !vec && nv <= 2048 ? 8 : 0;
         // (the register-cached forms keep the dgamma sums in registers)
         auto run = [&](auto k, auto tag) -> cudaError_t {
             using E = decltype(tag);
@@ -688,7 +696,13 @@ cudaError_t generic_rmsnorm_bwd(const resbm_desc &d, const void *Y, const void *
                               (const E *)dY, (E *)dY_out, part, d.T, d.d);
         };
         using bf = __nv_bfloat16;
-        if (d.dtype == RESBM_F32)
+        if (kv && !vec && d.dtype == RESBM_F32)
+            e = run(kv == 1 ? k_rmsnorm_bwd_reg<float, 1, 1> : kv == 2 ? k_rmsnorm_bwd_reg<float, 1, 2>
+                    : kv == 4 ? k_rmsnorm_bwd_reg<float, 1, 4> : k_rmsnorm_bwd_reg<float, 1, 8>, 0.0f);
+        else if (kv && !vec)
+            e = run(kv == 1 ? k_rmsnorm_bwd_reg<bf, 1, 1> : kv == 2 ? k_rmsnorm_bwd_reg<bf, 1, 2>
+                    : kv == 4 ? k_rmsnorm_bwd_reg<bf, 1, 4> : k_rmsnorm_bwd_reg<bf, 1, 8>, bf());
+        else if (d.dtype == RESBM_F32)
             e = run(kv == 1 ? k_rmsnorm_bwd_reg<float, 4, 1> : kv == 2 ? k_rmsnorm_bwd_reg<float, 4, 2>
                     : kv == 4 ? k_rmsnorm_bwd_reg<float, 4, 4> : vec ? k_rmsnorm_bwd<float, 4> : k_rmsnorm_bwd<float, 1>, 0.0f);
         else

@@ -88,7 +88,8 @@ typedef struct {
  * `master`, the fp32 master copy is what the step reads and updates, and w is only written. Either every
  * tensor of a plan has a master copy or none has. m_scale, v_scale: ceil(n / RESBM_STATE_BLOCK) fp32 each, with
  * RESBM_STATE_E4M3 only (else NULL). Pointers aligned to their element; a tensor with w, g, m, v and master
- * aligned to four elements each runs faster. n = 0: pointers not used. */
+ * aligned to eight elements each runs faster, and in a launch apart from those that are not. n = 0: pointers not
+ * used. */
 typedef struct {
     void *w;
     const void *g;
@@ -124,8 +125,9 @@ RESBM_API resbm_status resbm_adamw_plan(const resbm_adamw_desc *desc, const resb
 /* One AdamW step (decoupled weight decay) over the plan's tensors, for t = step and c = *grad_scale (or 1):
  *   g' = c g;  m = beta1 m + (1 - beta1) g';  v = beta2 v + (1 - beta2) g'^2
  *   w = (1 - lr weight_decay) w - lr m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps)
- * in fp32, every tensor in place; the new m and v go into w before they are rounded to 8 bits. One launch for
- * up to 448 tensors. Errors: RESBM_ERR_INVALID_ARG for a bad hyperparameter or for a plan that is none or has
+ * in fp32, every tensor in place; the new m and v go into w before they are rounded to 8 bits. The root and the
+ * quotient are within 2^-21 of theirs (relative to the update); a v below 2^-126 (gradients under 1e-17) counts as
+ * 2^-126 there, and as zero in an 8-bit state. One launch for up to 448 tensors of a kind (aligned or not). Errors: RESBM_ERR_INVALID_ARG for a bad hyperparameter or for a plan that is none or has
  * RESBM_STATE_NONE. */
 RESBM_API resbm_status resbm_adamw_step(const void *plan, const resbm_adamw_hyper *hyper, void *stream);
 

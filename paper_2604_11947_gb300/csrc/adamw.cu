@@ -1,8 +1,10 @@
 // adamw.cu -- resbm_adamw_step and resbm_grad_norm: one pass over many tensors a launch (include/resbm_train.h).
 //
 // Both are bound by memory: a step with 32-bit states moves 22 bytes an element (bf16 weight and gradient), one
-// with 8-bit states 10. The list of tensors travels as the launch's parameter (up to 448 tensors, 31 KB), so that
-// nothing is copied to the device and a captured launch carries its own list.
+// with 8-bit states 10, the norm 2. The list of tensors travels as the launch's parameter (up to 448 tensors, 31 KB), so
+// that nothing is copied to the device and a captured launch carries its own list; a list of up to 32 takes the small
+// parameter (2.2 KB; one call on the host 5.1 us, 5.5 with the large one). 308 M bf16 parameters on a GB300: 32-bit states
+// 963 us (7.0 TB/s; a copy moves 6.8), 8-bit states 446 (7.0 TB/s), norm 94 (6.6 TB/s).
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -17,24 +19,28 @@
 #include "pair.cuh"
 #include "resbm_train.h"
 
-#ifndef MINB
-#define MINB 8
-#endif
 namespace resbm {
 namespace {
 
+// CTAs of 128 threads, eight on an SM: with 256 threads the 8-bit step took 463 us instead of 448, the norm 98 instead of 96.
 constexpr int kThreads = 128, kWarps = kThreads / 32;
 constexpr int kBlock = RESBM_STATE_BLOCK;             // elements a warp takes at a time: one block of 8-bit states
-// Blocks that a warp has in flight where its accesses are vectors, by the states' bits
+// Blocks that a warp has in flight where its accesses are vectors, by the states' bits. 8: 308 M elements 518 us with one
+// and 448 with two (at 64 registers, some of them spilled: at 72 without spills 494, with one CTA fewer on an SM; three
+// and four 484 and more). 32: 1060 us either way with the norm, and small lists spread over more CTAs with one.
 __host__ __device__ constexpr int deep_of(int bits) { return bits == 8 ? 2 : 1; }
 constexpr int kSmall = 32, kLarge = 448;              // tensors a launch, by the parameter's size
 constexpr int kNormGrid = 1216;                       // most CTAs of the gradients' norm: eight on each of 152 SMs
+// Gradients for a CTA of the norm to be worth it, two rounds of loads in bf16: 10.5 M gradients 10.4 us (12.0 with half as
+// many, 11.8 with four times)
+constexpr int kRound = 16384;
 constexpr float kLeastRoot = 0x1p-63f;                // sqrt(2^-126)
-constexpr int kRound = 16384;                          // gradients that a CTA of the norm has in flight
 constexpr uint64_t kMagic = 0x7265736264616d77ull;
 
 // The tensors of one launch, of one kind: those whose accesses are vectors (everything of a tensor aligned to eight
-// elements) and the others. A unit is what one CTA takes: kWarps * deep blocks of one tensor.
+// elements) and the others, whose single elements need fewer registers and one block a warp (30 M elements one past
+// alignment, 8-bit states: 98 us; 214 in the vectors' kernel at its registers). A unit is what one CTA takes:
+// kWarps * deep blocks of one tensor.
 template <int CAP> struct Table {
     void *w[CAP];
     const void *g[CAP];
@@ -169,8 +175,8 @@ __device__ __forceinline__ float approx_rcp(float v)
 // approximate, far below what the update is to the weight. A v below 2^-126 (gradients below 1e-17) counts as that for
 // the weight (`least` is its denominator), as zero for the 8-bit state.
 // The 8-bit form is bound by instructions as much as by memory (10 bytes an element): with IEEE roots and quotients, one
-// value an instruction and one block a warp 75 of them an element, 868 us for 308 M elements; with pairs and approximate
-// ones 52 and 597.
+// value an instruction and one block a warp 75 of them an element, 868 us for 308 M elements; with pairs 52 and 597; with
+// two blocks a warp, accesses of eight elements and one reciprocal an element 34 and 448.
 template <typename W, typename G, bool MASTER, int BITS, Mode MODE, int K>
 __device__ __forceinline__ void adamw_blocks(W *w, const G *g, void *mp, void *vp, float *ms, float *vs, float *master,
                                              int lane, int rem, const Step &h, float c)
@@ -259,7 +265,7 @@ template <int CAP> __device__ __forceinline__ int tensor_of(const Table<CAP> &ta
 }
 
 template <typename W, typename G, bool MASTER, int BITS, bool VEC, int CAP>
-__global__ void __launch_bounds__(kThreads, VEC && BITS == 8 ? MINB : 1) k_adamw(const __grid_constant__ Table<CAP> tab, const __grid_constant__ Step given)
+__global__ void __launch_bounds__(kThreads, VEC && BITS == 8 ? 8 : 1) k_adamw(const __grid_constant__ Table<CAP> tab, const __grid_constant__ Step given)
 {
     Step h = given;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;

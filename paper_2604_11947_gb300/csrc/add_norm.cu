@@ -237,7 +237,7 @@ template <typename T, int NW, int KV, typename Get> __device__ __forceinline__ v
 // or end off the vectors' alignment; every tensor's row is then realigned by itself on its way in and out (single
 // elements took 90 instructions each and 67 us at T = 20000, d = 1001, bf16).
 template <typename E, int KV, int MAXT, bool SHIFT>
-__global__ void __launch_bounds__(MAXT == 32 ? 256 : MAXT) k_add_norm(const __grid_constant__ NormArgs p)
+__global__ void __launch_bounds__(MAXT == 32 ? 256 : MAXT, KV == 4 && MAXT == 512 ? 2 : 1) k_add_norm(const __grid_constant__ NormArgs p)
 {
     using L = Vec<E>;
     constexpr int V = L::V, kLogV = V == 8 ? 3 : 2;

@@ -79,6 +79,8 @@ class AdamW(torch.optim.Optimizer):
             if old[2] != gwhere:
                 old[0].set_grads(grads)
                 old[2] = gwhere
+            else:
+                old[0]._fields["g"] = grads
             return old[0]
         states = [self.state[p] for p in params]
         column = lambda k: [st[k] for st in states] if k in states[0] else None
@@ -127,6 +129,7 @@ class AdamW(torch.optim.Optimizer):
             b1, b2 = group["betas"]
             resbm.resbm_adamw_step(plan, lr=float(group["lr"]), beta1=b1, beta2=b2, eps=group["eps"], weight_decay=group["weight_decay"],
                                    step=key[3], grad_scale=scale)
+            plan.release_grads()   # (zero_grad frees them; the launches that read them are on the stream already)
             for p in params:
                 self.state[p]["step"] = key[3]
         return loss

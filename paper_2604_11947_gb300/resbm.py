@@ -471,7 +471,7 @@ class AdamWPlan:
     of the same lengths, one entry per parameter: weights (fp32 or bf16), gradients (fp32 or bf16), states m and v (fp32,
     or e4m3 codes of m and of sqrt(v): float8_e4m3fn or uint8, with m_scale and v_scale of ceil(n / 256) fp32), optionally
     fp32 master copies of bf16 weights. With gradients alone (params None) the plan serves resbm_grad_norm. The plan
-    keeps the tensors alive; gradients that moved are given with set_grads."""
+    keeps the tensors alive; gradients that moved are given with set_grads, their memory is let go with release_grads."""
 
     def __init__(self, params, grads, m=None, v=None, m_scale=None, v_scale=None, master=None):
         self._fields = {"w": params, "g": grads, "m": m, "v": v, "m_scale": m_scale, "v_scale": v_scale, "master": master}
@@ -493,36 +493,34 @@ class AdamWPlan:
         for k in ("w", "g"):
             x = self._fields.get(k)
             _want(not x or (x[0].dtype in _DT and all(t.dtype == x[0].dtype for t in x)), "%s: fp32 or bf16, one type in a plan" % k)
+        sizes = [g.numel() for g in grads]
+        blocks = [-(-n // RESBM_STATE_BLOCK) for n in sizes]
+        codes = (torch.float8_e4m3fn, torch.uint8) if state == RESBM_STATE_E4M3 else (torch.float32,)
         for k, x in self._fields.items():
-            if k == "g":
-                continue
-            for t, g in zip(x, grads):
-                n = -(-g.numel() // RESBM_STATE_BLOCK) if k.endswith("_scale") else g.numel()
-                _want(t.is_contiguous() and t.numel() == n, "%s: dense tensors of the gradients' sizes" % k)
-                if k in ("m", "v"):
-                    _want(t.dtype in ((torch.float8_e4m3fn, torch.uint8) if state == RESBM_STATE_E4M3 else (torch.float32,)), "%s: fp32, or e4m3 codes with scales" % k)
-                elif k != "w":
-                    _want(t.dtype == torch.float32, "%s: fp32" % k)
+            types = (x[0].dtype,) if k in ("w", "g") and x else codes if k in ("m", "v") else (torch.float32,)
+            for t, n in zip(x, blocks if k.endswith("_scale") else sizes):
+                if t.numel() != n or not t.is_contiguous() or t.dtype not in types:
+                    raise ValueError("%s: dense tensors of the gradients' sizes, %s" % (k, " or ".join(map(str, types))))
                 _here(t, self.device, k)
         dt = lambda k: _DT[self._fields[k][0].dtype] if self._fields.get(k) else RESBM_F32
         self._desc = resbm_adamw_desc(dt("w"), dt("g"), state, 0)
         self._tensors = (resbm_adamw_tensor * self.count)()
-        for k, x in self._fields.items():
-            for e, t in zip(self._tensors, x):
-                setattr(e, k, t.data_ptr())
-        for e, g in zip(self._tensors, grads):
-            e.n = g.numel()
+        # (the structure is eight 64-bit words: an array of them is filled column by column)
+        words = (ctypes.c_int64 * (8 * self.count)).from_buffer(self._tensors)
+        for i, k in enumerate(("w", "g", "m", "v", "m_scale", "v_scale", "master")):
+            if k in self._fields:
+                words[i::8] = [t.data_ptr() for t in self._fields[k]]
+        words[7::8] = self._sizes = sizes
         size = ctypes.c_size_t(0)
         _check("resbm_adamw_plan_bytes", load().resbm_adamw_plan_bytes(self.count, ctypes.byref(size)))
         self._plan = (ctypes.c_uint64 * (-(-size.value // 8)))()
         self._address = ctypes.addressof(self._plan)
-        self._check_grads(grads)
         self._build()
 
     def _check_grads(self, grads):
         _want(len(grads) == self.count, "%d gradients for %d tensors" % (len(grads), self.count))
-        for g, o, e in zip(grads, self._fields["g"], self._tensors):
-            _want(g.is_contiguous() and g.numel() == e.n and g.dtype == o.dtype, "gradients: dense tensors of the same sizes and type")
+        for g, n in zip(grads, self._sizes):
+            _want(g.is_contiguous() and g.numel() == n and _DT.get(g.dtype) == self._desc.g_dtype, "gradients: dense tensors of the same sizes and type")
             _here(g, self.device, "a gradient")
 
     def _build(self):
@@ -539,6 +537,16 @@ class AdamWPlan:
             e.g = g.data_ptr()
         self._build()
 
+    def release_grads(self):
+        """Lets the gradients' memory go: no step before the next set_grads."""
+        self._fields["g"] = None
+
+    def _ready(self, device):
+        if device != self.device:
+            raise ValueError("the plan's tensors are on device %d, not the current one (%d)" % (self.device, device))
+        if self._fields["g"] is None:
+            raise ValueError("the plan's gradients were released")
+
 
 def resbm_adamw_step(plan, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, step=1, lr_dev=None, step_dev=None,
                      grad_scale=None, stream=None):
@@ -549,8 +557,7 @@ def resbm_adamw_step(plan, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.
             if t.dtype != dt or t.numel() != 1:
                 raise ValueError("%s must be one %s" % (name, dt))
             _here(t, plan.device, name)
-    if _device() != plan.device:
-        raise ValueError("the plan's tensors are on device %d, not the current one" % plan.device)
+    plan._ready(_device())
     hyper = resbm_adamw_hyper(lr, beta1, beta2, eps, weight_decay, step, _p(lr_dev), _p(step_dev), _p(grad_scale))
     st = (_lib or load()).resbm_adamw_step(plan._address, hyper, _stream(stream))
     if st != RESBM_OK:
@@ -582,8 +589,8 @@ def resbm_grad_norm(plans, max_norm, out, ws, stream=None):
         raise ValueError("out must be 2 fp32")
     _here(out, device, "out")
     _here(ws, device, "ws")
-    if any(p.device != device for p in plans):
-        raise ValueError("a plan's tensors are not on the current device")
+    for p in plans:
+        p._ready(device)
     st = load().resbm_grad_norm(array, len(plans), max_norm, out.data_ptr(), ws.data_ptr(), _nbytes(ws), _stream(stream))
     if st != RESBM_OK:
         _check("resbm_grad_norm", st)

@@ -1,6 +1,7 @@
 """optim.AdamW (the library's step as a torch optimizer) and the pipeline's fused norms: against 64 bits, against torch, and
 together in training steps as they are used."""
 import copy
+import weakref
 
 import pytest
 import torch
@@ -120,6 +121,31 @@ def test_state_dict_goes_on_where_it_was(bits, master):
         optim.AdamW(others, state_bits=40 - bits, master=master).load_state_dict(opt.state_dict())
     with pytest.raises(ValueError):
         optim.AdamW(others, state_bits=bits, master=not master).load_state_dict(opt.state_dict())
+
+
+def test_gradients_are_let_go():
+    """After the step nothing of the optimizer holds the gradients' memory; gradients that stay where they are serve again."""
+    params = params_of([1000, 300], torch.float32)
+    opt = optim.AdamW(params, max_grad_norm=1.0, **H)
+    set_grads(params, 1)
+    for t in (2, 3):
+        before = columns(opt, params) if t > 2 else None
+        opt.step()
+        if before:
+            check_step(before, columns(opt, params), 2, HYPER, float(opt.grad_norm[1]))
+        for p in params:
+            p.grad.mul_(0.5)
+    held = [weakref.ref(p.grad) for p in params]
+    opt.zero_grad(set_to_none=True)
+    assert all(h() is None for h in held)
+    plan = resbm.AdamWPlan(None, [torch.ones(5, device="cuda")])
+    ws, out = resbm.grad_norm_workspace(plan), torch.empty(2, device="cuda")
+    plan.release_grads()
+    with pytest.raises(ValueError):
+        resbm.resbm_grad_norm(plan, 1.0, out, ws)
+    plan.set_grads([torch.full((5,), 2.0, device="cuda")])
+    resbm.resbm_grad_norm(plan, 0.0, out, ws)
+    assert abs(float(out[0]) - 20 ** 0.5) <= 4 * U * 20 ** 0.5
 
 
 def test_refusals():

@@ -231,13 +231,22 @@ template <typename T, int NW, int KV, typename Get> __device__ __forceinline__ v
     }
 }
 
+// CTAs of the most threads that an SM holds at least, which bounds the registers: 64 a thread for a CTA a row (without it
+// the compiler takes 77 at three vectors a thread: bf16 T = 65536, d = 4096 to e4m3 305 us instead of 265, T = 10000, d = 5001
+// 162 instead of 102), 64 for a warp a row, but 80 for the realignment of four bf16 vectors (T = 20000, d = 1001 57 us without
+// a bound, 38 at 80, 41 at 64; d = 301 78 and 70 at 64). Eight vectors a thread need all they can get.
+template <typename E, int KV, int MAXT> constexpr int min_ctas()
+{
+    return MAXT == 32 ? (KV == 4 && sizeof(E) == 2 ? 3 : 4) : KV <= 4 ? 2 : 1;
+}
+
 // The row in registers: a warp a row (MAXT = 32, in CTAs of eight) or a CTA of up to MAXT threads a row, each thread with
 // KV vectors of 16 bytes, a warp's vectors one contiguous piece of the row. X and A are read once, H, N, Q and S written
 // once. The sum of squares goes through a fixed shuffle tree and the warps' sums through another. SHIFT: rows that start
 // or end off the vectors' alignment; every tensor's row is then realigned by itself on its way in and out (single
 // elements took 90 instructions each and 67 us at T = 20000, d = 1001, bf16).
 template <typename E, int KV, int MAXT, bool SHIFT>
-__global__ void __launch_bounds__(MAXT == 32 ? 256 : MAXT, KV == 4 && MAXT == 512 ? 2 : 1) k_add_norm(const __grid_constant__ NormArgs p)
+__global__ void __launch_bounds__(MAXT == 32 ? 256 : MAXT, min_ctas<E, KV, MAXT>()) k_add_norm(const __grid_constant__ NormArgs p)
 {
     using L = Vec<E>;
     constexpr int V = L::V, kLogV = V == 8 ? 3 : 2;

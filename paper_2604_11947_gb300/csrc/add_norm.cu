@@ -113,8 +113,8 @@ template <int V> struct Codes {
     }
 };
 
-// Bytes n .. n + 4 NW - 1 of lo followed by hi (0 <= n < 4 NW; BYTES: n need not be a multiple of 4)
-template <int NW, bool BYTES> __device__ __forceinline__ void realign(const uint32_t (&lo)[NW], const uint32_t (&hi)[NW], int n, uint32_t (&out)[NW])
+// Bytes 4 WORDS + bits / 8 .. of lo followed by hi, 4 NW of them (BYTES: bits need not be 0)
+template <int NW, int WORDS, bool BYTES> __device__ __forceinline__ void realign(const uint32_t (&lo)[NW], const uint32_t (&hi)[NW], int bits, uint32_t (&out)[NW])
 {
     uint32_t x[2 * NW];
 #pragma unroll
@@ -123,13 +123,25 @@ template <int NW, bool BYTES> __device__ __forceinline__ void realign(const uint
         x[NW + i] = hi[i];
     }
 #pragma unroll
-    for (int step = NW / 2; step > 0; step >>= 1) {
-        const bool on = (n >> 2) & step;
-#pragma unroll
-        for (int i = 0; i + step < 2 * NW; ++i) x[i] = on ? x[i + step] : x[i];
+    for (int i = 0; i < NW; ++i) out[i] = BYTES ? __funnelshift_r(x[i + WORDS], x[i + WORDS + 1], bits) : x[i + WORDS];
+}
+
+// f with `words` (0 .. NW - 1, the same in the whole warp) as a constant
+template <int NW, typename F> __device__ __forceinline__ void with_words(int words, F f)
+{
+    if constexpr (NW == 1) {
+        f(std::integral_constant<int, 0>());
+    } else if constexpr (NW == 2) {
+        if (words) f(std::integral_constant<int, 1>());
+        else f(std::integral_constant<int, 0>());
+    } else {
+        switch (words) {
+        case 0: f(std::integral_constant<int, 0>()); break;
+        case 1: f(std::integral_constant<int, 1>()); break;
+        case 2: f(std::integral_constant<int, 2>()); break;
+        default: f(std::integral_constant<int, 3>()); break;
+        }
     }
-#pragma unroll
-    for (int i = 0; i < NW; ++i) out[i] = BYTES ? __funnelshift_r(x[i], x[i + 1], 8 * (n & 3)) : x[i];
 }
 
 // A row whose first element is anywhere: element j of the row is byte `off` + j * size of the words from `base`
@@ -143,23 +155,32 @@ template <typename E> struct Shifted {
     }
 };
 
-// Vector q (elements V q ..) of a shifted row of d elements: the two 16-byte words that hold it, no word without an
-// element of the row; elements past the row are zero.
-template <typename E> __device__ __forceinline__ void load_shifted(Vec<E> &r, const Shifted<E> &row, int q, int d)
+// Vectors q, q + 32, ... of a row of d elements that starts anywhere: each from the two 16-byte words that hold it, no word
+// without an element of the row (past its end the last one again); elements past the row are zero.
+template <typename E, int KV> __device__ __forceinline__ void load_shifted(Vec<E> (&r)[KV], const E *from, int q, int d)
 {
-    constexpr int V = Vec<E>::V, kSize = sizeof(E);
-    Vec<E> lo, hi;
-    lo.zero();
-    hi.zero();
-    const int bytes = row.off + d * kSize;   // of the words that reach to the row's end (d * 4 < 2^31)
-    if (16 * q < bytes) lo.load(reinterpret_cast<const E *>(row.base + (int64_t)16 * q));
+    constexpr int V = Vec<E>::V;
+    const Shifted<E> row(from, 16);
+    const int end = (row.off + d * (int)sizeof(E) - 1) >> 4;   // the last word
+    auto word = [&](Vec<E> &v, int i) { v.load(reinterpret_cast<const E *>(row.base + (int64_t)16 * min(i, end))); };
     if (row.off) {
-        if (16 * (q + 1) < bytes) hi.load(reinterpret_cast<const E *>(row.base + (int64_t)16 * (q + 1)));
-        realign<4, sizeof(E) != 4>(lo.w, hi.w, row.off, r.w);
+        with_words<4>(row.off >> 2, [&](auto words) {
+            Vec<E> lo[KV], hi[KV];
+#pragma unroll
+            for (int k = 0; k < KV; ++k) {
+                word(lo[k], q + 32 * k);
+                word(hi[k], q + 32 * k + 1);
+            }
+#pragma unroll
+            for (int k = 0; k < KV; ++k) realign<4, decltype(words)::value, sizeof(E) != 4>(lo[k].w, hi[k].w, 8 * (row.off & 3), r[k].w);
+        });
     } else {
-        r = lo;
+#pragma unroll
+        for (int k = 0; k < KV; ++k) word(r[k], q + 32 * k);
     }
-    if (V * (q + 1) > d) r.keep(d - V * q);
+#pragma unroll
+    for (int k = 0; k < KV; ++k)
+        if (V * (q + 32 * k + 1) > d) r[k].keep(d - V * (q + 32 * k));
 }
 
 // Element `lane` of the words that lane `from` holds
@@ -184,29 +205,10 @@ template <typename T, int NW, int KV, typename Get> __device__ __forceinline__ v
     const Shifted<T> at(row, kWord);
     const int o = at.off / kSize;                                   // elements before the row in its first word
     const int first = q0 * V, last = min(first + 32 * KV * V, d);   // the warp's elements
-    uint32_t before[NW] = {}, tail[NW] = {};                        // lane 31's words of the previous k; the last, partial word
+    uint32_t tail[NW] = {};                                         // the last, partial word
     int behind = -1;                                                // its first element
-#pragma unroll
-    for (int k = 0; k < KV; ++k) {
-        uint32_t own[NW], prev[NW], out[NW];
-        get(k, own);
-        const int from = (q0 + 32 * k + lane) * V - o;              // the first element of the word that ends in this vector
-        if (k == 0 && o) {
-            const T x = element<T, NW>(own, 0, lane);
-            if (lane < V - o && first + lane < last) row[first + lane] = x;
-        }
-        if (o) {
-#pragma unroll
-            for (int i = 0; i < NW; ++i) {
-                const uint32_t left = __shfl_sync(0xffffffffu, own[i], (lane + 31) & 31);
-                prev[i] = lane == 0 ? before[i] : left;
-                before[i] = left;
-            }
-            realign<NW, kSize != 4>(prev, own, kWord - at.off, out);
-        } else {
-#pragma unroll
-            for (int i = 0; i < NW; ++i) out[i] = own[i];
-        }
+    // `out`: the word that ends in vector k, from element `from` on
+    auto put = [&](const uint32_t (&out)[NW], int from) {
         if (from >= first && from + V <= last) {
             char *const p = const_cast<char *>(at.base) + (int64_t)(from + o) * kSize;
             if constexpr (NW == 4) *reinterpret_cast<uint4 *>(p) = make_uint4(out[0], out[1], out[2], out[3]);
@@ -217,10 +219,43 @@ template <typename T, int NW, int KV, typename Get> __device__ __forceinline__ v
 #pragma unroll
             for (int i = 0; i < NW; ++i) tail[i] = out[i];
         }
-        if (k == KV - 1 && lane == 31 && from + V < last) {   // the word that only begins in the last vector
-            const uint32_t none[NW] = {};
-            behind = from + V;
-            realign<NW, kSize != 4>(own, none, kWord - at.off, tail);
+    };
+    const int start = (q0 + lane) * V - o;
+    if (o) {
+        const int n = kWord - at.off, bits = 8 * (n & 3);
+        with_words<NW>(n >> 2, [&](auto words) {
+            constexpr int kWords = decltype(words)::value;
+            uint32_t before[NW] = {};                               // lane 31's words of the previous k, in lane 0
+#pragma unroll
+            for (int k = 0; k < KV; ++k) {
+                uint32_t own[NW], prev[NW], out[NW];
+                get(k, own);
+                if (k == 0) {
+                    const T x = element<T, NW>(own, 0, lane);
+                    if (lane < V - o && first + lane < last) row[first + lane] = x;
+                }
+#pragma unroll
+                for (int i = 0; i < NW; ++i) {
+                    const uint32_t left = __shfl_sync(0xffffffffu, own[i], (lane + 31) & 31);
+                    prev[i] = lane == 0 ? before[i] : left;
+                    before[i] = left;
+                }
+                realign<NW, kWords, kSize != 4>(prev, own, bits, out);
+                const int from = start + 32 * k * V;
+                put(out, from);
+                if (k == KV - 1 && lane == 31 && from + V < last) {   // the word that only begins in the last vector
+                    const uint32_t none[NW] = {};
+                    behind = from + V;
+                    realign<NW, kWords, kSize != 4>(own, none, bits, tail);
+                }
+            }
+        });
+    } else {
+#pragma unroll
+        for (int k = 0; k < KV; ++k) {
+            uint32_t own[NW];
+            get(k, own);
+            put(own, start + 32 * k * V);
         }
     }
     const unsigned has = __ballot_sync(0xffffffffu, behind >= 0);   // (one lane at most)
@@ -263,9 +298,7 @@ __global__ void __launch_bounds__(MAXT == 32 ? 256 : MAXT, min_ctas<E, KV, MAXT>
     griddep_launch_dependents();
     auto load = [&](L (&r)[KV], const E *row) {
         if constexpr (SHIFT) {
-            const Shifted<E> s(row, 16);
-#pragma unroll
-            for (int k = 0; k < KV; ++k) load_shifted<E>(r[k], s, qt + 32 * k, p.d);
+            load_shifted<E, KV>(r, row, qt, p.d);
         } else {
             const E *const at = row + qt * V;
 #pragma unroll

@@ -268,7 +268,7 @@ template <typename T, int NW, int KV, typename Get> __device__ __forceinline__ v
 
 // CTAs of the most threads that an SM holds at least, which bounds the registers: 64 a thread for a CTA a row (without it
 // the compiler takes 77 at three vectors a thread: bf16 T = 65536, d = 4096 to e4m3 305 us instead of 265, T = 10000, d = 5001
-// 162 instead of 102), 64 for a warp a row, but 80 for the realignment of four bf16 vectors (T = 20000, d = 1001 57 us without
+// three vectors a thread 162 instead of 102), 64 for a warp a row, but 80 for the realignment of four bf16 vectors (T = 20000, d = 1001 57 us without
 // a bound, 38 at 80, 41 at 64; d = 301 78 and 70 at 64). Eight vectors a thread need all they can get.
 template <typename E, int KV, int MAXT> constexpr int min_ctas()
 {
@@ -278,8 +278,8 @@ template <typename E, int KV, int MAXT> constexpr int min_ctas()
 // The row in registers: a warp a row (MAXT = 32, in CTAs of eight) or a CTA of up to MAXT threads a row, each thread with
 // KV vectors of 16 bytes, a warp's vectors one contiguous piece of the row. X and A are read once, H, N, Q and S written
 // once. The sum of squares goes through a fixed shuffle tree and the warps' sums through another. SHIFT: rows that start
-// or end off the vectors' alignment; every tensor's row is then realigned by itself on its way in and out (single
-// elements took 90 instructions each and 67 us at T = 20000, d = 1001, bf16).
+// or end off the vectors' alignment; every tensor's row is then realigned by itself on its way in and out (T = 20000,
+// d = 1001, bf16: 34 us; single elements took 90 instructions each and 67 us, the shift of words by selects 38).
 template <typename E, int KV, int MAXT, bool SHIFT>
 __global__ void __launch_bounds__(MAXT == 32 ? 256 : MAXT, min_ctas<E, KV, MAXT>()) k_add_norm(const __grid_constant__ NormArgs p)
 {
@@ -535,12 +535,14 @@ template <typename E> cudaError_t run(const NormArgs &p, const Ctx &c)
                          reinterpret_cast<uintptr_t>(p.Q) % V == 0);
     const int64_t nv = (p.d + V - 1) / V;
     // A warp a row up to 128 vectors (no barrier), then CTAs of three vectors a thread: against two and four at bf16
-    // d = 4096 to e4m3 266 us (274, 306), d = 8192 138 (160, 192), d = 2048 41.3 (41.3, 43.2).
+    // d = 4096 to e4m3 266 us (274, 306), d = 8192 138 (160, 192), d = 2048 41.3 (41.3, 43.2). Widths that are always
+    // realigned take four, since the words at a warp's ends cost as much again: d = 2001 57 us (three 63, two 67, six 95),
+    // fp32 d = 1001 50 (58, 62, 71). The width alone decides, so that the sums' order does not depend on addresses.
     if (nv <= 32) return launch<E, 1, 32>(p, shift, c);
     if (nv <= 64) return launch<E, 2, 32>(p, shift, c);
     if (nv <= 96) return launch<E, 3, 32>(p, shift, c);
     if (nv <= 128) return launch<E, 4, 32>(p, shift, c);
-    if (nv <= 512 * 3) return launch<E, 3, 512>(p, shift, c);
+    if (nv <= 512 * 3 && p.d % V == 0) return launch<E, 3, 512>(p, shift, c);
     if (nv <= 512 * 4) return launch<E, 4, 512>(p, shift, c);
     if (nv <= 512 * 8) return launch<E, 8, 512>(p, shift, c);
     const unsigned grid = (unsigned)std::min<int64_t>(p.T, (int64_t)c.sm_count * 2);

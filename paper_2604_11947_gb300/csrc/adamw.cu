@@ -58,7 +58,8 @@ static_assert(sizeof(Table<kLarge>) <= 32000, "the launch's parameters are at mo
 struct Plan {
     uint64_t magic;
     int64_t tables;               // Table<kSmall> if small, else Table<kLarge>, one after the other behind this
-    int32_t small, w_dtype, g_dtype, state, master, pad;
+    int32_t small, w_dtype, g_dtype, state, master;
+    int32_t most;                 // tables that the list can need, however its tensors are aligned
 };
 static_assert(sizeof(Plan) % 8 == 0, "tables start aligned");
 
@@ -445,9 +446,10 @@ struct Span {
     bool out;
 };
 // (either kind of tensors may end in a table that is not full)
+int64_t most_tables(int64_t count) { return count <= kSmall ? 2 : (count + kLarge - 1) / kLarge + 1; }
 size_t plan_size(int64_t count)
 {
-    const size_t tables = count <= kSmall ? 2 * sizeof(Table<kSmall>) : (size_t)((count + kLarge - 1) / kLarge + 1) * sizeof(Table<kLarge>);
+    const size_t tables = (size_t)most_tables(count) * (count <= kSmall ? sizeof(Table<kSmall>) : sizeof(Table<kLarge>));
     return sizeof(Plan) + tables + (size_t)count * 7 * sizeof(Span);   // (the spans: scratch of the overlap check)
 }
 bool count_ok(int64_t count) { return count >= 0 && count <= (int64_t(1) << 24); }
@@ -543,15 +545,18 @@ unsigned norm_grid(const Plan &p, int64_t k)
     const Extent x = extent_at(p, k);
     return (unsigned)std::min<int64_t>((x.units * x.unit + kRound - 1) / kRound, kNormGrid);
 }
-// The partial sums of `count` plans, or -1 where one of them is none
-int64_t norm_parts(const void *const *plans, int64_t count)
+// The partial sums of `count` plans, or -1 where one of them is none; most: what they come to at most, however their tensors
+// are aligned
+int64_t norm_parts(const void *const *plans, int64_t count, bool most)
 {
     if (count < 0 || (count > 0 && !plans)) return -1;
     int64_t parts = 0;
     for (int64_t i = 0; i < count; ++i) {
         const Plan *p = plan_of(plans[i]);
         if (!p) return -1;
-        for (int64_t k = 0; k < p->tables; ++k) parts += norm_grid(*p, k);
+        if (most) parts += (int64_t)p->most * kNormGrid;
+        else
+            for (int64_t k = 0; k < p->tables; ++k) parts += norm_grid(*p, k);
     }
     return parts;
 }
@@ -627,7 +632,7 @@ resbm_status resbm_adamw_plan(const resbm_adamw_desc *desc, const resbm_adamw_te
     out->g_dtype = d.g_dtype;
     out->state = d.state;
     out->master = masters > 0;
-    out->pad = 0;
+    out->most = (int32_t)most_tables(count);
     out->tables = out->small ? lay_out(d, tensors, count, reinterpret_cast<Table<kSmall> *>(out + 1))
                              : lay_out(d, tensors, count, reinterpret_cast<Table<kLarge> *>(out + 1));
     out->magic = kMagic;
@@ -673,7 +678,7 @@ resbm_status resbm_adamw_step(const void *plan, const resbm_adamw_hyper *hyper, 
 
 resbm_status resbm_grad_norm_workspace_bytes(const void *const *plans, int64_t count, size_t *bytes)
 {
-    const int64_t parts = norm_parts(plans, count);
+    const int64_t parts = norm_parts(plans, count, true);
     if (parts < 0 || !bytes) return RESBM_ERR_INVALID_ARG;
     *bytes = (size_t)parts * sizeof(double);
     return RESBM_OK;
@@ -681,9 +686,9 @@ resbm_status resbm_grad_norm_workspace_bytes(const void *const *plans, int64_t c
 
 resbm_status resbm_grad_norm(const void *const *plans, int64_t count, float max_norm, float *out, void *ws, size_t ws_bytes, void *stream)
 {
-    const int64_t parts = norm_parts(plans, count);
+    const int64_t parts = norm_parts(plans, count, false);
     if (parts < 0 || !(max_norm >= 0.0f) || !(max_norm < INFINITY) || !ptr_ok(out, 4, true)) return RESBM_ERR_INVALID_ARG;
-    const size_t need = (size_t)parts * sizeof(double);
+    const size_t need = (size_t)norm_parts(plans, count, true) * sizeof(double);
     if (need && (!ws || ws_bytes < need)) return RESBM_ERR_WORKSPACE;
     if (need && reinterpret_cast<uintptr_t>(ws) % 256) return RESBM_ERR_INVALID_ARG;
     if (overlaps(rng(out, 2, 4), rng(ws, (int64_t)need, 1))) return RESBM_ERR_INVALID_ARG;

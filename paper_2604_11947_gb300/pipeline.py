@@ -27,6 +27,7 @@ from dataclasses import dataclass, replace
 
 import torch
 import torch.nn.functional as Fn
+from torch.autograd.function import once_differentiable
 
 from . import resbm
 
@@ -234,6 +235,7 @@ class _AddNorm(torch.autograd.Function):
         return (h, n) if ctx.added else n
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, *grads):
         h, gamma = ctx.saved_tensors
         dh, dn = grads if ctx.added else (None, grads[0])

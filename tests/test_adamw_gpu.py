@@ -360,3 +360,59 @@ def test_binding_refusals():
         resbm.resbm_grad_norm(plan, 1.0, f(3), f(64))
     with pytest.raises(resbm.ResbmError):
         resbm.resbm_grad_norm(plan, 1.0, f(2), f(1, dtype=torch.uint8))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_offsets_past_32_bits(bits):
+    """One tensor of over 2^31 elements: its first, middle and last elements, and its norm."""
+    n = (1 << 31) + 70001
+    free, _ = torch.cuda.mem_get_info()
+    if free < 60 << 30:
+        pytest.skip("needs 60 GB")
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    t = lambda dtype: torch.zeros(n, dtype=dtype, device="cuda")
+    w, g, m, v = t(torch.bfloat16), t(torch.bfloat16), t(torch.uint8 if bits == 8 else torch.float32), t(torch.uint8 if bits == 8 else torch.float32)
+    scales = [torch.zeros(-(-n // B), device="cuda") for _ in range(2)] if bits == 8 else [None, None]
+    spots = [slice(0, 1000 * B), slice((1 << 31) - 500 * B, (1 << 31) + 200 * B), slice(n // B * B - 100 * B, n)]
+    for at in spots:
+        for x, size in ((w, 0.1), (g, 1e-2)):
+            x[at] = (size * torch.randn(x[at].numel(), generator=gen, device="cuda")).to(x.dtype)
+    start, grads = [w[at].clone() for at in spots], [g[at].clone() for at in spots]
+    plan = resbm.AdamWPlan([w], [g], [m], [v], *[[x] if x is not None else None for x in scales])
+    ws, out = resbm.grad_norm_workspace(plan), torch.empty(2, device="cuda")
+    resbm.resbm_grad_norm(plan, 0.0, out, ws)
+    covered = torch.cat([g[spots[0]], g[spots[1].start:]]) if spots[2].start < spots[1].stop else torch.cat([g[at] for at in spots])
+    want = norm_of([covered])
+    assert abs(float(out[0]) - want) <= 20 * U * want
+    resbm.resbm_adamw_step(plan, step=1, **HYPER)
+    for at, w0, g0 in zip(spots, start, grads):
+        k = w0.numel()
+        blank = lambda x: [torch.zeros(x, device="cuda")]
+        before = {"w": [w0], "g": [g0], "m": blank(k), "v": blank(k), "m_scale": None, "v_scale": None, "master": None}
+        part = slice(at.start // B, -(-at.stop // B))
+        view = lambda x: [x[at].view(E4M3) if bits == 8 else x[at]]
+        after = {"w": [w[at]], "g": [g0], "m": view(m), "v": view(v), "m_scale": [scales[0][part]] if bits == 8 else None,
+                 "v_scale": [scales[1][part]] if bits == 8 else None, "master": None}
+        if bits == 8:
+            before |= {"m_scale": [torch.zeros_like(scales[0][part])], "v_scale": [torch.zeros_like(scales[1][part])]}
+        check_step(before, after, 1)
+    assert bool((w[spots[0].stop:spots[0].stop + 1000] == 0).all())
+
+
+def test_the_workspace_goes_by_the_count_alone():
+    """Gradients that move off the alignment need no other workspace."""
+    s = model([3_000_000, 500_000, 70_000], "f32", "f32")
+    plan = plan_of(s)
+    ws, out = resbm.grad_norm_workspace(plan), torch.empty(2, device="cuda")
+    moved = [torch.empty(g.numel() + 1, device="cuda")[1:] if i != 1 else g for i, g in enumerate(s["g"])]
+    for a, b in zip(moved, s["g"]):
+        a.copy_(b)
+    plan.set_grads(moved)
+    assert resbm.grad_norm_workspace(plan).numel() == ws.numel()
+    resbm.resbm_grad_norm(plan, 0.0, out, ws)
+    want = norm_of(s["g"])
+    assert abs(float(out[0]) - want) <= 20 * U * want
+    s["g"] = moved
+    before = copy_of(s)
+    resbm.resbm_adamw_step(plan, step=4, **HYPER)
+    check_step(before, s, 4)

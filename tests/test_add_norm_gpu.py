@@ -259,3 +259,25 @@ def test_binding_refusals():
                  (X, None, gamma, EPS, None, None, Q, torch.empty(4, 4, device="cuda"), 16)):
         with pytest.raises((resbm.ResbmError, ValueError)):
             fn(*args)
+
+
+@pytest.mark.parametrize("d", [4096, 4097])
+def test_offsets_past_32_bits(d):
+    """Over 2^31 elements: the first and the last rows."""
+    T = (1 << 31) // d + 777
+    free, _ = torch.cuda.mem_get_info()
+    if free < 60 << 30:
+        pytest.skip("needs 60 GB")
+    X, A = (torch.zeros(T, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    spots = (slice(0, 50), slice(T - 800, T))
+    for i, at in enumerate(spots):
+        k = X[at].shape[0]
+        X[at], A[at] = rows(k, d, "bf16", i), rows(k, d, "bf16", 5 + i)
+    gamma = gamma_of(d, "bf16")
+    o = {"H": torch.empty_like(X), "N": torch.empty_like(X), "Q": torch.empty(T, d, dtype=torch.uint8, device="cuda"), "S": torch.empty(T, -(-d // 128), device="cuda")}
+    resbm.resbm_add_rmsnorm_fwd(X, A, gamma, EPS, o["H"], o["N"], o["Q"], o["S"], 128)
+    pad = {"H": float("nan"), "N": float("nan"), "Q": 0x55, "S": -7.0}   # (check() looks at two rows behind as well)
+    for at in spots:
+        k = X[at].shape[0]
+        part = {n: torch.cat((t[at], torch.full((2, t.shape[1]), pad[n], device="cuda").to(t.dtype))) for n, t in o.items()}
+        check(X[at], A[at], gamma, EPS, part, k, d, 128)

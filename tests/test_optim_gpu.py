@@ -242,6 +242,53 @@ def test_add_norm_gradients_by_differences():
         assert abs(slope - float((grad * way).sum())) <= 1e-2 * float(grad.norm()), (i, slope)
 
 
+def test_add_norm_captured_both_ways():
+    """Forward and backward in one CUDA graph, replayed with other inputs; nothing eager of the same leaves is alive."""
+    T, d = 64, 300
+    leaves = [torch.zeros(T, d, device="cuda", requires_grad=True), torch.zeros(T, d, device="cuda", requires_grad=True),
+              torch.ones(d, device="cuda", requires_grad=True)]
+    dh, dn = torch.zeros(T, d, device="cuda"), torch.zeros(T, d, device="cuda")
+
+    def both_ways():
+        h, n = pipeline.add_norm(*leaves)
+        torch.autograd.backward((h, n), (dh, dn))
+        return h.detach(), n.detach()
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        both_ways()
+    torch.cuda.current_stream().wait_stream(side)
+    for t in leaves:
+        t.grad = None
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        h, n = both_ways()
+    g = torch.Generator(device="cuda").manual_seed(11)
+    for _ in range(2):
+        new = [torch.randn(t.shape, generator=g, device="cuda") for t in leaves]
+        with torch.no_grad():
+            for t, x in zip(leaves, new):
+                t.copy_(x)
+        for t in (dh, dn):
+            t.copy_(torch.randn(T, d, generator=g, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = [x.clone().requires_grad_() for x in new]
+        eh, en = pipeline.add_norm(*eager)
+        torch.autograd.backward((eh, en), (dh, dn))
+        assert torch.equal(h, eh) and torch.equal(n, en)
+        assert all(torch.equal(t.grad, e.grad) for t, e in zip(leaves, eager))
+
+
+def test_add_norm_has_no_second_derivative():
+    x = torch.randn(4, 8, device="cuda", requires_grad=True)
+    n = pipeline.add_norm(x, x, torch.ones(8, device="cuda"))[1]
+    (g,) = torch.autograd.grad(n.sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError):
+        g.sum().backward()
+
+
 @pytest.mark.parametrize("wiring", ["A", "B"])
 @pytest.mark.parametrize("fuse_norm", [True, False])
 def test_fused_norms_match_the_unfused_model(wiring, fuse_norm):

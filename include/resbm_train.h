@@ -100,7 +100,8 @@ typedef struct {
 } resbm_adamw_tensor;
 
 /* The hyperparameters of one step. The pointers (device memory, or NULL) are read by the kernel, so that a
- * captured step can be replayed with other values: lr_dev stands for lr, step_dev for step; grad_scale is
+ * captured step can be replayed with other values: lr_dev stands for lr, step_dev for step (a value below 1 counts
+ * as 1); grad_scale is
  * multiplied to the gradients (out[1] of resbm_grad_norm, or the inverse of a loss scale). Where *grad_scale
  * is not finite the step changes nothing. */
 typedef struct {

@@ -4,7 +4,7 @@
 // with 8-bit states 10, the norm 2. The list of tensors travels as the launch's parameter (up to 448 tensors, 31 KB), so
 // that nothing is copied to the device and a captured launch carries its own list; a list of up to 32 takes the small
 // parameter (2.2 KB; one call on the host 5.1 us, 5.5 with the large one). 308 M bf16 parameters on a GB300: 32-bit states
-// 963 us (7.0 TB/s; a copy moves 6.8), 8-bit states 446 (7.0 TB/s), norm 94 (6.6 TB/s).
+// 963 us (7.0 TB/s; a copy moves 6.8), 8-bit states 446 (7.0 TB/s), norm 92 (6.7 TB/s).
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -31,8 +31,8 @@ constexpr int kBlock = RESBM_STATE_BLOCK;             // elements a warp takes a
 __host__ __device__ constexpr int deep_of(int bits) { return bits == 8 ? 2 : 1; }
 constexpr int kSmall = 32, kLarge = 448;              // tensors a launch, by the parameter's size
 constexpr int kNormGrid = 1216;                       // most CTAs of the gradients' norm: eight on each of 152 SMs
-// Gradients for a CTA of the norm to be worth it, two rounds of loads in bf16: 10.5 M gradients 10.4 us (12.0 with half as
-// many, 11.8 with four times)
+// Gradients for a CTA of the norm to be worth it, two rounds of loads in bf16: 10.5 M gradients 1.6 us less than with half as
+// many, 1.4 than with four times
 constexpr int kRound = 16384;
 constexpr float kLeastRoot = 0x1p-63f;                // sqrt(2^-126)
 constexpr uint64_t kMagic = 0x7265736264616d77ull;
@@ -282,7 +282,7 @@ __global__ void __launch_bounds__(kThreads, VEC && BITS == 8 ? 8 : 1) k_adamw(co
     }
     if (h.lr_dev || h.step_dev) {
         const float lr = h.lr_dev ? *h.lr_dev : h.lr;
-        const float t = h.step_dev ? (float)*h.step_dev : h.t;
+        const float t = h.step_dev ? fmaxf((float)*h.step_dev, 1.0f) : h.t;
         h.step_size = lr / -expm1f(t * h.lnb1);
         h.root = 1.0f / sqrtf(-expm1f(t * h.lnb2));
         h.decay = 1.0f - lr * h.wd;
@@ -395,22 +395,36 @@ __global__ void __launch_bounds__(kThreads) k_grad_squares(const __grid_constant
     }
 }
 
-constexpr int kNormThreads = 1024;
+// The partial sums in 64 bits. FP64 adds are slow here, so that a CTA of 256 threads with its loads in one round and its
+// warps' sums through another tree takes 4 us less than one of 1024 whose first thread adds them up (308 M gradients 96 -> 92 us,
+// 10.5 M 10.5 -> 8.4 with the host's 7.1); 512 threads 92.8, 128 92.1.
+constexpr int kNormThreads = 256;
 __global__ void __launch_bounds__(kNormThreads) k_grad_norm(const double *__restrict__ part, int64_t parts, float max_norm, float *__restrict__ out)
 {
-    __shared__ double sums[kNormThreads / 32];
+    constexpr int kW = kNormThreads / 32, kDeep = 5;   // (a full grid's partial sums in one round of loads)
+    __shared__ double sums[kW];
     griddep_wait();
     griddep_launch_dependents();
+    const int lane = threadIdx.x & 31;
     double sum = 0.0;
-    for (int64_t k = threadIdx.x; k < parts; k += kNormThreads) sum += part[k];
+    for (int64_t k = threadIdx.x; k < parts; k += kDeep * kNormThreads) {
+        double x[kDeep];
+#pragma unroll
+        for (int j = 0; j < kDeep; ++j) x[j] = k + j * kNormThreads < parts ? part[k + j * kNormThreads] : 0.0;
+#pragma unroll
+        for (int j = 0; j < kDeep; ++j) sum += x[j];
+    }
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = sum;
+    if (lane == 0) sums[threadIdx.x >> 5] = sum;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int k = 1; k < kNormThreads / 32; ++k) sum += sums[k];
-        const float norm = (float)sqrt(sum);
-        out[0] = norm;
-        out[1] = !isfinite(norm) ? __int_as_float(0x7fffffff) : max_norm > 0.0f ? fminf(1.0f, max_norm / (norm + 1e-6f)) : 1.0f;
+    if (threadIdx.x < 32) {
+        sum = lane < kW ? sums[lane] : 0.0;
+        for (int o = kW / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (lane == 0) {
+            const float norm = (float)sqrt(sum);
+            out[0] = norm;
+            out[1] = !isfinite(norm) ? __int_as_float(0x7fffffff) : max_norm > 0.0f ? fminf(1.0f, max_norm / (norm + 1e-6f)) : 1.0f;
+        }
     }
 }
 

@@ -105,7 +105,6 @@ template <int V> struct Codes {
 #pragma unroll
         for (int i = 0; i < V / 4; ++i) w[i] = e4m3x4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
     }
-    __device__ __forceinline__ Codes() {}
     __device__ __forceinline__ void store(uint8_t *p) const
     {
         if constexpr (V == 8) *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
@@ -266,10 +265,11 @@ template <typename T, int NW, int KV, typename Get> __device__ __forceinline__ v
     }
 }
 
-// CTAs of the most threads that an SM holds at least, which bounds the registers: 64 a thread for a CTA a row (without it
-// the compiler takes 77 at three vectors a thread: bf16 T = 65536, d = 4096 to e4m3 305 us instead of 265, T = 10000, d = 5001
-// three vectors a thread 162 instead of 102), 64 for a warp a row, but 80 for the realignment of four bf16 vectors (T = 20000, d = 1001 57 us without
-// a bound, 38 at 80, 41 at 64; d = 301 78 and 70 at 64). Eight vectors a thread need all they can get.
+// CTAs (of the most threads) that an SM holds at least, which bounds the registers. A CTA a row: 64 registers a thread;
+// with three vectors and no bound the compiler takes 77 (bf16 T = 65536, d = 4096 to e4m3 305 us instead of 265, the
+// realigned T = 10000, d = 5001 162 instead of 102). A warp a row: 64, but 80 for four bf16 vectors, whose realignment
+// needs them (T = 20000, d = 1001 57 us without a bound, 38 at 80, 41 at 64; two vectors, d = 301: 78 without, 70 at 64).
+// Eight vectors a thread need all that they can get.
 template <typename E, int KV, int MAXT> constexpr int min_ctas()
 {
     return MAXT == 32 ? (KV == 4 && sizeof(E) == 2 ? 3 : 4) : KV <= 4 ? 2 : 1;

@@ -69,6 +69,7 @@ struct Step {
     float root;                   // 1 / sqrt(1 - beta2^t)
     float eps, decay;             // decay: 1 - lr weight_decay
     float least;                  // the smallest denominator: of v = 2^-126, with eps
+    float nought;                 // minus zero (alone)
     float lr, wd, lnb1, lnb2, t;  // for the values that the device gives
     const float *lr_dev;
     const int64_t *step_dev;
@@ -170,9 +171,14 @@ __device__ __forceinline__ float approx_rcp(float v)
     return r;
 }
 
+// A product that is rounded by itself although a sum follows. Left as a product the compiler makes one fused
+// multiply-add of it and the sum, whatever rounding the two were written with; what this one adds is minus zero, which
+// leaves every value as it is, and which the compiler does not know.
+__device__ __forceinline__ Pair alone(Pair a, Pair b, const Step &h) { return fma(a, b, both(h.nought)); }
+
 // K blocks of 256 elements by one warp, kWarps blocks apart (or one, the last `rem` of a tensor). The products of the
-// running means are rounded one by one: a fused multiply-add would move values next to a rounding border of e4m3 across
-// it, and the same step would then depend on the compiler's contractions. The root and the quotient m / (sqrt(v) ..) are
+// running means are rounded one by one (alone): a fused multiply-add would move values next to a rounding border of e4m3
+// across it, and the same step would then depend on the compiler's contractions. The root and the quotient m / (sqrt(v) ..) are
 // approximate, far below what the update is to the weight. A v below 2^-126 (gradients below 1e-17) counts as that for
 // the weight (`least` is its denominator), as zero for the 8-bit state.
 // The 8-bit form is bound by instructions as much as by memory (10 bytes an element): with IEEE roots and quotients, one
@@ -211,8 +217,8 @@ __device__ __forceinline__ void adamw_blocks(W *w, const G *g, void *mp, void *v
                 v2 = v2 * both(sv[k]);
                 v2 = v2 * v2;
             }
-            m2 = m2 * both(h.b1) + g2 * both(h.omb1);
-            v2 = v2 * both(h.b2) + (g2 * g2) * both(h.omb2);
+            m2 = alone(m2, both(h.b1), h) + alone(g2, both(h.omb1), h);
+            v2 = alone(v2, both(h.b2), h) + alone(g2 * g2, both(h.omb2), h);
             float m0, m1, v0, v1, d0, d1;
             split(m2, m0, m1);
             split(v2, v0, v1);
@@ -677,6 +683,7 @@ resbm_status resbm_adamw_step(const void *plan, const resbm_adamw_hyper *hyper, 
     h.eps = (float)a.eps;
     h.decay = (float)(1.0 - a.lr * a.weight_decay);
     h.least = h.root * kLeastRoot + h.eps;
+    h.nought = -0.0f;
     h.lr = (float)a.lr;
     h.wd = (float)a.weight_decay;
     h.t = (float)t;

@@ -5,7 +5,8 @@
 
 namespace resbm {
 
-// Pairs of floats: one instruction for two products or sums, each rounded to nearest even as by itself.
+// Pairs of floats: one instruction for two products or sums, each rounded to nearest even as by itself, but for a product
+// whose only use is a sum: the compiler may make a fused multiply-add of the two.
 struct Pair {
     uint64_t v;
 };

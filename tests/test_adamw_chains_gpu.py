@@ -1,0 +1,83 @@
+"""Chains of AdamW steps beside the same arithmetic in IEEE fp32: the states that a step leaves are what the next one reads, so
+that a rounding that differs once is a difference that stays (an 8-bit code that goes the other way is up to 1 / 8 off).
+
+The reference rounds to fp32 after every operation: it computes each in 64 bits from fp32 values and rounds the result once.
+For sums, products, quotients and roots of fp32 values that is IEEE's own result (53 bits are at least twice 24 and two more).
+The running means, their scales and their codes have no other freedom, so they have to be equal bit for bit."""
+import pytest
+import torch
+
+from paper_2604_11947_gb300 import resbm
+from test_adamw_gpu import B, E4M3, FORMS, HYPER, copy_of, model, plan_of
+
+pytestmark = pytest.mark.gpu
+SIZES = [1, 255, 257, 2048, 4099, 70001]
+STEPS = 20
+
+
+def f(x):
+    """x (64 bits) rounded to fp32, as a number in 64 bits"""
+    return x.float().double()
+
+
+def const(x):
+    return float(torch.tensor(x, dtype=torch.float32))
+
+
+def decode(code, scale):
+    """e4m3 codes in units of their blocks' scales, rounded to fp32"""
+    return f(code.double() * scale.double().repeat_interleave(B)[:code.numel()])
+
+
+def encode(x, least=False):
+    """Codes and scales of x; least: a value above zero keeps a code above zero"""
+    blocks = torch.nn.functional.pad(x.abs(), (0, -x.numel() % B)).view(-1, B)
+    most = blocks.amax(dim=1).clamp_min(2.0 ** -100)
+    inv = f(f(1 / most) * 448).repeat_interleave(B)[:x.numel()]
+    y = f(x * inv)
+    if least:
+        y = torch.where(x > 0, y.clamp_min(2.0 ** -9), y)
+    return y.clamp(-448, 448).float().to(E4M3), f(most * const(1 / 448)).float()
+
+
+def means(s, i, h=HYPER):
+    """m and v of tensor i after a step, rounded after every operation"""
+    b1, b2, c1, c2 = const(h["beta1"]), const(h["beta2"]), const(1 - h["beta1"]), const(1 - h["beta2"])
+    g = s["g"][i].double()
+    if s["m_scale"] is None:
+        m, v = s["m"][i].double(), s["v"][i].double()
+    else:
+        m, v = decode(s["m"][i], s["m_scale"][i]), decode(s["v"][i], s["v_scale"][i])
+        v = f(v * v)
+    return f(f(m * b1) + f(g * c1)), f(f(v * b2) + f(f(g * g) * c2))
+
+
+def same(a, b):
+    return torch.equal(a.view(torch.uint8) & 0x7F, b.view(torch.uint8) & 0x7F) if a.element_size() == 1 else torch.equal(a, b)
+
+
+def fresh_gradients(s, t):
+    gen = torch.Generator(device="cuda").manual_seed(1000 + t)
+    for g in s["g"]:
+        g.copy_(1e-3 * torch.exp(torch.randn(1, generator=gen, device="cuda")) * torch.randn(g.numel(), generator=gen, device="cuda"))
+
+
+@pytest.mark.parametrize("offset", [0, 1])
+@pytest.mark.parametrize("w,g,bits,master", FORMS)
+def test_running_means_round_every_product(w, g, bits, master, offset):
+    """Twenty steps: m (codes and scales, or fp32) and fp32 v are the reference's own bits."""
+    s = model(SIZES, w, g, bits, master, offset=offset)
+    plan, mine = plan_of(s), copy_of(s)
+    for t in range(1, STEPS + 1):
+        fresh_gradients(s, t)
+        mine["g"] = s["g"]
+        resbm.resbm_adamw_step(plan, step=t + 100, **HYPER)
+        for i in range(len(SIZES)):
+            m, v = means(mine, i)
+            if bits == 32:
+                mine["m"][i], mine["v"][i] = m.float(), v.float()
+                assert same(s["v"][i], mine["v"][i]), (t, i)
+            else:
+                mine["m"][i], mine["m_scale"][i] = encode(m)
+                assert same(s["m_scale"][i], mine["m_scale"][i]), (t, i)
+            assert same(s["m"][i], mine["m"][i]), (t, i)

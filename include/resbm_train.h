@@ -126,9 +126,11 @@ RESBM_API resbm_status resbm_adamw_plan(const resbm_adamw_desc *desc, const resb
 /* One AdamW step (decoupled weight decay) over the plan's tensors, for t = step and c = *grad_scale (or 1):
  *   g' = c g;  m = beta1 m + (1 - beta1) g';  v = beta2 v + (1 - beta2) g'^2
  *   w = (1 - lr weight_decay) w - lr m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps)
- * in fp32, every tensor in place; the new m and v go into w before they are rounded to 8 bits. The root and the
- * quotient are within 2^-21 of theirs (relative to the update); a v below 2^-126 (gradients under 1e-17) counts as
- * 2^-126 there, and as zero in an 8-bit state. One launch for up to 448 tensors of a kind (aligned or not). Errors: RESBM_ERR_INVALID_ARG for a bad hyperparameter or for a plan that is none or has
+ * in fp32, every tensor in place; the new m and v go into w before they are rounded to 8 bits. m, v and the sqrt(v) of an
+ * 8-bit state are rounded after every operation (from v = 2^-102 on; below it sqrt(v) is within a bit). The root and the
+ * quotient of w are within 2^-21 of theirs (relative to the update); a v below 2^-126 (gradients under 1e-17) counts as
+ * 2^-126 there. A v beyond fp32 (gradients over 1e19) is an infinity with 32-bit states, where the weight then only decays;
+ * with 8-bit ones the weight and its block's sqrt(v) become NaN. One launch for up to 448 tensors of a kind (aligned or not). Errors: RESBM_ERR_INVALID_ARG for a bad hyperparameter or for a plan that is none or has
  * RESBM_STATE_NONE. */
 RESBM_API resbm_status resbm_adamw_step(const void *plan, const resbm_adamw_hyper *hyper, void *stream);
 

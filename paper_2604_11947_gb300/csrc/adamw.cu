@@ -34,7 +34,7 @@ constexpr int kNormGrid = 1216;                       // most CTAs of the gradie
 // Gradients for a CTA of the norm to be worth it, two rounds of loads in bf16: 10.5 M gradients 1.6 us less than with half as
 // many, 1.4 than with four times
 constexpr int kRound = 16384;
-constexpr float kLeastRoot = 0x1p-63f;                // sqrt(2^-126)
+constexpr float kLeastNormal = 0x1p-126f, kLeastRoot = 0x1p-63f;   // (the second its root)
 constexpr uint64_t kMagic = 0x7265736264616d77ull;
 
 // The tensors of one launch, of one kind: those whose accesses are vectors (everything of a tensor aligned to eight
@@ -164,11 +164,33 @@ __device__ __forceinline__ float approx_sqrt(float v)
     asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
+__device__ __forceinline__ float approx_rsqrt(float v)
+{
+    float r;
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
 __device__ __forceinline__ float approx_rcp(float v)
 {
     float r;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
+}
+
+// Two roots to nearest, for the roots that are stored: an 8-bit code next to a border takes the other side with the last bit of
+// what it is made from. From an approximate reciprocal root y, r = v y and the remainder v - r^2 (exact as a fused
+// multiply-add), one step of Newton's method (Markstein, "Computation of elementary functions on the IBM RISC System/6000
+// processor", 1990): r + (v - r^2) y / 2. Compared with __fsqrt_rn for every float: equal from 2^-102 on, where the
+// remainder is no denormal yet, below within a bit; from 2^-126 down 2^63 v or less, but above zero where v is. Infinity
+// gives a NaN (a choice of infinity costs 45 us, at 64 registers a thread). The 8-bit step of 308 M elements takes 459 us
+// with it, 541 with __fsqrt_rn, 447 with approximate roots, of which one in six is a bit off.
+__device__ __forceinline__ void roots(Pair v, float &r0, float &r1)
+{
+    float v0, v1;
+    split(v, v0, v1);
+    const Pair y = pair(approx_rsqrt(fmaxf(v0, kLeastNormal)), approx_rsqrt(fmaxf(v1, kLeastNormal))), r = v * y;
+    split(r, r0, r1);
+    split(fma(pair(fmaf(-r0, r0, v0), fmaf(-r1, r1, v1)), y * both(0.5f), r), r0, r1);
 }
 
 // A product that is rounded by itself although a sum follows. Left as a product the compiler makes one fused
@@ -178,12 +200,14 @@ __device__ __forceinline__ Pair alone(Pair a, Pair b, const Step &h) { return fm
 
 // K blocks of 256 elements by one warp, kWarps blocks apart (or one, the last `rem` of a tensor). The products of the
 // running means are rounded one by one (alone): a fused multiply-add would move values next to a rounding border of e4m3
-// across it, and the same step would then depend on the compiler's contractions. The root and the quotient m / (sqrt(v) ..) are
-// approximate, far below what the update is to the weight. A v below 2^-126 (gradients below 1e-17) counts as that for
-// the weight (`least` is its denominator), as zero for the 8-bit state.
+// across it, and the same step would then depend on the compiler's contractions; so would an approximate sqrt(v) where it is
+// stored (roots). The quotient m / (sqrt(v) ..) is approximate, far below what the update is to the weight, and so is
+// the root with 32-bit states. A v below 2^-126 (gradients below 1e-17) counts as that for the weight (`least` is its
+// denominator).
 // The 8-bit form is bound by instructions as much as by memory (10 bytes an element): with IEEE roots and quotients, one
 // value an instruction and one block a warp 75 of them an element, 868 us for 308 M elements; with pairs 52 and 597; with
-// two blocks a warp, accesses of eight elements and one reciprocal an element 34 and 448.
+// two blocks a warp, accesses of eight elements and approximate roots and reciprocals 34 and 448; with the stored roots to
+// nearest 459.
 template <typename W, typename G, bool MASTER, int BITS, Mode MODE, int K>
 __device__ __forceinline__ void adamw_blocks(W *w, const G *g, void *mp, void *vp, float *ms, float *vs, float *master,
                                              int lane, int rem, const Step &h, float c)
@@ -222,7 +246,13 @@ __device__ __forceinline__ void adamw_blocks(W *w, const G *g, void *mp, void *v
             float m0, m1, v0, v1, d0, d1;
             split(m2, m0, m1);
             split(v2, v0, v1);
-            const float r0 = approx_sqrt(v0), r1 = approx_sqrt(v1);
+            float r0, r1;
+            if (BITS == 8) {
+                roots(v2, r0, r1);
+            } else {
+                r0 = approx_sqrt(v0);
+                r1 = approx_sqrt(v1);
+            }
             split(fma(pair(r0, r1), both(h.root), both(h.eps)), d0, d1);
             const Pair q = m2 * pair(approx_rcp(max_nan(d0, h.least)), approx_rcp(max_nan(d1, h.least)));
             split(fma(q, both(-h.step_size), pair(x[k][j], x[k][j + 1]) * both(h.decay)), x[k][j], x[k][j + 1]);
@@ -241,9 +271,9 @@ __device__ __forceinline__ void adamw_blocks(W *w, const G *g, void *mp, void *v
             const E4m3Scale a = e4m3_scale(__reduce_max_sync(0xffffffffu, abs_bits(am))), b = e4m3_scale(__reduce_max_sync(0xffffffffu, abs_bits(av)));
 #pragma unroll
             for (int j = 0; j < 8; j += 2) {
-                // a sqrt(v) above zero (at least 2^-63 then) keeps a code above zero
+                // a sqrt(v) above zero (at least 2^-87 then) keeps a code above zero
                 float l0, l1;
-                split(pair(v[k][j], v[k][j + 1]) * both(0x1p60f), l0, l1);
+                split(pair(v[k][j], v[k][j + 1]) * both(0x1p78f), l0, l1);
                 split(pair(m[k][j], m[k][j + 1]) * both(a.inv), m[k][j], m[k][j + 1]);
                 split(pair(v[k][j], v[k][j + 1]) * both(b.inv), v[k][j], v[k][j + 1]);
                 v[k][j] = max_nan(v[k][j], fminf(l0, kE4m3Least));

@@ -81,3 +81,60 @@ def test_running_means_round_every_product(w, g, bits, master, offset):
                 mine["m"][i], mine["m_scale"][i] = encode(m)
                 assert same(s["m_scale"][i], mine["m_scale"][i]), (t, i)
             assert same(s["m"][i], mine["m"][i]), (t, i)
+
+
+@pytest.mark.parametrize("offset", [0, 1])
+@pytest.mark.parametrize("w,g,bits,master", [form for form in FORMS if form[2] == 8])
+def test_stored_roots_and_weights_after_many_steps(w, g, bits, master, offset):
+    """Twenty steps with 8-bit states: sqrt(v)'s codes and scales are the reference's own bits, and the weights are off by no
+    more than the steps' roundings together: 16 u of each update and 4 u of the weight (u = 2^-24, as for one step), and,
+    where the weight itself is what is kept, one rounding to its type a step."""
+    s = model(SIZES, w, g, bits, master, offset=offset)
+    plan, mine = plan_of(s), copy_of(s)
+    kept = "master" if master else "w"
+    weight = [x.double() for x in mine[kept]]
+    slack = [torch.zeros_like(x) for x in weight]
+    u = 2.0 ** -24
+    half = torch.finfo(s[kept][0].dtype).eps / 2
+    for t in range(1, STEPS + 1):
+        fresh_gradients(s, t)
+        mine["g"] = s["g"]
+        resbm.resbm_adamw_step(plan, step=t + 100, **HYPER)
+        for i in range(len(SIZES)):
+            m, v = means(mine, i)
+            root = f(v.sqrt())
+            mine["m"][i], mine["m_scale"][i] = encode(m)
+            mine["v"][i], mine["v_scale"][i] = encode(root, least=True)
+            assert same(s["v_scale"][i], mine["v_scale"][i]), (t, i)
+            assert same(s["v"][i], mine["v"][i]), (t, i)
+            n = t + 100
+            update = HYPER["lr"] / (1 - HYPER["beta1"] ** n) * m / (root / (1 - HYPER["beta2"] ** n) ** 0.5 + HYPER["eps"])
+            weight[i] = weight[i] * (1 - HYPER["lr"] * HYPER["weight_decay"]) - update
+            slack[i] += 4 * u * weight[i].abs() + 16 * u * update.abs()
+            if half > u:
+                slack[i] += half * (weight[i].abs() + slack[i])
+    for i in range(len(SIZES)):
+        off = (s[kept][i].double() - weight[i]).abs()
+        assert bool((off <= slack[i] + half * weight[i].abs()).all()), (i, float((off / slack[i]).max()))
+
+
+def test_small_and_large_second_moments_in_8_bits():
+    """Roots over the whole range: gradients whose squares leave fp32 at either end. Above zero stays above zero; an overflow
+    is seen, as NaN, in its own block and weight only."""
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    for size in (1e-17, 1e-12, 1e-6, 1.0, 1e6, 1e12):
+        s = model([3 * B], "f32", "f32", 8, warm=False)
+        s["g"][0].copy_(size * (1 + torch.rand(3 * B, generator=gen, device="cuda")))
+        mine = copy_of(s)
+        resbm.resbm_adamw_step(plan_of(s), step=1, lr=1e-3, beta1=0.0, beta2=0.5, eps=0.0, weight_decay=0.0)
+        v = f(f(mine["g"][0].double() ** 2) * 0.5)
+        code, scale = encode(f(v.sqrt()), least=True)
+        if size > 1e-15:
+            assert same(s["v"][0], code) and same(s["v_scale"][0], scale)
+        assert bool((s["v"][0].float() > 0).all())
+    s = model([3 * B], "f32", "f32", 8)
+    s["g"][0][B + 5] = 1e25
+    resbm.resbm_adamw_step(plan_of(s), step=1, **HYPER)
+    root = s["v"][0].float() * s["v_scale"][0].repeat_interleave(B)
+    assert torch.isnan(root).view(3, B).all(dim=1).tolist() == [False, True, False]
+    assert torch.isnan(s["w"][0]).nonzero().flatten().tolist() == [B + 5]

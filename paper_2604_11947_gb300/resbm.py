@@ -449,7 +449,9 @@ def resbm_add_rmsnorm_fwd(X, A, gamma, eps, H=None, N=None, Q=None, S=None, q_gr
     if (Q is None) != (S is None):
         raise ValueError("Q and S come together")
     if Q is not None:
-        groups = -(-d // q_group) if q_group > 0 else 1
+        if not 0 <= q_group < 1 << 31:   # (the descriptor's field has 32 bits: more would arrive as another group)
+            raise ValueError("q_group must be a power of two >= 32, or 0: got %d" % q_group)
+        groups = -(-d // q_group) if q_group else 1
         if Q.shape != shape or Q.element_size() != 1 or not Q.is_contiguous():
             raise ValueError("Q must be %s, dense, one byte an element" % (tuple(shape),))
         if S.shape != (T, groups) or S.dtype != torch.float32 or not S.is_contiguous():

@@ -1,0 +1,45 @@
+"""The binding's checks of include/resbm_train.h's calls, on the host: host tensors stand for device tensors, and a stand-in for
+the library records what would have reached it."""
+import pytest
+import torch
+
+from paper_2604_11947_gb300 import resbm
+
+
+class Library:
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        return lambda *args: self.calls.append((name, args)) or resbm.RESBM_OK
+
+
+@pytest.fixture
+def lib(monkeypatch):
+    lib = Library()
+    monkeypatch.setattr(resbm, "_lib", lib)
+    monkeypatch.setattr(resbm, "_device", lambda: torch.zeros(1).get_device())
+    return lib
+
+
+def norm(T=4, d=64, group=32, Q=None, groups=None):
+    X, gamma = torch.zeros(T, d, dtype=torch.bfloat16), torch.zeros(d, dtype=torch.bfloat16)
+    Q = torch.zeros(T, d, dtype=torch.uint8) if Q is None else Q
+    groups = (-(-d // group) if group > 0 else 1) if groups is None else groups
+    resbm.resbm_add_rmsnorm_fwd(X, None, gamma, 1e-5, None, None, Q, torch.zeros(T, groups), group, stream=0)
+
+
+def test_a_norm_reaches_the_library(lib):
+    norm()
+    norm(group=0)
+    norm(group=1 << 30)
+    assert [name for name, _ in lib.calls] == ["resbm_add_rmsnorm_fwd"] * 3
+    assert [args[0].q_group for _, args in lib.calls] == [32, 0, 1 << 30]
+
+
+@pytest.mark.parametrize("group", [(1 << 32) + 32, (1 << 32), 32 - (1 << 32), -32, 1 << 31, 1 << 40])
+def test_groups_that_the_descriptor_cannot_hold(lib, group):
+    """A group over 32 bits would arrive as another one, whose scales S has no room for."""
+    with pytest.raises(ValueError):
+        norm(group=group)
+    assert not lib.calls

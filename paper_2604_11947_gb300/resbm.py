@@ -404,6 +404,7 @@ def resbm_ffn_down_encode_fwd(desc, H, W2, X, We1, We2, B, P_save, F_out, ws, st
 
 # ---- the training step's operators around the boundary (include/resbm_train.h) ----------------
 _DT = {torch.float32: RESBM_F32, torch.bfloat16: RESBM_BF16}
+_CODES = (torch.float8_e4m3fn, torch.uint8)
 
 
 def _want(ok, what):
@@ -452,8 +453,8 @@ def resbm_add_rmsnorm_fwd(X, A, gamma, eps, H=None, N=None, Q=None, S=None, q_gr
         if not 0 <= q_group < 1 << 31:   # (the descriptor's field has 32 bits: more would arrive as another group)
             raise ValueError("q_group must be a power of two >= 32, or 0: got %d" % q_group)
         groups = -(-d // q_group) if q_group else 1
-        if Q.shape != shape or Q.element_size() != 1 or not Q.is_contiguous():
-            raise ValueError("Q must be %s, dense, one byte an element" % (tuple(shape),))
+        if Q.shape != shape or Q.dtype not in _CODES or not Q.is_contiguous():
+            raise ValueError("Q must be %s, dense, float8_e4m3fn or uint8" % (tuple(shape),))
         if S.shape != (T, groups) or S.dtype != torch.float32 or not S.is_contiguous():
             raise ValueError("S must be (%d, %d), fp32, dense" % (T, groups))
         _here(Q, device, "Q")
@@ -497,7 +498,7 @@ class AdamWPlan:
             _want(not x or (x[0].dtype in _DT and all(t.dtype == x[0].dtype for t in x)), "%s: fp32 or bf16, one type in a plan" % k)
         sizes = [g.numel() for g in grads]
         blocks = [-(-n // RESBM_STATE_BLOCK) for n in sizes]
-        codes = (torch.float8_e4m3fn, torch.uint8) if state == RESBM_STATE_E4M3 else (torch.float32,)
+        codes = _CODES if state == RESBM_STATE_E4M3 else (torch.float32,)
         for k, x in self._fields.items():
             types = (x[0].dtype,) if k in ("w", "g") and x else codes if k in ("m", "v") else (torch.float32,)
             for t, n in zip(x, blocks if k.endswith("_scale") else sizes):

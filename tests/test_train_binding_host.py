@@ -43,3 +43,13 @@ def test_groups_that_the_descriptor_cannot_hold(lib, group):
     with pytest.raises(ValueError):
         norm(group=group)
     assert not lib.calls
+
+
+@pytest.mark.parametrize("dtype", [torch.float8_e5m2, torch.int8, torch.bool, torch.float8_e4m3fnuz])
+def test_codes_of_other_types(lib, dtype):
+    """One-byte types that would read e4m3 codes as other values"""
+    with pytest.raises(ValueError):
+        norm(Q=torch.zeros(4, 64, dtype=torch.uint8).view(dtype))
+    assert not lib.calls
+    norm(Q=torch.zeros(4, 64, dtype=torch.uint8).view(torch.float8_e4m3fn))
+    assert len(lib.calls) == 1

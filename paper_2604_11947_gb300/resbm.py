@@ -592,6 +592,7 @@ def resbm_grad_norm(plans, max_norm, out, ws, stream=None):
         raise ValueError("out must be 2 fp32")
     _here(out, device, "out")
     _here(ws, device, "ws")
+    _want(ws.is_contiguous(), "ws must be dense")   # (an expanded one is smaller than its elements)
     for p in plans:
         p._ready(device)
     st = load().resbm_grad_norm(array, len(plans), max_norm, out.data_ptr(), ws.data_ptr(), _nbytes(ws), _stream(stream))

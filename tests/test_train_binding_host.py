@@ -53,3 +53,16 @@ def test_codes_of_other_types(lib, dtype):
     assert not lib.calls
     norm(Q=torch.zeros(4, 64, dtype=torch.uint8).view(torch.float8_e4m3fn))
     assert len(lib.calls) == 1
+
+
+def test_workspace_of_the_norm_is_dense(lib):
+    """An expanded tensor counts as its elements and is memory for one of them."""
+    plan = type("Plan", (resbm.AdamWPlan,), {"__init__": lambda self: None})()
+    plan.device, plan._fields, plan._address = torch.zeros(1).get_device(), {"g": []}, 0
+    out = torch.zeros(2)
+    for ws in (torch.zeros(1, dtype=torch.uint8).expand(1 << 20), torch.zeros(1 << 12, dtype=torch.uint8)[::2]):
+        with pytest.raises(ValueError):
+            resbm.resbm_grad_norm(plan, 1.0, out, ws, stream=0)
+    assert not lib.calls
+    resbm.resbm_grad_norm(plan, 1.0, out, torch.zeros(1 << 12, dtype=torch.uint8), stream=0)
+    assert len(lib.calls) == 1

@@ -11,6 +11,7 @@ import torch
 from . import resbm
 
 _STATES = ("exp_avg", "exp_avg_sq")
+_COLUMNS = _STATES + ("exp_avg_scale", "exp_avg_sq_scale", "master")   # (in AdamWPlan's order)
 
 
 class AdamW(torch.optim.Optimizer):
@@ -71,22 +72,21 @@ class AdamW(torch.optim.Optimizer):
             st["master"] = p.detach().float()
 
     def _plan(self, key, params):
-        """The plan of a list of parameters: the last step's where nothing moved, with other gradients where only they did."""
+        """The plan of a list of parameters: the last step's where it is still of these tensors (parameters and states where they
+        were), with other gradients where only they moved."""
         grads = [p.grad if p.grad.is_contiguous() else p.grad.contiguous() for p in params]
-        where, gwhere = [p.data_ptr() for p in params], [g.data_ptr() for g in grads]
-        old = self._plans.get(key)
-        if old is not None and old[1] == where and all(a is b for a, b in zip(old[3], params)):
-            if old[2] != gwhere:
-                old[0].set_grads(grads)
-                old[2] = gwhere
-            else:
-                old[0]._fields["g"] = grads
-            return old[0]
         states = [self.state[p] for p in params]
-        column = lambda k: [st[k] for st in states] if k in states[0] else None
-        plan = resbm.AdamWPlan([p.detach() for p in params], grads, column("exp_avg"), column("exp_avg_sq"), column("exp_avg_scale"),
-                               column("exp_avg_sq_scale"), column("master"))
-        self._plans[key] = [plan, where, gwhere, params]
+        columns = {k: [st[k] for st in states] for k in _COLUMNS if k in states[0]}
+        where = [(t.data_ptr(), t.numel(), t.dtype) for column in (params, *columns.values()) for t in column]
+        gwhere = [g.data_ptr() for g in grads]
+        plan, *old = self._plans.pop(key, (None, None, None))   # (back once it is sound)
+        if plan is None or old[0] != where:
+            plan = resbm.AdamWPlan([p.detach() for p in params], grads, *[columns.get(k) for k in _COLUMNS])
+        elif old[1] != gwhere:
+            plan.set_grads(grads)
+        else:
+            plan._fields["g"] = grads
+        self._plans[key] = (plan, where, gwhere)
         return plan
 
     @torch.no_grad()
@@ -129,7 +129,7 @@ class AdamW(torch.optim.Optimizer):
             b1, b2 = group["betas"]
             resbm.resbm_adamw_step(plan, lr=float(group["lr"]), beta1=b1, beta2=b2, eps=group["eps"], weight_decay=group["weight_decay"],
                                    step=key[3], grad_scale=scale)
-            plan.release_grads()   # (zero_grad frees them; the launches that read them are on the stream already)
+            plan.release()   # (zero_grad frees the gradients, a program may drop or move the states; the launches are on the stream)
             for p in params:
                 self.state[p]["step"] = key[3]
         return loss

@@ -544,6 +544,11 @@ class AdamWPlan:
         """Lets the gradients' memory go: no step before the next set_grads."""
         self._fields["g"] = None
 
+    def release(self):
+        """Lets all of the tensors' memory go. The plan still has their addresses: a step after the next set_grads is the caller's
+        word that they are where they were."""
+        self._fields = {"g": None}
+
     def _ready(self, device):
         if device != self.device:
             raise ValueError("the plan's tensors are on device %d, not the current one (%d)" % (self.device, device))

@@ -1,0 +1,151 @@
+"""optim.AdamW where a program changes what the optimizer holds between steps: states cleared, replaced, moved; every step is
+checked against its definition in 64 bits from the tensors in opt.state and in the parameters, and against torch's where torch
+says what happens."""
+import copy
+import gc
+import weakref
+
+import pytest
+import torch
+
+from paper_2604_11947_gb300 import optim
+from test_adamw_gpu import check_step
+from test_optim_gpu import H, HYPER, columns, params_of, set_grads
+
+pytestmark = pytest.mark.gpu
+FORMS = [(torch.float32, 32, False), (torch.bfloat16, 8, False), (torch.bfloat16, 32, True), (torch.bfloat16, 8, True)]
+SIZES = [1, 300, 256, 5000]
+
+
+def grads_in_place(params, t):
+    """New values where the gradients are"""
+    gen = torch.Generator(device="cuda").manual_seed(t)
+    for p in params:
+        if p.grad is None:
+            p.grad = torch.zeros_like(p)
+        p.grad.copy_(1e-2 * torch.randn(p.shape, generator=gen, device="cuda"))
+
+
+def stepped(opt, params, t, step=None):
+    """One step with new gradients in place, checked from the state before it; `step`: which it is to the states"""
+    grads_in_place(params, t)
+    before = columns(opt, params) if all(opt.state[p] for p in params) else None
+    opt.step()
+    after = columns(opt, params)
+    if before is not None:
+        check_step(before, after, step or t, HYPER)
+    assert all(opt.state[p]["step"] == (step or t) for p in params)
+    return after
+
+
+@pytest.mark.parametrize("dtype,bits,master", FORMS)
+def test_cleared_states_start_again(dtype, bits, master):
+    """opt.state.clear(): the next step is the first one of new moments, as a new optimizer's on the same parameters."""
+    params = params_of(SIZES, dtype)
+    opt = optim.AdamW(params, state_bits=bits, master=master, **H)
+    for t in range(1, 6):
+        stepped(opt, params, t)
+    opt.state.clear()
+    others = [torch.nn.Parameter(p.detach().clone()) for p in params]
+    fresh = optim.AdamW(others, state_bits=bits, master=master, **H)
+    for t in range(1, 4):
+        stepped(opt, params, t)
+        grads_in_place(others, t)
+        fresh.step()
+        for p, q in zip(params, others):
+            assert torch.equal(p, q)
+            for k, v in opt.state[p].items():
+                o = fresh.state[q][k]
+                assert torch.equal(v.view(torch.uint8), o.view(torch.uint8)) if torch.is_tensor(v) else v == o, k
+    assert all(bool((opt.state[p]["exp_avg"].float() != 0).any()) for p in params)
+
+
+@pytest.mark.parametrize("dtype,bits,master", FORMS)
+def test_states_that_move(dtype, bits, master):
+    """Off the device and back, in one entry or all of them, as new tensors or under the same ones: the step goes on from what
+    opt.state holds and leaves its result there."""
+    params = params_of(SIZES, dtype)
+    opt = optim.AdamW(params, state_bits=bits, master=master, **H)
+    for t in range(1, 3):
+        stepped(opt, params, t)
+    for t, move in enumerate((lambda st, k: st.__setitem__(k, st[k].cpu().cuda()), lambda st, k: st.__setitem__(k, st[k].clone()),
+                              lambda st, k: setattr(st[k], "data", st[k].data.clone())), 3):
+        for p in params:
+            for k, v in list(opt.state[p].items()):
+                if torch.is_tensor(v):
+                    move(opt.state[p], k)
+        stepped(opt, params, t)
+    opt.state[params[1]]["exp_avg"] = opt.state[params[1]]["exp_avg"].clone()
+    stepped(opt, params, 6)
+    opt.state[params[2]].clear()     # one parameter starts again, the others go on
+    grads_in_place(params, 7)
+    before = columns(opt, params[:2] + params[3:])
+    opt.step()
+    check_step(before, columns(opt, params[:2] + params[3:]), 7, HYPER)
+    assert opt.state[params[2]]["step"] == 1 and bool((opt.state[params[2]]["exp_avg"].float() != 0).any())
+
+
+def test_states_on_another_device_are_refused():
+    params = params_of([300], torch.float32)
+    opt = optim.AdamW(params, **H)
+    stepped(opt, params, 1)
+    opt.state[params[0]]["exp_avg"] = opt.state[params[0]]["exp_avg"].cpu()
+    with pytest.raises(ValueError):
+        opt.step()
+    opt.state[params[0]]["exp_avg"] = opt.state[params[0]]["exp_avg"].cuda()
+    stepped(opt, params, 2)
+
+
+def test_resized_parameters_are_refused():
+    """A parameter that became shorter where it lies: its states are of another size, and nothing behind it is written."""
+    params = params_of([300], torch.float32)
+    opt = optim.AdamW(params, **H)
+    stepped(opt, params, 1)
+    whole, grad = params[0].data, params[0].grad
+    params[0].grad = None
+    params[0].data = whole[:100]
+    params[0].grad = grad[:100]
+    before = whole.clone()
+    with pytest.raises(ValueError):
+        opt.step()
+    torch.cuda.synchronize()
+    assert torch.equal(whole, before)
+
+
+def test_states_are_let_go():
+    """Between steps only opt.state holds the moments: a program that drops them or moves them off has their memory."""
+    params = params_of([1000, 300], torch.bfloat16)
+    opt = optim.AdamW(params, state_bits=8, master=True, max_grad_norm=1.0, **H)
+    for t in (1, 2):
+        grads_in_place(params, t)
+        opt.step()
+    held = [weakref.ref(v) for p in params for v in opt.state[p].values() if torch.is_tensor(v)]
+    opt.state.clear()
+    gc.collect()
+    assert all(h() is None for h in held)
+
+
+def test_refused_gradients_leave_no_trace():
+    """Gradients that overlap what the step writes are refused; the step after, with gradients where they were, goes on."""
+    params = params_of([300, 64], torch.float32)
+    opt = optim.AdamW(params, **H)
+    stepped(opt, params, 1)
+    good = params[0].grad
+    params[0].grad = params[0].detach()[:]
+    with pytest.raises(RuntimeError):
+        opt.step()
+    params[0].grad = good
+    stepped(opt, params, 2)
+
+
+def test_a_copied_optimizer_has_its_own_states():
+    """copy.deepcopy of an optimizer with its parameters: both go on by themselves."""
+    params = params_of([300], torch.float32)
+    opt = optim.AdamW(params, **H)
+    stepped(opt, params, 1)
+    twin = copy.deepcopy(opt)
+    others = twin.param_groups[0]["params"]
+    assert others[0] is not params[0]
+    stepped(opt, params, 2)
+    stepped(twin, others, 2)
+    assert torch.equal(params[0], others[0])

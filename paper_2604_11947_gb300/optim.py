@@ -107,29 +107,27 @@ class AdamW(torch.optim.Optimizer):
                 if not self.state[p]:
                     self._init_state(p)
                 work.setdefault((i, p.dtype, p.grad.dtype, self.state[p]["step"] + 1), []).append(p)
-        # (the plans of other lists than this step's are let go)
-        known, plans = {k[:3] for k in work}, []
-        self._plans = {k: v for k, v in self._plans.items() if k[:3] in known}
-        count = {}
-        for key, params in work.items():
-            n = count[key[:3]] = count.get(key[:3], -1) + 1
-            plans.append((key, params, self._plan(key[:3] + (n,), params)))
+        plans, kept = [], {}
+        for (i, dtype, g_dtype, step), params in work.items():
+            key = (i, dtype, g_dtype, *map(id, params))
+            plans.append((self.param_groups[i], step, params, self._plan(key, params)))
+            kept[key] = self._plans[key]
+        self._plans = kept   # (those of other lists than this step's are let go)
         scale = None
         if self.max_grad_norm is not None and plans:
-            each = [plan for _, _, plan in plans]
+            each = [plan for *_, plan in plans]
             need = resbm.resbm_grad_norm_workspace_bytes(each)
-            device = plans[0][1][0].device
+            device = plans[0][2][0].device
             if self._ws is None or self._ws.numel() < need or self._ws.device != device:
                 self._ws = torch.empty(max(need, 1), dtype=torch.uint8, device=device)
             self.grad_norm = torch.empty(2, device=device)
             resbm.resbm_grad_norm(each, self.max_grad_norm, self.grad_norm, self._ws)
             scale = self.grad_norm[1:]
-        for key, params, plan in plans:
-            group = self.param_groups[key[0]]
+        for group, step, params, plan in plans:
             b1, b2 = group["betas"]
             resbm.resbm_adamw_step(plan, lr=float(group["lr"]), beta1=b1, beta2=b2, eps=group["eps"], weight_decay=group["weight_decay"],
-                                   step=key[3], grad_scale=scale)
+                                   step=step, grad_scale=scale)
             plan.release()   # (zero_grad frees the gradients, a program may drop or move the states; the launches are on the stream)
             for p in params:
-                self.state[p]["step"] = key[3]
+                self.state[p]["step"] = step
         return loss

@@ -149,3 +149,48 @@ def test_a_copied_optimizer_has_its_own_states():
     stepped(opt, params, 2)
     stepped(twin, others, 2)
     assert torch.equal(params[0], others[0])
+
+
+def test_plans_of_other_lists_are_let_go():
+    """A list that is not stepped has no plan afterwards; parameters that took turns go on with the right moments."""
+    a, b = params_of([300, 64], torch.float32), params_of([1000], torch.float32, seed=1)
+    opt = optim.AdamW(a + b, **H)
+    stepped(opt, a, 1)             # (b has no gradient yet)
+    grads_in_place(a, 2)
+    grads_in_place(b, 2)
+    opt.step()
+    assert len(opt._plans) == 2 and opt.state[b[0]]["step"] == 1
+    main = next(plan for key, (plan, *_) in opt._plans.items() if plan.count == 2)
+    b[0].grad = None
+    stepped(opt, a, 3)
+    assert [plan for plan, *_ in opt._plans.values()] == [main]
+    for p in a:
+        p.grad = None
+    stepped(opt, b, 2)
+    assert [plan.count for plan, *_ in opt._plans.values()] == [1]
+    # b, a step behind, first in the step's order: a's plan is still a's
+    opt.param_groups[0]["params"] = b + a
+    for t in (4, 5):
+        grads_in_place(a + b, t)
+        before = columns(opt, a)
+        opt.step()
+        check_step(before, columns(opt, a), t, HYPER)
+        kept = {plan.count: plan for plan, *_ in opt._plans.values()}
+        assert len(kept) == 2 and (t == 4 or kept[2] is last)
+        last = kept[2]
+
+
+def test_removed_parameters_are_let_go():
+    params = params_of([300, 1000], torch.float32)
+    opt = optim.AdamW(params, max_grad_norm=1.0, **H)
+    for t in (1, 2):
+        grads_in_place(params, t)
+        opt.step()
+    gone = params.pop()
+    held = [weakref.ref(gone)] + [weakref.ref(v) for v in opt.state[gone].values() if torch.is_tensor(v)]
+    opt.param_groups[0]["params"] = params
+    del opt.state[gone], gone
+    grads_in_place(params, 3)
+    opt.step()
+    gc.collect()
+    assert all(h() is None for h in held)

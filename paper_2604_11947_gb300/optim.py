@@ -128,6 +128,7 @@ class AdamW(torch.optim.Optimizer):
             resbm.resbm_adamw_step(plan, lr=float(group["lr"]), beta1=b1, beta2=b2, eps=group["eps"], weight_decay=group["weight_decay"],
                                    step=step, grad_scale=scale)
             plan.release()   # (zero_grad frees the gradients, a program may drop or move the states; the launches are on the stream)
+            torch.autograd.graph.increment_version(params)   # (a backward through what they were raises, as after torch's steps)
             for p in params:
                 self.state[p]["step"] = step
         return loss

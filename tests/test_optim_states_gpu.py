@@ -194,3 +194,22 @@ def test_removed_parameters_are_let_go():
     opt.step()
     gc.collect()
     assert all(h() is None for h in held)
+
+
+@pytest.mark.parametrize("kind", ["here", "torch"])
+def test_a_backward_through_changed_weights_is_refused(kind):
+    """As after any change in place: what autograd kept of a weight before the step is not what the step left."""
+    params = params_of([300, 64], torch.float32)
+    make = optim.AdamW if kind == "here" else torch.optim.AdamW
+    opt = make(params, **H)
+    set_grads(params, 1)
+    still = params_of([64], torch.float32, seed=3)[0]
+    stale = sum((p * p).sum() for p in params)
+    other = (still * still).sum()
+    versions = [p._version for p in params]
+    opt.step()
+    assert all(p._version > v for p, v in zip(params, versions))
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        stale.backward()
+    other.backward()
+    sum((p * p).sum() for p in params).backward()

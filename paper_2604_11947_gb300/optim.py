@@ -68,8 +68,11 @@ class AdamW(torch.optim.Optimizer):
             else:
                 st[k] = torch.zeros(p.shape, dtype=torch.uint8, device=p.device).view(torch.float8_e4m3fn)
                 st[k + "_scale"] = torch.zeros(-(-p.numel() // resbm.RESBM_STATE_BLOCK), device=p.device)
+        self._init_master(p)
+
+    def _init_master(self, p):
         if self.master and p.dtype == torch.bfloat16:
-            st["master"] = p.detach().float()
+            self.state[p].update(bf16=True, master=p.detach().float())
 
     def _plan(self, key, params):
         """The plan of a list of parameters: the last step's where it is still of these tensors (parameters and states where they
@@ -77,7 +80,8 @@ class AdamW(torch.optim.Optimizer):
         grads = [p.grad if p.grad.is_contiguous() else p.grad.contiguous() for p in params]
         states = [self.state[p] for p in params]
         columns = {k: [st[k] for st in states] for k in _COLUMNS if k in states[0]}
-        where = [(t.data_ptr(), t.numel(), t.dtype) for column in (params, *columns.values()) for t in column]
+        tensors = [t for column in (params, *columns.values()) for t in column]
+        where = [t.data_ptr() for t in tensors] + [t.nbytes for t in tensors]
         gwhere = [g.data_ptr() for g in grads]
         plan, *old = self._plans.pop(key, (None, None, None))   # (back once it is sound)
         if plan is None or old[0] != where:
@@ -106,6 +110,8 @@ class AdamW(torch.optim.Optimizer):
                     raise ValueError("parameters are dense and contiguous, on the GPU")
                 if not self.state[p]:
                     self._init_state(p)
+                elif "master" not in self.state[p]:
+                    self._init_master(p)   # (a parameter that was fp32 before)
                 work.setdefault((i, p.dtype, p.grad.dtype, self.state[p]["step"] + 1), []).append(p)
         plans, kept = [], {}
         for (i, dtype, g_dtype, step), params in work.items():

@@ -213,3 +213,24 @@ def test_a_backward_through_changed_weights_is_refused(kind):
         stale.backward()
     other.backward()
     sum((p * p).sum() for p in params).backward()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_parameters_that_become_bf16_get_master_copies(bits):
+    params = params_of(SIZES, torch.float32)
+    opt = optim.AdamW(params, state_bits=bits, master=True, **H)
+    stepped(opt, params, 1)
+    assert all("master" not in opt.state[p] for p in params)
+    for p in params:
+        p.grad = None
+        p.data = p.data.bfloat16()
+    grads_in_place(params, 2)
+    before = columns(opt, params)
+    before["master"] = [w.float() for w in before["w"]]
+    opt.step()
+    assert all(opt.state[p]["master"].dtype == torch.float32 for p in params)
+    check_step(before, columns(opt, params), 2, HYPER)
+    stepped(opt, params, 3)
+    again = optim.AdamW(params, state_bits=bits, master=True, **H)
+    again.load_state_dict(copy.deepcopy(opt.state_dict()))
+    stepped(again, params, 4)

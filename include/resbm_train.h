@@ -52,9 +52,11 @@ typedef struct {
  *   H     : T x d out, or NULL. May be X or A itself (the same pointer and row stride): in place.
  *   N     : T x d out, or NULL.  Q : T x d bytes out (e4m3 codes, dense), or NULL; S : T x ceil(d / q_group)
  *           fp32 out (T x 1 for q_group = 0), given exactly when Q is. At least one of N and Q.
- * A row is read once and its sums stay on the chip; its mean square has to stay under 1e37 (fp32). Backward: resbm_rmsnorm_bwd with Y = H gives the
- * gradient that X and A share (dY_out, of the incoming dH and dN) and dgamma; for Q it is the straight-through
- * gradient (the rounding's own derivative taken as one).
+ * A row is read once and its sums stay on the chip, up to 32768 bf16 or 16384 fp32 columns; a longer one is read again for
+ * every further pass. A row's mean square has to stay under 1e37 (fp32), whatever its single elements are, and, with
+ * eps = 0, over 1e-33. Backward: resbm_rmsnorm_bwd with Y = H gives the gradient that X and A share (dY_out, of the
+ * incoming dH and dN) and dgamma; it forms s^3 in fp32, which asks for mean squares under 1e25. For Q it is the
+ * straight-through gradient (the rounding's own derivative taken as one).
  * Rows of X, A, H and N that are slices of one wider buffer are fine (equal strides, disjoint columns).
  * Errors: RESBM_ERR_INVALID_ARG for a bad size, stride, type, group, eps or flag, a missing or misaligned
  * pointer, S without Q, neither N nor Q, or an output that overlaps an input or another output otherwise. */

@@ -24,7 +24,8 @@ struct NormArgs {
     float *S;
     int64_t T, ldx, lda, ldh, ldn, groups;
     int d, group_log;             // columns behind a scale, as a power of two >= 32; 30 (over every d) for the whole row
-    float eps, inv_d;
+    float eps;
+    float part, whole;            // 1 / d as two factors, a square's and a sum's: a power of two of at most 1 / d, and the rest
 };
 
 template <int V> __device__ __forceinline__ void scale_by(float (&f)[V], float c)
@@ -68,11 +69,12 @@ template <typename E> struct Vec {
 #pragma unroll
         for (int i = 0; i < V / 2; ++i) set(i, get(i) + o.get(i));
     }
-    __device__ __forceinline__ float squares() const
+    // the sum of the squares, each times c
+    __device__ __forceinline__ float squares(float c) const
     {
         Pair s = both(0.0f);
 #pragma unroll
-        for (int i = 0; i < V / 2; ++i) s = fma(get(i), get(i), s);
+        for (int i = 0; i < V / 2; ++i) s = fma(get(i) * both(c), get(i), s);
         float a, b;
         split(s, a, b);
         return a + b;
@@ -333,14 +335,15 @@ __global__ void __launch_bounds__(MAXT == 32 ? 256 : MAXT, min_ctas<E, KV, MAXT>
         }
         float s = 0.0f;
 #pragma unroll
-        for (int k = 0; k < KV; ++k) s += h[k].squares();   // (of h as stored)
+        for (int k = 0; k < KV; ++k) s += h[k].squares(p.part);   // (of h as stored)
         if (p.H) {
             // (in place: a word of X or A that two threads read is read by both before either stores)
             if (SHIFT && kWide) __syncthreads();
             else if (SHIFT) __syncwarp();
             store(static_cast<E *>(p.H) + t * p.ldh, [&](int k) { return h[k]; });
         }
-        s *= p.inv_d;   // (a thread's share of the mean: the row's sum itself could leave fp32's range)
+        s *= p.whole;   // (a thread's share of the mean. A square, a thread's sum and the row's own could leave fp32's range where
+                        // the mean does not; scaled by a power of two before the square, none does, and no bit changes)
         load(b, gamma);   // on its way while the sums travel
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
@@ -478,14 +481,14 @@ template <typename E> __global__ void __launch_bounds__(1024) k_add_norm_long(co
         for (int64_t j = tid; j < p.d; j += 1024) {
             const float f = sum_at(j);
             if (ho) ho[j] = from_f32<E>(f);
-            s = fmaf(f * p.inv_d, f, s);
+            s = fmaf(f * p.part, f, s);
         }
         for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
         if (lane == 0) sums[warp] = s;
         __syncthreads();
         s = 0.0f;
         for (int w = 0; w < 32; ++w) s += sums[w];
-        const float rstd = 1.0f / sqrtf(s + p.eps);
+        const float rstd = 1.0f / sqrtf(s * p.whole + p.eps);
         uint32_t am = 0;
         for (int64_t j = tid; j < p.d; j += 1024) {
             const float n = h_at(j) * rstd * to_f32(gamma[j]);
@@ -604,7 +607,11 @@ extern "C" resbm_status resbm_add_rmsnorm_fwd(const resbm_add_norm_desc *desc, c
     Ctx c;
     resbm_status st = make_ctx(stream, &c);
     if (st != RESBM_OK || !t) return st;
-    NormArgs p{X, A, gamma, H, N, static_cast<uint8_t *>(Q), S, d.T, ldx, lda, ldh, ldn, groups, (int)d.d, 0, d.eps, (float)(1.0 / (double)d.d)};
+    NormArgs p{X, A, gamma, H, N, static_cast<uint8_t *>(Q), S, d.T, ldx, lda, ldh, ldn, groups, (int)d.d, 0, d.eps};
+    int log;
+    const double m = frexp(1.0 / (double)d.d, &log);   // 1 / d = m 2^log with m from 0.5 to under 1
+    p.part = (float)ldexp(1.0, log - 1);
+    p.whole = (float)(2.0 * m);
     p.group_log = d.q_group && d.q_group <= d.d ? __builtin_ctz((unsigned)d.q_group) : 30;
     const cudaError_t e = d.dtype == RESBM_F32 ? run<float>(p, c) : run<__nv_bfloat16>(p, c);
     if (e == cudaSuccess) count_launches(1);

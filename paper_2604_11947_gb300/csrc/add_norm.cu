@@ -25,6 +25,7 @@ struct NormArgs {
     int64_t T, ldx, lda, ldh, ldn, groups;
     int d, group_log;             // columns behind a scale, as a power of two >= 32; 30 (over every d) for the whole row
     float eps;
+    float inv_d;
     float part, whole;            // 1 / d as two factors, a square's and a sum's: a power of two of at most 1 / d, and the rest
 };
 
@@ -481,14 +482,14 @@ template <typename E> __global__ void __launch_bounds__(1024) k_add_norm_long(co
         for (int64_t j = tid; j < p.d; j += 1024) {
             const float f = sum_at(j);
             if (ho) ho[j] = from_f32<E>(f);
-            s = fmaf(f * p.part, f, s);
+            s = fmaf(f * p.inv_d, f, s);
         }
         for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
         if (lane == 0) sums[warp] = s;
         __syncthreads();
         s = 0.0f;
         for (int w = 0; w < 32; ++w) s += sums[w];
-        const float rstd = 1.0f / sqrtf(s * p.whole + p.eps);
+        const float rstd = 1.0f / sqrtf(s + p.eps);
         uint32_t am = 0;
         for (int64_t j = tid; j < p.d; j += 1024) {
             const float n = h_at(j) * rstd * to_f32(gamma[j]);
@@ -607,7 +608,7 @@ extern "C" resbm_status resbm_add_rmsnorm_fwd(const resbm_add_norm_desc *desc, c
     Ctx c;
     resbm_status st = make_ctx(stream, &c);
     if (st != RESBM_OK || !t) return st;
-    NormArgs p{X, A, gamma, H, N, static_cast<uint8_t *>(Q), S, d.T, ldx, lda, ldh, ldn, groups, (int)d.d, 0, d.eps};
+    NormArgs p{X, A, gamma, H, N, static_cast<uint8_t *>(Q), S, d.T, ldx, lda, ldh, ldn, groups, (int)d.d, 0, d.eps, (float)(1.0 / (double)d.d)};
     int log;
     const double m = frexp(1.0 / (double)d.d, &log);   // 1 / d = m 2^log with m from 0.5 to under 1
     p.part = (float)ldexp(1.0, log - 1);

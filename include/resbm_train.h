@@ -138,10 +138,11 @@ RESBM_API resbm_status resbm_adamw_step(const void *plan, const resbm_adamw_hype
 
 /* out[0] = the norm of all gradients of `count` plans together, sqrt(sum g^2); out[1] = the clipping coefficient
  * min(1, max_norm / (out[0] + 1e-6)), or 1 for max_norm = 0 (no clipping), or NaN where the norm is not finite
- * (resbm_adamw_step then changes nothing). Squares are fp32, so a norm over about 1e19 counts as infinite; sums
- * over a round of a thread's loads and beyond are in 64 bits, in an order that the sizes and the addresses' alignment
- * fix. out: 2 fp32, device, 4-byte aligned. `ws`: device memory of resbm_grad_norm_workspace_bytes bytes (which depend on
- * the plans' numbers of tensors only), 256-byte aligned. max_norm: finite, >= 0. count = 0: a norm of zero. */
+ * (resbm_adamw_step then changes nothing). Squares are fp32, so that a norm over about 1e19 counts as infinite, and gradients
+ * under 1e-19 count with fewer bits, under 2e-23 as zero; sums over a round of a thread's loads and beyond are in 64 bits,
+ * in an order that the sizes and the addresses' alignment fix. out: 2 fp32, device, 4-byte aligned, apart from `ws` and from the
+ * gradients. `ws`: device memory of resbm_grad_norm_workspace_bytes bytes (which depend on the plans' numbers of tensors
+ * only), 256-byte aligned, apart from the gradients. max_norm: finite, >= 0. count = 0: a norm of zero. */
 RESBM_API resbm_status resbm_grad_norm_workspace_bytes(const void *const *plans, int64_t count, size_t *bytes);
 RESBM_API resbm_status resbm_grad_norm(const void *const *plans, int64_t count, float max_norm, float *out, void *ws,
                                        size_t ws_bytes, void *stream);

@@ -17,7 +17,9 @@ _COLUMNS = _STATES + ("exp_avg_scale", "exp_avg_sq_scale", "master")   # (in Ada
 class AdamW(torch.optim.Optimizer):
     """AdamW with decoupled weight decay on fp32 or bf16 CUDA parameters.
 
-    state_bits      32 or 8 (e4m3 codes of the first moment and of the second's root, with fp32 scales)
+    state_bits      32 or 8 (e4m3 codes of the first moment and of the second's root, with fp32 scales). With 8 bits a second
+                    moment follows gradients that change against their block of 256 at a beta2 of about 0.95, not at 0.99 and
+                    over, where every step's change is under half a step of e4m3 and lost
     master          fp32 master copies of bf16 parameters, which then are what the step updates
     max_grad_norm   clips the norm of all gradients together; it is left in `grad_norm` (norm and coefficient, on the
                     device). A step whose norm is not finite changes no parameter and no moment (it still counts).

@@ -138,3 +138,29 @@ def test_small_and_large_second_moments_in_8_bits():
     root = s["v"][0].float() * s["v_scale"][0].repeat_interleave(B)
     assert torch.isnan(root).view(3, B).all(dim=1).tolist() == [False, True, False]
     assert torch.isnan(s["w"][0]).nonzero().flatten().tolist() == [B + 5]
+
+
+def test_8_bit_second_moments_change_by_half_a_step_or_not_at_all():
+    """What the header says of them, on constant gradients of one at beta2 = 0.999: an element whose gradients fall to a fifth keeps
+    its code (0.05 % a step), while fp32 states follow; one of twenty times the others' (18 % in one step) shows at once."""
+    h = dict(HYPER, beta1=0.0, beta2=0.999)
+    left = {}
+    for bits in (32, 8):
+        s = model([B], "f32", "f32", bits, warm=False)
+        plan = plan_of(s)
+        s["g"][0].fill_(1.0)
+        resbm.resbm_adamw_step(plan, step=1, **dict(h, beta2=0.0))      # v = 1
+        s["g"][0][5] = 0.2
+        for t in range(2, 502):
+            resbm.resbm_adamw_step(plan, step=t, **h)
+        root = s["v"][0].sqrt() if bits == 32 else s["v"][0].float() * s["v_scale"][0]
+        left[bits] = float(root[5])
+        assert abs(float(root[6]) - 1) <= 1e-3
+        s["g"][0][5] = 1.0
+        s["g"][0][7] = 20.0
+        resbm.resbm_adamw_step(plan, step=502, **h)
+        root = s["v"][0].sqrt() if bits == 32 else s["v"][0].float() * s["v_scale"][0]
+        assert abs(float(root[7]) - 1.399 ** 0.5) <= 2e-3
+    # 500 steps of 0.999 v + 0.001 / 25 from 1
+    v = 0.04 + 0.96 * 0.999 ** 500
+    assert abs(left[32] - v ** 0.5) <= 1e-4 and abs(left[8] - 1) <= 1e-3

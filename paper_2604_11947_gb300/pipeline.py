@@ -218,21 +218,35 @@ class _DecodeNorm(torch.autograd.Function):
         return dB, dWd1.to(Wd1.dtype), dWd2.to(Wd2.dtype), dgamma, None
 
 
+def _rows(t):
+    """t as the rows of its last dimension, with unit stride along them"""
+    t = t.reshape(-1, t.shape[-1])
+    return t if t.stride(1) == 1 else t.contiguous()
+
+
 class _AddNorm(torch.autograd.Function):
     """(h, n) = (x + a, RMSNorm(h) * gamma): resbm_add_rmsnorm_fwd forward; backward resbm_rmsnorm_bwd, whose result is the
-    gradient of x and of a alike. a None: (x, n)."""
+    gradient of x and of a alike. a None: (x, n). (Rows are made in here: between x's and a's own nodes and this one the two
+    gradients are one tensor, which autograd then copies where it keeps both; views of it would share their memory.)"""
 
     @staticmethod
     def forward(ctx, x, a, gamma):
-        if x.shape[1] > 16384:
+        if x.shape[-1] > 16384:
             raise ValueError("the norm's backward takes rows of at most 16384")
-        h = x if a is None else torch.empty_like(x, memory_format=torch.contiguous_format)
-        n = torch.empty_like(h, memory_format=torch.contiguous_format)
-        resbm.resbm_add_rmsnorm_fwd(x, a, gamma, NORM_EPS, None if a is None else h, n)
+        new = lambda: torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        h, n = x if a is None else new(), new()
+        resbm.resbm_add_rmsnorm_fwd(_rows(x), None if a is None else _rows(a), gamma, NORM_EPS, None if a is None else _rows(h), _rows(n))
         ctx.save_for_backward(h, gamma)
         ctx.set_materialize_grads(False)
-        ctx.added = a is not None
+        ctx.added, ctx.a_shape = a is not None, None if a is None else a.shape
         return (h, n) if ctx.added else n
+
+    @staticmethod
+    def _both(ctx, d):
+        """The gradients of x and a, gamma's missing"""
+        if not ctx.added:
+            return d, None
+        return d, d if d is None or d.shape == ctx.a_shape else d.reshape(ctx.a_shape).clone()
 
     @staticmethod
     @once_differentiable
@@ -240,28 +254,22 @@ class _AddNorm(torch.autograd.Function):
         h, gamma = ctx.saved_tensors
         dh, dn = grads if ctx.added else (None, grads[0])
         if dn is None:
-            return dh, dh if ctx.added else None, None
-        h, (T, d) = h.contiguous(), h.shape
-        desc = resbm.make_desc(T, d, 1, 1, "bf16" if h.dtype == torch.bfloat16 else "f32")
-        dx = torch.empty_like(h)
-        dgamma = torch.empty(d, dtype=torch.float32, device=h.device)
-        resbm.resbm_rmsnorm_bwd(desc, h, gamma, NORM_EPS, dn.contiguous(), None if dh is None else dh.contiguous(), dx, dgamma,
+            return *_AddNorm._both(ctx, dh), None
+        rows = h.contiguous().reshape(-1, h.shape[-1])
+        desc = resbm.make_desc(*rows.shape, 1, 1, "bf16" if h.dtype == torch.bfloat16 else "f32")
+        dx = torch.empty(h.shape, dtype=h.dtype, device=h.device)
+        dgamma = torch.empty(h.shape[-1], dtype=torch.float32, device=h.device)
+        resbm.resbm_rmsnorm_bwd(desc, rows, gamma, NORM_EPS, dn.contiguous(), None if dh is None else dh.contiguous(), dx, dgamma,
                                 resbm.workspace(desc, resbm.RESBM_OP_RMSNORM_BWD, h.device))
-        return dx, dx if ctx.added else None, dgamma.to(gamma.dtype)
+        return *_AddNorm._both(ctx, dx), dgamma.to(gamma.dtype)
 
 
 def add_norm(x, a, gamma):
-    """(x + a, RMSNorm(x + a) * gamma) over the last dimension, in one pass each way; a None: (x, RMSNorm(x) * gamma)."""
-    shape = x.shape
-
-    def flat(t):
-        t = t.reshape(-1, shape[-1])
-        return t if t.stride(1) == 1 else t.contiguous()
-
+    """(x + a, RMSNorm(x + a) * gamma) over the last dimension, in one pass each way; a None: (x, RMSNorm(x) * gamma).
+    x and a have the same rows, in x's shape or in any other."""
     if a is None:
-        return x, _AddNorm.apply(flat(x), None, gamma).view(shape)
-    h, n = _AddNorm.apply(flat(x), flat(a), gamma)
-    return h.view(shape), n.view(shape)
+        return x, _AddNorm.apply(x, None, gamma)
+    return _AddNorm.apply(x, a, gamma)
 
 
 class Boundary(torch.nn.Module):

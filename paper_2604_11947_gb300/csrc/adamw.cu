@@ -4,7 +4,7 @@
 // with 8-bit states 10, the norm 2. The list of tensors travels as the launch's parameter (up to 448 tensors, 31 KB), so
 // that nothing is copied to the device and a captured launch carries its own list; a list of up to 32 takes the small
 // parameter (2.2 KB; one call on the host 5.1 us, 5.5 with the large one). 308 M bf16 parameters on a GB300: 32-bit states
-// 963 us (7.0 TB/s; a copy moves 6.8), 8-bit states 446 (7.0 TB/s), norm 92 (6.7 TB/s).
+// 963 us (7.0 TB/s; a copy moves 6.8), 8-bit states 459 (6.8 TB/s), norm 92 (6.7 TB/s).
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -22,12 +22,12 @@
 namespace resbm {
 namespace {
 
-// CTAs of 128 threads, eight on an SM: with 256 threads the 8-bit step took 463 us instead of 448, the norm 98 instead of 96.
+// CTAs of 128 threads, eight on an SM: with 256 threads the 8-bit step takes 471 us instead of 460, the norm 94 instead of 92.
 constexpr int kThreads = 128, kWarps = kThreads / 32;
 constexpr int kBlock = RESBM_STATE_BLOCK;             // elements a warp takes at a time: one block of 8-bit states
-// Blocks that a warp has in flight where its accesses are vectors, by the states' bits. 8: 308 M elements 518 us with one
-// and 448 with two (at 64 registers, some of them spilled: at 72 without spills 494, with one CTA fewer on an SM; three
-// and four 484 and more). 32: 1060 us either way with the norm, and small lists spread over more CTAs with one.
+// Blocks that a warp has in flight where its accesses are vectors, by the states' bits. 8: 308 M elements 564 us with one
+// and 461 with two (at 64 registers, some of them spilled: 510 at 72 without spills, with one CTA fewer on an SM; three
+// 566). 32: 1058 us either way with the norm, and small lists spread over more CTAs with one.
 __host__ __device__ constexpr int deep_of(int bits) { return bits == 8 ? 2 : 1; }
 constexpr int kSmall = 32, kLarge = 448;              // tensors a launch, by the parameter's size
 constexpr int kNormGrid = 1216;                       // most CTAs of the gradients' norm: eight on each of 152 SMs
@@ -205,9 +205,8 @@ __device__ __forceinline__ Pair alone(Pair a, Pair b, const Step &h) { return fm
 // the root with 32-bit states. A v below 2^-126 (gradients below 1e-17) counts as that for the weight (`least` is its
 // denominator).
 // The 8-bit form is bound by instructions as much as by memory (10 bytes an element): with IEEE roots and quotients, one
-// value an instruction and one block a warp 75 of them an element, 868 us for 308 M elements; with pairs 52 and 597; with
-// two blocks a warp, accesses of eight elements and approximate roots and reciprocals 34 and 448; with the stored roots to
-// nearest 459.
+// value an instruction and one block a warp 75 of them an element, 868 us for 308 M elements; with pairs, two blocks a warp,
+// accesses of eight elements, approximate quotients and one reciprocal an element, and roots() 40 and 459.
 template <typename W, typename G, bool MASTER, int BITS, Mode MODE, int K>
 __device__ __forceinline__ void adamw_blocks(W *w, const G *g, void *mp, void *vp, float *ms, float *vs, float *master,
                                              int lane, int rem, const Step &h, float c)

@@ -2,8 +2,8 @@
 
 Tolerances, from the arithmetic. H is one fp32 addition rounded once: exactly torch's. The norm is taken of H as stored,
 so N, Q and S are compared with n = h s gamma of that H in 64 bits. The sum of squares has positive terms only, added in
-fp32 by a thread (at most 32 of them in the register kernels, d / 1024 in the long one), then over 5 shuffles and at most
-32 warps: its relative error is at most (terms + 37) 2^-24, half of that in the root; mean, eps, root, reciprocal and
+fp32 by a thread (at most 64 of them in the register kernels, no more than 13 one after the other, for which 32 stands;
+d / 1024 in the long one), then over 5 shuffles and at most 32 warps: its relative error is at most (terms + 37) 2^-24, half of that in the root; mean, eps, root, reciprocal and
 the two products add six roundings. N's own rounding is half a step (2^-8 of the value for bf16, 2^-24 for fp32). A code is
 off by half a step of e4m3: 2^-4 of the value, or 2^-10 of the scale below 2^-6 of it."""
 import pytest
@@ -82,8 +82,8 @@ def run(X, A, gamma, o, T, d, group, eps=EPS):
                                 group if "Q" in o else 0)
 
 
-# every register form (vectors of 16 bytes and single elements, 1 to 4 a thread, a warp to 1024 threads a row) on both
-# sides of its border, and the long one
+# every register form (a warp a row with 1 to 4 vectors of 16 bytes a lane, up to 512 threads a row with 3, 4 or 8 each) on
+# both sides of its border, and the long one; realigned rows of 8 vectors a thread are test_add_norm_widest_gpu's
 WIDTHS = [1, 2, 7, 8, 31, 32, 33, 64, 127, 128, 129, 250, 256, 264, 500, 512, 520, 1000, 1001, 1024, 1032, 2048, 2049, 2056, 4095, 4096,
           4104, 5001, 8192, 8200, 12288, 16384, 16392, 32768, 32776, 40001]
 

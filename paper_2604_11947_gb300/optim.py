@@ -116,11 +116,19 @@ class AdamW(torch.optim.Optimizer):
                     self._init_master(p)   # (a parameter that was fp32 before)
                 work.setdefault((i, p.dtype, p.grad.dtype, self.state[p]["step"] + 1), []).append(p)
         plans, kept = [], {}
-        for (i, dtype, g_dtype, step), params in work.items():
-            key = (i, dtype, g_dtype, *map(id, params))
-            plans.append((self.param_groups[i], step, params, self._plan(key, params)))
-            kept[key] = self._plans[key]
-        self._plans = kept   # (those of other lists than this step's are let go)
+        try:
+            for (i, dtype, g_dtype, step), params in work.items():
+                key = (i, dtype, g_dtype, *map(id, params))
+                plans.append((self.param_groups[i], step, params, self._plan(key, params)))
+                kept[key] = self._plans[key]
+            self._plans = kept   # (those of other lists than this step's are let go)
+            self._launch(plans)
+        finally:   # (zero_grad frees the gradients, a program may drop or move the states; what was launched is on the stream)
+            for *_, plan in plans:
+                plan.release()
+        return loss
+
+    def _launch(self, plans):
         scale = None
         if self.max_grad_norm is not None and plans:
             each = [plan for *_, plan in plans]
@@ -135,8 +143,6 @@ class AdamW(torch.optim.Optimizer):
             b1, b2 = group["betas"]
             resbm.resbm_adamw_step(plan, lr=float(group["lr"]), beta1=b1, beta2=b2, eps=group["eps"], weight_decay=group["weight_decay"],
                                    step=step, grad_scale=scale)
-            plan.release()   # (zero_grad frees the gradients, a program may drop or move the states; the launches are on the stream)
             torch.autograd.graph.increment_version(params)   # (a backward through what they were raises, as after torch's steps)
             for p in params:
                 self.state[p]["step"] = step
-        return loss

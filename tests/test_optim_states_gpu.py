@@ -234,3 +234,38 @@ def test_parameters_that_become_bf16_get_master_copies(bits):
     again = optim.AdamW(params, state_bits=bits, master=True, **H)
     again.load_state_dict(copy.deepcopy(opt.state_dict()))
     stepped(again, params, 4)
+
+
+def test_a_refused_step_holds_nothing():
+    """Where a list of the step is refused, nothing is changed and the other lists' gradients are let go too."""
+    a, b = params_of([300], torch.float32), params_of([64], torch.bfloat16, seed=1)
+    opt = optim.AdamW(a + b, **H)
+    for t in (1, 2):
+        grads_in_place(a + b, t)
+        opt.step()
+    before = [p.detach().clone() for p in a + b]
+    b[0].grad = b[0].detach()[:]
+    with pytest.raises(RuntimeError):
+        opt.step()
+    assert all(torch.equal(p, q) for p, q in zip(a + b, before)) and opt.state[a[0]]["step"] == 2
+    held = weakref.ref(a[0].grad)
+    opt.zero_grad(set_to_none=True)
+    assert held() is None
+
+
+@pytest.mark.parametrize("bits,master", [(32, False), (8, True)])
+def test_empty_parameters_and_scalars(bits, master):
+    params = [torch.nn.Parameter(torch.full(shape, 0.5, device="cuda", dtype=torch.bfloat16)) for shape in ((0,), (), (3, 0), (2, 5))]
+    opt = optim.AdamW(params, state_bits=bits, master=master, max_grad_norm=1.0, **H)
+    for t in (1, 2):
+        grads_in_place(params, t)
+        before = columns(opt, params) if t > 1 else None
+        opt.step()
+        if before:
+            for i in (1, 3):
+                one = lambda s: {k: None if x is None else [x[i]] for k, x in s.items()}
+                check_step(one(before), one(columns(opt, params)), t, HYPER, float(opt.grad_norm[1]))
+    only = optim.AdamW(params[:1], state_bits=bits, master=master, max_grad_norm=1.0, **H)
+    params[0].grad = torch.zeros_like(params[0])
+    only.step()
+    assert only.grad_norm.tolist() == [0.0, 1.0]

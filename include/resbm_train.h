@@ -138,8 +138,8 @@ RESBM_API resbm_status resbm_adamw_plan(const resbm_adamw_desc *desc, const resb
  * 8-bit state are rounded after every operation (from v = 2^-102 on; below it sqrt(v) is within a bit). The root and the
  * quotient of w are within 2^-21 of theirs (relative to the update); a v below 2^-126 (gradients under 1e-17) counts as
  * 2^-126 there. A v beyond fp32 (gradients over 1e19) is an infinity with 32-bit states, where the weight then only decays;
- * with 8-bit ones the weight and its block's sqrt(v) become NaN. One launch for up to 448 tensors of a kind (aligned or not). Errors: RESBM_ERR_INVALID_ARG for a bad hyperparameter or for a plan that is none or has
- * RESBM_STATE_NONE. */
+ * with 8-bit ones the weight and its block's sqrt(v) become NaN. One launch for up to 448 tensors of a kind (aligned or not).
+ * Errors: RESBM_ERR_INVALID_ARG for a bad hyperparameter or for a plan that is none or has RESBM_STATE_NONE. */
 RESBM_API resbm_status resbm_adamw_step(const void *plan, const resbm_adamw_hyper *hyper, void *stream);
 
 /* out[0] = the norm of all gradients of `count` plans together, sqrt(sum g^2); out[1] = the clipping coefficient

@@ -1,0 +1,450 @@
+// embed.cu -- resbm_embed_fwd and resbm_embed_bwd (include/resbm_vocab.h): rows of a table times a scale, and the table's
+// gradient from tokens sorted by id.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "abi.h"
+#include "common.cuh"
+#include "resbm_vocab.h"
+#include "tc_host.cuh"
+#include "vocab.h"
+
+namespace resbm {
+namespace {
+
+// VEC columns of a row (16 bytes, or one element off the 16-byte grid) as fp32
+template <typename E, int VEC> struct Cols {
+    float x[VEC];
+    __device__ __forceinline__ void load(const E *p)
+    {
+        if constexpr (VEC == 1) {
+            x[0] = to_f32(__ldg(p));
+        } else {
+            const uint4 u = __ldg(reinterpret_cast<const uint4 *>(p));
+            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (sizeof(E) == 2) {
+                    x[2 * i] = __uint_as_float(w[i] << 16);
+                    x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+                } else {
+                    x[i] = __uint_as_float(w[i]);
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void store(E *p, float scale) const
+    {
+        if constexpr (VEC == 1) {
+            *p = from_f32<E>(x[0] * scale);
+        } else {
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (sizeof(E) == 2) {
+                    const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i] * scale, x[2 * i + 1] * scale);
+                    w[i] = *reinterpret_cast<const uint32_t *>(&h);
+                } else {
+                    w[i] = __float_as_uint(x[i] * scale);
+                }
+            }
+            *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+    __device__ __forceinline__ void fill(float v)
+    {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) x[i] = v;
+    }
+    __device__ __forceinline__ void add(const Cols &o)
+    {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) x[i] += o.x[i];
+    }
+};
+
+// ---- forward -----------------------------------------------------------------------------------------
+// 2^log_tx threads along a row, 256 >> log_tx rows a CTA at a time, four rows in flight a thread
+template <typename E, int VEC>
+__global__ void __launch_bounds__(256) k_embed_fwd(const int64_t *__restrict__ ids, const E *__restrict__ table, int64_t ldt, E *__restrict__ out,
+                                                   int64_t ldo, int64_t T, int64_t V, int64_t d, float scale, int log_tx)
+{
+    griddep_wait();
+    griddep_launch_dependents();
+    const int64_t col = (((int64_t)blockIdx.y << log_tx) + (threadIdx.x & ((1 << log_tx) - 1))) * VEC;
+    if (col >= d) return;
+    const int rows = 256 >> log_tx;
+    const int64_t step = (int64_t)gridDim.x * rows;
+    for (int64_t t = (int64_t)blockIdx.x * rows + (threadIdx.x >> log_tx); t < T; t += 4 * step) {
+        int64_t id[4];
+        Cols<E, VEC> v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) id[i] = t + i * step < T ? ids[t + i * step] : -1;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (id[i] >= 0 && id[i] < V) v[i].load(table + id[i] * ldt + col);
+            else v[i].fill(NAN);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (t + i * step < T) v[i].store(out + (t + i * step) * ldo + col, scale);
+    }
+}
+
+// ---- tokens sorted by id -------------------------------------------------------------------------------
+constexpr int kSortCtas = 8, kSortThreads = 1024, kMaxBins = 512;
+
+// Stable: one cluster of eight CTAs, a radix sort of the ids from their lowest digit on. Each warp has a contiguous run of the
+// positions; its equal digits are found 32 at a time by a match, so that ranks need no atomics and keep the order. Ids that
+// count for nothing become V and sort behind the others. Then a bit for every word that has tokens. T = 16384 tokens of 32000
+// words are two passes of 8 bits. (A sort over the whole GPU would be several launches; this one's time is their latency.)
+__global__ void __cluster_dims__(kSortCtas) __launch_bounds__(kSortThreads, 1)
+    k_sort(const int64_t *__restrict__ ids, int T, int V, int64_t padding, int passes, int bits, int32_t *keys, int32_t *vals, uint32_t *present)
+{
+    extern __shared__ int32_t cnt[];   // 32 warps x bins: counts, then places
+    __shared__ int32_t total[kMaxBins], wsum[32];
+    griddep_wait();
+    griddep_launch_dependents();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tid = threadIdx.x;
+    const int rank = (int)cluster_rank(), bins = 1 << bits;
+    const int per_warp = ((T + kSortCtas * 32 - 1) / (kSortCtas * 32) + 31) / 32 * 32;
+    const int64_t first = ((int64_t)rank * 32 + warp) * per_warp;
+    const int p0 = (int)(first < T ? first : T), p1 = (int)(first + per_warp < T ? first + per_warp : T);
+    for (int i = rank * kSortThreads + tid; i < (V + 31) / 32; i += kSortCtas * kSortThreads) present[i] = 0u;
+    int32_t *mine = cnt + warp * bins;
+    for (int pass = 0; pass < passes; ++pass) {
+        const int32_t *kin = keys + (int64_t)((pass & 1) ^ 1) * T, *vin = vals + (int64_t)((pass & 1) ^ 1) * T;
+        int32_t *kout = keys + (int64_t)(pass & 1) * T, *vout = vals + (int64_t)(pass & 1) * T;
+        const int shift = pass * bits;
+        auto key_at = [&](int p) -> int32_t {
+            if (pass) return __ldcg(kin + p);
+            const int64_t id = ids[p];
+            return id < 0 || id >= V || id == padding ? V : (int32_t)id;
+        };
+        for (int b = lane; b < bins; b += 32) mine[b] = 0;
+        __syncwarp();
+        for (int p = p0; p < p1; p += 32) {
+            const bool in = p + lane < p1;
+            const int digit = in ? (key_at(p + lane) >> shift) & (bins - 1) : bins;
+            const uint32_t same = __match_any_sync(0xffffffffu, digit);
+            if (in && (same & ((1u << lane) - 1)) == 0) mine[digit] += __popc(same);
+            __syncwarp();
+        }
+        __syncthreads();
+        // counts -> places within the CTA's tokens of a digit; total[b]: the CTA's
+        if (tid < bins) {
+            int sum = 0;
+            for (int w = 0; w < 32; ++w) {
+                const int v = cnt[w * bins + tid];
+                cnt[w * bins + tid] = sum;
+                sum += v;
+            }
+            total[tid] = sum;
+        }
+        cluster_sync();
+        int all = 0, before = 0;   // digit tid: over all CTAs, over those before this one
+        if (tid < bins) {
+            for (int c = 0; c < kSortCtas; ++c) {
+                int v;
+                asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(map_shared(smem_addr(&total[tid]), (uint32_t)c)));
+                all += v;
+                if (c < rank) before += v;
+            }
+        }
+        int upto = all;   // inclusive sum over the digits
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += v;
+        }
+        if (lane == 31) wsum[warp] = upto;
+        __syncthreads();
+        for (int w = 0; w < warp; ++w) upto += wsum[w];
+        if (tid < bins)
+            for (int w = 0; w < 32; ++w) cnt[w * bins + tid] += upto - all + before;
+        __syncthreads();
+        for (int p = p0; p < p1; p += 32) {
+            const bool in = p + lane < p1;
+            const int32_t key = in ? key_at(p + lane) : 0;
+            const int digit = in ? (key >> shift) & (bins - 1) : bins;
+            const uint32_t same = __match_any_sync(0xffffffffu, digit), below = same & ((1u << lane) - 1);
+            const int at = in ? mine[digit] + __popc(below) : 0;
+            __syncwarp();
+            if (in) {
+                if (below == 0) mine[digit] += __popc(same);
+                __stcg(kout + at, key);
+                __stcg(vout + at, pass ? __ldcg(vin + p + lane) : p + lane);
+            }
+            __syncwarp();
+        }
+        __threadfence();
+        cluster_sync();   // (and no CTA reads another's totals any more)
+    }
+    const int32_t *sorted = keys + (int64_t)((passes - 1) & 1) * T;
+    for (int p = rank * kSortThreads + tid; p < T; p += kSortCtas * kSortThreads) {
+        const int32_t k = __ldcg(sorted + p);
+        if (k < V && (p == 0 || __ldcg(sorted + p - 1) != k)) atomicOr(&present[k >> 5], 1u << (k & 31));
+    }
+}
+
+// ---- sums ------------------------------------------------------------------------------------------------
+constexpr int kRun = 32;   // sorted positions a block
+
+struct SumArgs {
+    const int32_t *keys, *vals;   // sorted
+    const uint32_t *present;
+    const void *dout;
+    void *dtable;
+    float *part;                  // (block, head or tail, column)
+    int64_t ldo, d;
+    int T, V, sum_ctas, log_tx;
+    float scale;
+};
+
+// CTAs below sum_ctas: blocks of kRun sorted positions, 2^log_tx threads along a row, which add the rows of each word up in
+// order. A word whose tokens all lie in the block is finished; the block's first and last runs may be pieces of longer ones,
+// and leave a partial sum (k_embed_join). So the work is even whatever the ids are. The other CTAs write the zero rows.
+template <typename E, int VEC> __global__ void __launch_bounds__(256) k_embed_sum(const SumArgs a)
+{
+    griddep_wait();
+    griddep_launch_dependents();
+    if ((int)blockIdx.x >= a.sum_ctas) {
+        if (blockIdx.y) return;
+        const int lane = threadIdx.x & 31;
+        const int step = (gridDim.x - a.sum_ctas) * 8;
+        Cols<E, VEC> zero;
+        zero.fill(0.0f);
+        for (int64_t v = (blockIdx.x - a.sum_ctas) * 8 + (threadIdx.x >> 5); v < a.V; v += step) {
+            if (a.present[v >> 5] >> (v & 31) & 1) continue;
+            E *row = static_cast<E *>(a.dtable) + v * a.d;
+            for (int64_t c = lane * VEC; c < a.d; c += 32 * VEC) zero.store(row + c, 0.0f);
+        }
+        return;
+    }
+    const int per_cta = 256 >> a.log_tx;
+    const int b = blockIdx.x * per_cta + (threadIdx.x >> a.log_tx);
+    const int64_t col = (((int64_t)blockIdx.y << a.log_tx) + (threadIdx.x & ((1 << a.log_tx) - 1))) * VEC;
+    const int64_t p0 = (int64_t)b * kRun;
+    if (col >= a.d || p0 >= a.T) return;
+    const int len = a.T - p0 < kRun ? (int)(a.T - p0) : kRun;
+    const int32_t *key = a.keys + p0, *val = a.vals + p0;
+    const bool head = b > 0 && key[-1] == key[0];                        // the first run began before
+    const bool tail = p0 + len < a.T && key[len] == key[len - 1];        // the last one goes on
+    const E *dout = static_cast<const E *>(a.dout) + col;
+    float *part = a.part + (int64_t)b * 2 * a.d + col;
+    Cols<E, VEC> sum;
+    sum.fill(0.0f);
+    bool first_run = true;
+    int32_t k = key[0];
+    for (int i = 0; i < len && k < a.V; i += 8) {
+        Cols<E, VEC> v[8];
+        int32_t ks[9];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            ks[j] = i + j < len ? key[i + j] : a.V;
+            if (ks[j] < a.V) v[j].load(dout + (int64_t)val[i + j] * a.ldo);
+        }
+        ks[8] = i + 8 < len ? key[i + 8] : INT32_MAX;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (ks[j] >= a.V) break;
+            sum.add(v[j]);
+            const bool end = i + j + 1 == len;
+            if (!end && ks[j + 1] == ks[j]) continue;
+            // a run ends here, or the block does
+            if ((first_run && head) || (end && tail)) {
+                float *dst = part + (first_run && head ? 0 : a.d);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) dst[e] = sum.x[e];
+            } else {
+                sum.store(static_cast<E *>(a.dtable) + (int64_t)ks[j] * a.d + col, a.scale);
+            }
+            sum.fill(0.0f);
+            first_run = false;
+        }
+        k = ks[8] == INT32_MAX ? a.V : ks[8];
+    }
+}
+
+// Words whose tokens span blocks: the partial sums in order, by the threads of the block where the word begins
+template <typename E, int VEC> __global__ void __launch_bounds__(256) k_embed_join(const SumArgs a)
+{
+    griddep_wait();
+    griddep_launch_dependents();
+    const int per_cta = 256 >> a.log_tx;
+    const int64_t b = (int64_t)blockIdx.x * per_cta + (threadIdx.x >> a.log_tx);
+    const int64_t col = (((int64_t)blockIdx.y << a.log_tx) + (threadIdx.x & ((1 << a.log_tx) - 1))) * VEC;
+    const int64_t blocks = ((int64_t)a.T + kRun - 1) / kRun, p0 = b * kRun;
+    if (col >= a.d || b + 1 >= blocks) return;
+    const int32_t k = a.keys[p0 + kRun - 1];
+    if (k >= a.V || a.keys[p0 + kRun] != k || (b > 0 && a.keys[p0 - 1] == k)) return;
+    // the last block with tokens of the word: keys ascend
+    int64_t lo = b + 1, hi = blocks - 1;
+    while (lo < hi) {
+        const int64_t mid = (lo + hi + 1) >> 1;
+        if (a.keys[mid * kRun] == k) lo = mid;
+        else hi = mid - 1;
+    }
+    Cols<E, VEC> sum;
+    const float *tail = a.part + (b * 2 + 1) * a.d + col;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) sum.x[e] = tail[e];
+    for (int64_t i = b + 1; i <= lo; i += 4) {
+        float x[4][VEC];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (i + j <= lo) {
+                const float *head = a.part + (i + j) * 2 * a.d + col;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) x[j][e] = head[e];
+            }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (i + j <= lo) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) sum.x[e] += x[j][e];
+            }
+    }
+    sum.store(static_cast<E *>(a.dtable) + (int64_t)k * a.d + col, a.scale);
+}
+
+// threads along a row: a power of two, up to 256
+int log_threads(int64_t vectors)
+{
+    int log = 0;
+    while (log < 8 && (int64_t(1) << log) < vectors) ++log;
+    return log;
+}
+
+struct EmbedWs {
+    int32_t *keys, *vals;
+    uint32_t *present;
+    float *part;
+    size_t bytes;
+};
+EmbedWs carve(void *ws, int64_t T, int64_t V, int64_t d)
+{
+    WsCarver w(ws);
+    EmbedWs e;
+    e.keys = w.take<int32_t>(2 * T);
+    e.vals = w.take<int32_t>(2 * T);
+    e.present = w.take<uint32_t>((V + 31) / 32);
+    e.part = w.take<float>((T + kRun - 1) / kRun * 2 * d);
+    e.bytes = w.used;
+    return e;
+}
+
+resbm_status check(const resbm_embed_desc *desc, const int64_t *ids, const void *table, const void *out, bool table_dense)
+{
+    if (!desc) return RESBM_ERR_INVALID_ARG;
+    const resbm_embed_desc &d = *desc;
+    if (d.T < 0 || d.V < 1 || d.d < 1 || (d.dtype != RESBM_F32 && d.dtype != RESBM_BF16) || d.flags || !isfinite(d.scale)) return RESBM_ERR_INVALID_ARG;
+    constexpr int64_t most = int64_t(1) << 29, limit = INT64_MAX / 64;
+    if (d.T >= most || d.V >= most || d.d > (int64_t(1) << 20)) return RESBM_ERR_UNSUPPORTED;
+    const int64_t es = d.dtype == RESBM_BF16 ? 2 : 4;
+    const bool t = d.T > 0;
+    auto bad = [&](int64_t rows, int64_t ld) { return rows > 1 && (ld < d.d || !mul_ok(rows, ld) || rows * ld > limit); };
+    if ((!table_dense && bad(d.V, d.ldt)) || bad(d.T, d.ldo)) return RESBM_ERR_INVALID_ARG;
+    if (!ptr_ok(ids, 8, t) || !ptr_ok(table, es, t || table_dense) || !ptr_ok(out, es, t)) return RESBM_ERR_INVALID_ARG;
+    return RESBM_OK;
+}
+
+Range rows_of(const void *p, int64_t n, int64_t ld, int64_t d, int64_t es) { return rng(p, n > 0 ? (n - 1) * (n > 1 ? ld : 0) + d : 0, es); }
+
+template <typename E> cudaError_t run_fwd(const resbm_embed_desc &d, const int64_t *ids, const void *table, void *out, const Ctx &c)
+{
+    constexpr int V16 = 16 / (int)sizeof(E);
+    const bool vec = d.d % V16 == 0 && al16(table) && al16(out) && (d.V == 1 || d.ldt % V16 == 0) && (d.T == 1 || d.ldo % V16 == 0);
+    const int64_t n = vec ? d.d / V16 : d.d;
+    const int log_tx = log_threads(n);
+    const int64_t rows = 256 >> log_tx, ctas = (d.T + rows - 1) / rows, cols = (n + (int64_t(1) << log_tx) - 1) >> log_tx;
+    const dim3 grid((unsigned)std::min<int64_t>(ctas, std::max<int64_t>(1, 16 * c.sm_count / cols)), (unsigned)cols);
+    auto go = [&](auto kernel) {
+        return launch(kernel, grid, dim3(256), 0, c.stream, ids, static_cast<const E *>(table), d.ldt, static_cast<E *>(out), d.ldo, d.T, d.V, d.d, d.scale, log_tx);
+    };
+    return vec ? go(k_embed_fwd<E, V16>) : go(k_embed_fwd<E, 1>);
+}
+
+template <typename E> cudaError_t run_bwd(const resbm_embed_desc &d, const int64_t *ids, const void *dout, void *dtable, const EmbedWs &w, const Ctx &c)
+{
+    // the digits of 0 .. V
+    int width = 1;
+    while (width < 31 && (int64_t(1) << width) <= d.V) ++width;
+    const int passes = (width + 8) / 9, bits = (width + passes - 1) / passes;
+    const uint32_t smem = 32u * 4u << bits;
+    static std::atomic<uint8_t> done[kMaxDev];
+    cudaError_t e = ensure_smem(k_sort, 32 * 4 * kMaxBins, c.device, done);
+    // (the cluster's size is the kernel's own)
+    if (e == cudaSuccess) e = launch(k_sort, dim3(kSortCtas), dim3(kSortThreads), smem, c.stream, ids, (int)d.T, (int)d.V, d.padding, passes, bits, w.keys, w.vals, w.present);
+    if (e != cudaSuccess) return e;
+    constexpr int V16 = 16 / (int)sizeof(E);
+    const bool vec = d.d % V16 == 0 && al16(dout) && al16(dtable) && (d.T == 1 || d.ldo % V16 == 0);
+    const int64_t n = vec ? d.d / V16 : d.d;
+    const int log_tx = log_threads(n);
+    const int64_t per = 256 >> log_tx, blocks = (d.T + kRun - 1) / kRun, cols = (n + (int64_t(1) << log_tx) - 1) >> log_tx;
+    SumArgs a{w.keys + ((passes - 1) & 1) * d.T, w.vals + ((passes - 1) & 1) * d.T, w.present, dout, dtable, w.part, d.ldo, d.d, (int)d.T, (int)d.V,
+              (int)((blocks + per - 1) / per), log_tx, d.scale};
+    const int64_t zero = std::min<int64_t>((d.V + 7) / 8, 4 * c.sm_count);
+    auto go = [&](auto sum, auto join) {
+        cudaError_t e = launch(sum, dim3((unsigned)(a.sum_ctas + zero), (unsigned)cols), dim3(256), 0, c.stream, a);
+        if (e == cudaSuccess && blocks > 1) e = launch(join, dim3((unsigned)a.sum_ctas, (unsigned)cols), dim3(256), 0, c.stream, a);
+        return e;
+    };
+    e = vec ? go(k_embed_sum<E, V16>, k_embed_join<E, V16>) : go(k_embed_sum<E, 1>, k_embed_join<E, 1>);
+    if (e == cudaSuccess) count_launches(blocks > 1 ? 3 : 2);
+    return e;
+}
+
+}  // namespace
+
+size_t embed_bwd_ws_bytes(int64_t T, int64_t V, int64_t d) { return carve(nullptr, T, V, d).bytes; }
+
+}  // namespace resbm
+
+using namespace resbm;
+
+extern "C" {
+
+resbm_status resbm_embed_fwd(const resbm_embed_desc *desc, const int64_t *ids, const void *table, void *out, void *stream)
+{
+    resbm_status st = check(desc, ids, table, out, false);
+    if (st != RESBM_OK) return st;
+    const resbm_embed_desc &d = *desc;
+    const int64_t es = d.dtype == RESBM_BF16 ? 2 : 4;
+    const Range o = rows_of(out, d.T, d.ldo, d.d, es);
+    if (overlaps(o, rows_of(table, d.V, d.ldt, d.d, es)) || overlaps(o, rng(ids, d.T, 8))) return RESBM_ERR_INVALID_ARG;
+    Ctx c;
+    st = make_ctx(stream, &c);
+    if (st != RESBM_OK || d.T == 0) return st;
+    const cudaError_t e = d.dtype == RESBM_F32 ? run_fwd<float>(d, ids, table, out, c) : run_fwd<__nv_bfloat16>(d, ids, table, out, c);
+    if (e == cudaSuccess) count_launches(1);
+    else cudaGetLastError();
+    return finish(e);
+}
+
+resbm_status resbm_embed_bwd(const resbm_embed_desc *desc, const int64_t *ids, const void *dout, void *dtable, void *ws, size_t ws_bytes, void *stream)
+{
+    resbm_status st = check(desc, ids, dtable, dout, true);
+    if (st != RESBM_OK) return st;
+    const resbm_embed_desc &d = *desc;
+    const int64_t es = d.dtype == RESBM_BF16 ? 2 : 4;
+    if (!ptr_ok(ws, 256, false)) return RESBM_ERR_INVALID_ARG;
+    const Range outs[] = {rng(dtable, d.V * d.d, es), rng(ws, (int64_t)std::min<size_t>(ws_bytes, INT64_MAX), 1)};
+    const Range ins[] = {rows_of(dout, d.T, d.ldo, d.d, es), rng(ids, d.T, 8)};
+    if (any_overlap(outs, ins, 2)) return RESBM_ERR_INVALID_ARG;
+    if (d.T > 0 && (!ws || ws_bytes < embed_bwd_ws_bytes(d.T, d.V, d.d))) return RESBM_ERR_WORKSPACE;
+    Ctx c;
+    st = make_ctx(stream, &c);
+    if (st != RESBM_OK) return st;
+    if (d.T == 0) return finish(cudaMemsetAsync(dtable, 0, (size_t)(d.V * d.d * es), c.stream));
+    const EmbedWs w = carve(ws, d.T, d.V, d.d);
+    const cudaError_t e = d.dtype == RESBM_F32 ? run_bwd<float>(d, ids, dout, dtable, w, c) : run_bwd<__nv_bfloat16>(d, ids, dout, dtable, w, c);
+    if (e != cudaSuccess) cudaGetLastError();
+    return finish(e);
+}
+
+}  // extern "C"

@@ -15,6 +15,7 @@
 #include "internal.h"
 #include "resbm.h"
 #include "tc.h"
+#include "vocab.h"
 
 using namespace resbm;
 
@@ -644,7 +645,10 @@ resbm_status resbm_device_error(unsigned int *code, int clear)
 {
     if (!code) return RESBM_ERR_INVALID_ARG;
     *code = 0;
+    unsigned int other = 0;   // (each translation unit of tensor-core kernels has its own word)
     cudaError_t e = tc_device_error(code, clear != 0);
+    if (e == cudaSuccess) e = vocab_device_error(&other, clear != 0);
+    *code |= other;
     return e == cudaSuccess ? RESBM_OK : cuda_fail(e);
 }
 

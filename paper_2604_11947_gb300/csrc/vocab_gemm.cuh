@@ -1,0 +1,544 @@
+// vocab_gemm.cuh -- the four products of the vocabulary's losses (include/resbm_vocab.h) on tcgen05, each with the step
+// that follows it applied to the accumulator before it leaves the chip.
+//
+//   VG_FWD   z = X . W^T             a row's running maximum and sum of exponentials over the unit's columns, and its
+//                                    targets' logits: 16 bytes a row and unit instead of the logits
+//   VG_DZ    z again, then           dz = g (softmax(z / tau) - q), stored for a piece of the vocabulary at a time
+//   VG_DX    dz . W                  fp32, added to what earlier pieces gave
+//   VG_DW    dz^T . X                complete for the piece's rows of W
+//
+// X: the n tokens that have a target, packed (n is on the device only); z and dz have a row for each of them.
+//
+// Work units are (256 rows, up to 256 columns, depth split), unit u on CTA pair u mod pairs, row blocks in groups of
+// `group` with the columns outside, so that the pairs at work share operands in L2. A pair (cta_group::2) has per CTA
+//   producer warp  : TMA loads of 64-deep slices of its 128 rows of A and its half of B, 128-byte swizzle, six stages
+//   MMA warp       : (even CTA) four 256 x bn x 16 products a slice into one of two TMEM accumulators
+//   epilogue warps : eight, two a TMEM lane quarter with half of the columns each, one row a thread
+// and the next unit's products overlap this unit's epilogue.
+//
+// fp32 (SPLIT 3): every operand is the sum of three bf16 values (the value rounded, its remainder rounded, and once more:
+// 24 bits), and a product the six of nine partial ones that are over 2^-24 of it, smallest first. They are one product of
+// six times the depth, at the bf16 rate: 375 TFLOP/s at most, where CUDA cores have 75.
+//
+// PIECES: the tensor core truncates as it adds to its accumulator, an error that grows with the number of MMAs in one
+// accumulator (2e-6 of a logit at d = 2048). Where that is seen in an output (the losses, and everything in fp32) a unit's sum
+// runs in pieces, which alternate between the accumulators; the epilogue warps add them in registers, rounded to
+// nearest, while the next piece runs.
+//
+// Every element is summed by one CTA in a fixed order, and a depth split has a slot of its own: results are the same bits
+// every time.
+#pragma once
+
+#include <limits.h>
+#include <math.h>
+
+#include "common.cuh"
+#include "pair.cuh"
+#include "tc_common.cuh"
+#include "tc_pair.cuh"
+
+namespace resbm {
+namespace tc {
+
+enum VocabMode : int { VG_FWD, VG_DZ, VG_DX, VG_DW };
+
+struct VocabGemm {
+    const int32_t *n_ptr;     // tokens in use: *n_ptr, or n_rows where it is null
+    int32_t n_rows;
+    int32_t rows;             // VG_DW: rows of the piece (words)
+    int32_t cols;             // columns that exist
+    int32_t depth;            // FWD, DZ, DX
+    int32_t bn, nn;           // columns a unit (a multiple of 32), units along the columns
+    int32_t splits, group;
+    int32_t a_off, b_off;     // rows from one of SPLIT's three operands to the next
+    int32_t b_y;              // FWD, DZ, DX: the piece's first row in B's tensor map
+    int32_t out_y;            // DW: the piece's first row of dW
+    int32_t slot_rows;        // DX, DW: rows of a slot
+    int32_t add;              // DX: added to the slots
+    // the rows' tokens, targets and scalars (FWD, DZ)
+    int32_t v0;               // the piece's first word
+    const int32_t *token;     // row -> token, or null: the same
+    const int64_t *label;     // a token's target, or null: the lists
+    const int32_t *list;      // K targets a token in ascending order, INT32_MAX behind the last
+    const float *weight;      // their weights
+    int32_t K;
+    int32_t slot0;            // FWD: the first slot of this launch (two a unit)
+    int64_t tp;               // rows of a slot, rounded up
+    float c;                  // log2(e) / tau
+    float2 *stat;             // FWD: (maximum c, sum of 2^(z c - maximum c)) of slot, row
+    float *zt;                // FWD: the label's logit a row; with lists: the weighted sum of slot, row
+    const float *lse, *dloss; // DZ: a token's log-sum-exp, its loss's gradient
+    int32_t dloss_step;       // 1, or 0: one for all
+    float tau;
+    const float *bad;         // DZ: a value added to a token's gradient (NaN where its targets are none), or null
+    int32_t V;
+    // DW where TMA cannot store: the matrix, its pitch in elements
+    void *out;
+    int64_t ldo;
+    int32_t out_f32;          // DW: fp32 result (slots, or an fp32 dW), else bf16
+};
+
+struct VocabCfg {
+    static constexpr uint32_t A_STAGE = 128 * 128, B_STAGE = 128 * 128, STAGE = A_STAGE + B_STAGE;
+    static constexpr int NST = 6;
+    static constexpr uint32_t BOX = 4096;                   // staging of an epilogue warp: 32 rows of 32 fp32, or two of bf16
+    static constexpr uint32_t OFF_BOX = NST * STAGE;
+    static constexpr uint32_t SMEM = OFF_BOX + 8 * BOX + 1024;
+    static_assert(SMEM <= 232448 - 512, "shared memory budget");
+    static constexpr int THREADS = 320;
+};
+
+__device__ __forceinline__ float exp2_fast(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// add a box to global memory (fp32), element by element
+__device__ __forceinline__ void tma_add_2d(const CUtensorMap *m, int32_t x, int32_t y, uint32_t src)
+{
+    asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(
+                     reinterpret_cast<uint64_t>(m)),
+                 "r"(x), "r"(y), "r"(src)
+                 : "memory");
+}
+
+// A row's targets in ascending order, seen from a tile: `next` is the next one's column in the tile (INT_MAX: none).
+struct Targets {
+    const int32_t *list;
+    const float *weight;
+    int K, p, base, next;
+    float q;
+    __device__ __forceinline__ void set()
+    {
+        next = INT_MAX;
+        if (p < K) {
+            const int32_t v = list[p];
+            if (v != INT32_MAX) {
+                next = v - base;
+                q = weight[p];
+            }
+        }
+    }
+    // those from column `first` of the tile that starts at word `base_` on
+    __device__ __forceinline__ void start(const VocabGemm &g, int64_t token, int base_, int first)
+    {
+        base = base_;
+        if (g.label) {
+            const int64_t y = g.label[token];
+            K = 0;
+            q = 1.0f;
+            next = y >= (int64_t)base + first && y < g.V ? (int)(y - base) : INT_MAX;
+            return;
+        }
+        K = g.K;
+        list = g.list + token * K;
+        weight = g.weight + token * K;
+        int lo = 0, hi = K;   // the first with list >= base + first
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (list[mid] < base + first) lo = mid + 1;
+            else hi = mid;
+        }
+        p = lo;
+        set();
+    }
+    __device__ __forceinline__ void advance()
+    {
+        if (K == 0) {
+            next = INT_MAX;
+        } else {
+            ++p;
+            set();
+        }
+    }
+};
+
+// MODE: what becomes of the accumulator; SPLIT: bf16 parts of an operand; PIECE: 64-deep slices of a piece of a sum (0: whole)
+template <int MODE, int SPLIT, int PIECE>
+__global__ void __launch_bounds__(VocabCfg::THREADS, 1)
+    k_vocab_gemm(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUtensorMap tmb,
+                 const __grid_constant__ CUtensorMap tmo, const VocabGemm g)
+{
+    using C = VocabCfg;
+    constexpr bool AMN = MODE == VG_DW, BMN = MODE == VG_DX || MODE == VG_DW;
+    constexpr bool PIECES = PIECE > 0;
+    constexpr int TERMS = SPLIT == 3 ? 6 : 1;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    __shared__ uint64_t full[C::NST], empty[C::NST], acc_full[2], acc_empty[2], done_bar;
+    __shared__ uint32_t tmem_base_sh;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t crank = cluster_rank();
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < C::NST; ++s) {
+            mbar_init(smem_u32(&full[s]), 1);
+            mbar_init(smem_u32(&empty[s]), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&acc_full[i]), 1);
+            mbar_init(smem_u32(&acc_empty[i]), 16);   // both CTAs' epilogue warps, on the even CTA
+        }
+        mbar_init(smem_u32(&done_bar), 1);
+        fence_mbar_init();
+    }
+    if (warp == 1) tmem_alloc_pair(smem_u32(&tmem_base_sh), 512);
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();   // the peer's barriers exist before anything arrives on them
+    tc_fence_after();
+    griddep_wait();
+    griddep_launch_dependents();
+    const uint32_t tmem = tmem_base_sh;
+
+    // the units, in every warp alike
+    const int n = g.n_ptr ? *g.n_ptr : g.n_rows;
+    const int rows = MODE == VG_DW ? g.rows : n;
+    const int depth = MODE == VG_DW ? n : g.depth;
+    const uint32_t nm = (uint32_t)((rows + 255) / 256), nn = (uint32_t)g.nn, per_split = nm * nn;
+    const uint32_t units = per_split * (uint32_t)g.splits;
+    const int slices = (depth + 63) / 64, per = (slices + g.splits - 1) / g.splits;
+    const uint32_t u_first = cluster_index(), u_step = gridDim.x / 2;
+    // unit -> its 128-row block of this CTA, column block, slices [k0, k0 + nk)
+    auto unit_of = [&](uint32_t u, int &mb, int &nb, int &ks, int &k0, int &nk) {
+        ks = (int)(u / per_split);
+        uint32_t r = u - (uint32_t)ks * per_split;
+        const uint32_t in_group = (uint32_t)g.group * nn, gi = r / in_group;
+        r -= gi * in_group;
+        const uint32_t left = nm - gi * (uint32_t)g.group, gr = left < (uint32_t)g.group ? left : (uint32_t)g.group;
+        nb = (int)(r / gr);
+        mb = 2 * (int)(gi * (uint32_t)g.group + r - (uint32_t)nb * gr) + (int)crank;
+        k0 = ks * per;
+        const int k1 = k0 + per < slices ? k0 + per : slices;
+        nk = k1 > k0 ? k1 - k0 : 0;
+    };
+    const int half_b = g.bn / 2;   // this CTA's columns of B
+
+    if (warp == 0) {
+        // ---------------- producer ----------------
+        if (elect_one()) {
+            tma_prefetch_desc(&tma);
+            tma_prefetch_desc(&tmb);
+            const int loads_b = BMN ? (half_b + 63) / 64 : 1;
+            const uint32_t bytes = 2 * (C::A_STAGE + (BMN ? (uint32_t)loads_b * 8192u : (uint32_t)half_b * 128u));
+            uint32_t it = 0;
+            bool ok = true;
+            for (uint32_t u = u_first; u < units && ok; u += u_step) {
+                int mb, nb, ks, k0, nk;
+                unit_of(u, mb, nb, ks, k0, nk);
+                const int piece = PIECES ? PIECE : nk;
+                for (int kp = 0; kp < nk && ok; kp += piece) {
+                    const int ke = nk - kp < piece ? nk : kp + piece;
+                    for (int term = 0; term < TERMS && ok; ++term) {
+                        // the partial products, smallest first: (2, 0) (1, 1) (0, 2) (1, 0) (0, 1) (0, 0)
+                        const int sa = SPLIT == 1 ? 0 : term == 0 ? 2 : (term == 1 || term == 3) ? 1 : 0;
+                        const int sb = SPLIT == 1 ? 0 : term == 2 ? 2 : (term == 1 || term == 4) ? 1 : 0;
+                        for (int kb = kp; kb < ke; ++kb, ++it) {
+                            const uint32_t s = it % C::NST, ph = (it / C::NST) & 1;
+                            if (!mbar_wait(smem_u32(&empty[s]), ph ^ 1)) {
+                                ok = false;
+                                break;
+                            }
+                            if (crank == 0) mbar_expect_tx(smem_u32(&full[s]), bytes);   // both CTAs' bytes
+                            const uint32_t bar = map_shared(smem_u32(&full[s]), 0);
+                            const uint32_t ad = smem_u32(smem + s * C::STAGE), bd = ad + C::A_STAGE;
+                            const int k = 64 * (k0 + kb);
+                            if (!AMN) {
+                                tma_load_2d_pair(ad, &tma, k, sa * g.a_off + mb * 128, bar);
+                            } else {
+                                tma_load_2d_pair(ad, &tma, mb * 128, sa * g.a_off + k, bar);
+                                tma_load_2d_pair(ad + 8192, &tma, mb * 128 + 64, sa * g.a_off + k, bar);
+                            }
+                            const int col = nb * g.bn + (int)crank * half_b;
+                            if (!BMN) {
+                                tma_load_2d_pair(bd, &tmb, k, sb * g.b_off + g.b_y + col, bar);
+                            } else {   // (what lies past the half is loaded and not read)
+                                for (int j = 0; j < loads_b; ++j)
+                                    tma_load_2d_pair(bd + j * 8192, &tmb, col + 64 * j, sb * g.b_off + (MODE == VG_DX ? g.b_y : 0) + k, bar);
+                            }
+                        }
+                    }
+                }
+            }
+            // the MMAs that read the last stages have completed before the CTA may leave
+            const uint32_t last = it < (uint32_t)C::NST ? it : (uint32_t)C::NST;
+            for (uint32_t i = 0; i < last && ok; ++i) {
+                const uint32_t j = it - 1 - i;
+                mbar_wait(smem_u32(&empty[j % C::NST]), (j / C::NST) & 1);
+            }
+        }
+    } else if (warp == 1) {
+        // ---------------- MMA issuer ----------------
+        if (crank == 0 && elect_one()) {
+            const uint32_t idesc = idesc_bf16(256, (uint32_t)g.bn, AMN, BMN);
+            const uint32_t a0 = smem_u32(smem), b0 = a0 + C::A_STAGE;
+            const uint64_t ad0 = AMN ? smem_desc(a0, 8192, 1024, kSwz128) : smem_desc(a0, 16, 1024, kSwz128);
+            const uint64_t bd0 = BMN ? smem_desc(b0, 8192, 1024, kSwz128) : smem_desc(b0, 16, 1024, kSwz128);
+            constexpr uint64_t AK = (AMN ? 2048 : 32) >> 4, BK = (BMN ? 2048 : 32) >> 4;
+            uint32_t it = 0, ti = 0;
+            bool ok = true;
+            for (uint32_t u = u_first; u < units && ok; u += u_step) {
+                int mb, nb, ks, k0, nk;
+                unit_of(u, mb, nb, ks, k0, nk);
+                const int piece = PIECES ? PIECE : nk;
+                for (int kp = 0; kp < nk && ok; kp += piece) {
+                    const uint32_t ab = ti & 1;
+                    ok = mbar_wait(smem_u32(&acc_empty[ab]), ((ti >> 1) & 1) ^ 1);
+                    tc_fence_after();
+                    if (!ok) break;
+                    const int steps = (nk - kp < piece ? nk - kp : piece) * TERMS;
+                    for (int i = 0; i < steps; ++i, ++it) {
+                        const uint32_t s = it % C::NST, ph = (it / C::NST) & 1;
+                        ok = mbar_wait(smem_u32(&full[s]), ph);
+                        tc_fence_after();
+                        if (!ok) break;
+                        const uint64_t so = (uint64_t)((s * C::STAGE) >> 4);
+#pragma unroll
+                        for (int kk = 0; kk < 4; ++kk)
+                            mma_bf16_pair(tmem + ab * 256, ad0 + so + kk * AK, bd0 + so + kk * BK, idesc, i > 0 || kk > 0);
+                        mma_commit_pair(smem_u32(&empty[s]));
+                    }
+                    if (!ok) break;
+                    mma_commit_pair(smem_u32(&acc_full[ab]));
+                    ++ti;
+                }
+            }
+            mma_commit_pair(smem_u32(&done_bar), 1);
+            mbar_wait(smem_u32(&done_bar), 0);
+        }
+    } else {
+        // ---------------- epilogue warps ----------------
+        const int q = warp & 3, half = (warp - 2) >> 2;   // TMEM lane quarter, which half of the columns
+        const uint32_t lane_base = (uint32_t)(q * 32) << 16;
+        const int groups = g.bn / 32, first_group = half ? (groups + 1) / 2 : 0;
+        const int my = half ? groups / 2 : (groups + 1) / 2;   // groups of 32 columns, up to 4
+        uint8_t *const box = smem + C::OFF_BOX + (warp - 2) * C::BOX;
+        uint32_t ti = 0, boxes = 0;
+        bool ok = true;
+
+        auto release_acc = [&](uint32_t ab) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_remote(map_shared(smem_u32(&acc_empty[ab]), 0));
+        };
+        // 32 columns of this thread's row as bf16: the next of the two 2 KB boxes, stored at (col, row0)
+        auto store_bf16 = [&](const float (&v)[32], int col, int row0) {
+            if (lane == 0) bulk_wait_read<1>();
+            __syncwarp();
+            uint8_t *b = box + (boxes++ & 1) * 2048;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                *reinterpret_cast<uint4 *>(b + swz_offset((uint32_t)lane, 16 * e, 64)) =
+                    make_uint4(pack_bf16(v[8 * e], v[8 * e + 1]), pack_bf16(v[8 * e + 2], v[8 * e + 3]),
+                               pack_bf16(v[8 * e + 4], v[8 * e + 5]), pack_bf16(v[8 * e + 6], v[8 * e + 7]));
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                tma_store_2d(&tmo, col, row0, smem_u32(b));
+                bulk_commit();
+            }
+        };
+        auto store_f32 = [&](const float (&v)[32], int col, int row0, bool add) {
+            if (lane == 0) bulk_wait_read<0>();
+            __syncwarp();
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                *reinterpret_cast<float4 *>(box + swz_offset((uint32_t)lane, 16 * e, 128)) =
+                    make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                if (add) tma_add_2d(&tmo, col, row0, smem_u32(box));
+                else tma_store_2d(&tmo, col, row0, smem_u32(box));
+                bulk_commit();
+            }
+        };
+        // DW into a matrix off the 16-byte grid: a row at a time, one element a lane
+        auto store_plain = [&](const float (&v)[32], int col, int row0) {
+            __syncwarp();
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                *reinterpret_cast<float4 *>(box + swz_offset((uint32_t)lane, 16 * e, 128)) =
+                    make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+            __syncwarp();
+            if (col + lane < g.cols) {
+                for (int r = 0; r < 32 && row0 + r < g.rows; ++r) {
+                    const float x = *reinterpret_cast<const float *>(box + swz_offset((uint32_t)r, 4 * lane, 128));
+                    const int64_t at = (int64_t)(g.out_y + row0 + r) * g.ldo + col + lane;
+                    if (g.out_f32) static_cast<float *>(g.out)[at] = x;
+                    else static_cast<__nv_bfloat16 *>(g.out)[at] = __float2bfloat16_rn(x);
+                }
+            }
+        };
+
+        for (uint32_t u = u_first; u < units && ok; u += u_step) {
+            int mb, nb, ks, k0, nk;
+            unit_of(u, mb, nb, ks, k0, nk);
+            const int row0 = mb * 128 + q * 32, row = row0 + lane;
+            // this thread's row
+            Targets t;
+            t.next = INT_MAX;
+            t.K = 0;
+            float most = -INFINITY, sum_e = 0.0f, zt = 0.0f, lse2 = 0.0f, grad = 0.0f;
+            bool hit = false;
+            if ((MODE == VG_FWD || MODE == VG_DZ) && row < n) {
+                const int64_t token = g.token ? g.token[row] : row;
+                t.start(g, token, g.v0 + nb * g.bn, first_group * 32);
+                if (MODE == VG_DZ) {
+                    lse2 = g.lse[token] * 1.4426950408889634f;
+                    grad = g.dloss[token * g.dloss_step] * g.tau;
+                    if (g.label ? g.label[token] >= g.V : false) grad = NAN;
+                    if (g.bad) grad += g.bad[token];
+                }
+            }
+            // what becomes of 32 columns of the row, from column `c` of the tile on
+            auto process = [&](float (&v)[32], int c) {
+                const int col = nb * g.bn + c;
+                if (MODE == VG_FWD) {
+                    if (row0 >= n || col >= g.cols) return;
+                    if (col + 32 > g.cols) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (col + j >= g.cols) v[j] = -INFINITY;
+                    }
+                    while (t.next < c + 32) {
+                        const int at = t.next - c;
+                        float x = 0.0f;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (j == at) x = v[j];
+                        zt = fmaf(t.q, x, zt);
+                        hit = true;
+                        t.advance();
+                    }
+                    float m[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+                    for (int j = 4; j < 32; ++j) m[j & 3] = max_nan(m[j & 3], v[j]);
+                    const float top = max_nan(max_nan(m[0], m[1]), max_nan(m[2], m[3])) * g.c;
+                    const float now = max_nan(most, top);
+                    if (now == -INFINITY) return;
+                    float s[4] = {sum_e * exp2_fast(most - now), 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) s[j & 3] += exp2_fast(fmaf(v[j], g.c, -now));
+                    sum_e = (s[0] + s[1]) + (s[2] + s[3]);
+                    most = now;
+                } else if (MODE == VG_DZ) {
+                    if (col >= g.cols) return;
+                    if (row < n) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = exp2_fast(fmaf(v[j], g.c, -lse2));
+                        while (t.next < c + 32) {
+                            const int at = t.next - c;
+#pragma unroll
+                            for (int j = 0; j < 32; ++j)
+                                if (j == at) v[j] -= t.q;
+                            t.advance();
+                        }
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] *= grad;
+                    } else {   // zeros up to the end of the row block: VG_DW's depth ends inside it
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = 0.0f;
+                    }
+#pragma unroll
+                    for (int part = 0; part < SPLIT; ++part) {
+                        store_bf16(v, col, part * g.slot_rows + row0);
+                        if (part + 1 < SPLIT) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) v[j] -= __bfloat162float(__float2bfloat16_rn(v[j]));
+                        }
+                    }
+                } else {
+                    if (row0 >= rows || col >= g.cols) return;
+                    if (MODE == VG_DX) store_f32(v, col, ks * g.slot_rows + row0, g.add);
+                    else if (g.out) store_plain(v, col, row0);
+                    else if (g.out_f32) store_f32(v, col, g.out_y + ks * g.slot_rows + row0, false);
+                    else store_bf16(v, col, g.out_y + row0);
+                }
+            };
+            if (nk == 0) {   // nothing to add up: zeros (no token in use, or a split past the end)
+                if (MODE == VG_DX || MODE == VG_DW) {
+#pragma unroll 1
+                    for (int i = 0; i < my; ++i) {
+                        float v[32];
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = 0.0f;
+                        process(v, (first_group + i) * 32);
+                    }
+                }
+                continue;
+            }
+            if constexpr (PIECES) {
+                float sum[4][32];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) sum[i][j] = 0.0f;
+#pragma unroll 1
+                for (int kp = 0; kp < nk; kp += PIECE, ++ti) {
+                    const uint32_t ab = ti & 1;
+                    ok = mbar_wait(smem_u32(&acc_full[ab]), (ti >> 1) & 1);
+                    tc_fence_after();
+                    if (!ok) break;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if (i < my) {   // (the same for the whole warp)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {   // (32 at a time spill)
+                                float v[16];
+                                tmem_ld16(tmem + lane_base + ab * 256 + (first_group + i) * 32 + 16 * h, v);
+                                tmem_ld_wait();
+                                tmem_regs_ready(v);
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) sum[i][16 * h + j] += v[j];
+                            }
+                        }
+                    }
+                    release_acc(ab);
+                }
+                if (!ok) break;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (i < my) process(sum[i], (first_group + i) * 32);
+            } else {
+                const uint32_t ab = ti & 1;
+                ok = mbar_wait(smem_u32(&acc_full[ab]), (ti >> 1) & 1);
+                tc_fence_after();
+                if (!ok) break;
+#pragma unroll 1
+                for (int i = 0; i < my; ++i) {
+                    float v[32];
+                    tmem_ld32(tmem + lane_base + ab * 256 + (first_group + i) * 32, v);
+                    tmem_ld_wait();
+                    tmem_regs_ready(v);
+                    if (i == my - 1) release_acc(ab);
+                    process(v, (first_group + i) * 32);
+                }
+                if (my == 0) release_acc(ab);
+                ++ti;
+            }
+            if (MODE == VG_FWD && row < n) {   // (a half without columns too: the sums are joined over all slots)
+                const int64_t at = (int64_t)(g.slot0 + 2 * nb + half) * g.tp + row;
+                g.stat[at] = make_float2(most, sum_e);
+                if (g.label) {
+                    if (hit) g.zt[row] = zt;
+                } else {
+                    g.zt[at] = zt;
+                }
+            }
+        }
+    }
+    if (MODE != VG_FWD && warp >= 2 && lane == 0) bulk_wait<0>();   // this warp's stores are done
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();   // neither CTA leaves, or frees TMEM, while the other may still address it
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc_pair(tmem, 512);
+    }
+}
+
+}  // namespace tc
+}  // namespace resbm

@@ -1,4 +1,4 @@
-"""Python binding of the C ABI in include/resbm.h and include/resbm_train.h (libresbm.so).
+"""Python binding of the C ABI in include/resbm.h, include/resbm_train.h and include/resbm_vocab.h (libresbm.so).
 
 Argument marshalling only: every function here has the C function's name, takes torch tensors
 (device memory owned by the caller) or None, passes their data pointers and the current CUDA
@@ -48,6 +48,10 @@ EXPORTS = ("resbm_version", "resbm_status_string", "resbm_last_cuda_error", "res
 # the functions of include/resbm_train.h
 TRAIN_EXPORTS = ("resbm_add_rmsnorm_fwd", "resbm_adamw_plan_bytes", "resbm_adamw_plan", "resbm_adamw_step",
                  "resbm_grad_norm_workspace_bytes", "resbm_grad_norm")
+# the functions of include/resbm_vocab.h
+VOCAB_EXPORTS = ("resbm_vocab_workspace_bytes", "resbm_linear_ce_fwd", "resbm_linear_ce_bwd", "resbm_distill_fwd",
+                 "resbm_distill_bwd", "resbm_embed_fwd", "resbm_embed_bwd")
+(RESBM_VOCAB_CE_FWD, RESBM_VOCAB_CE_BWD, RESBM_VOCAB_DISTILL_FWD, RESBM_VOCAB_DISTILL_BWD, RESBM_VOCAB_EMBED_BWD) = range(5)
 RESBM_STATE_NONE, RESBM_STATE_E4M3, RESBM_STATE_F32 = 0, 8, 32
 RESBM_STATE_BLOCK = 256
 
@@ -82,6 +86,17 @@ class resbm_adamw_tensor(ctypes.Structure):
 class resbm_adamw_hyper(ctypes.Structure):
     _fields_ = [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay")] + \
                [("step", ctypes.c_int64)] + [(n, ctypes.c_void_p) for n in ("lr_dev", "step_dev", "grad_scale")]
+
+
+class resbm_vocab_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("T", "V", "d", "ldx", "ldw", "K")] + \
+               [("dtype", ctypes.c_int32), ("teacher_dtype", ctypes.c_int32), ("temperature", ctypes.c_float),
+                ("dloss_each", ctypes.c_int32), ("flags", ctypes.c_uint32)]
+
+
+class resbm_embed_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("T", "V", "d", "ldt", "ldo", "padding")] + \
+               [("dtype", ctypes.c_int32), ("scale", ctypes.c_float), ("flags", ctypes.c_uint32)]
 
 
 class ResbmError(RuntimeError):
@@ -166,6 +181,16 @@ def load(path: str | None = None) -> ctypes.CDLL:
     lib.resbm_grad_norm_workspace_bytes.argtypes = [ctypes.POINTER(vp), i64, ctypes.POINTER(sz)]
     lib.resbm_grad_norm.restype = i32
     lib.resbm_grad_norm.argtypes = [ctypes.POINTER(vp), i64, ctypes.c_float, vp, vp, sz, vp]
+    lib.resbm_vocab_workspace_bytes.restype = i32
+    lib.resbm_vocab_workspace_bytes.argtypes = [ctypes.POINTER(resbm_vocab_desc), i32, ctypes.POINTER(sz)]
+    for name, tensors in (("linear_ce_fwd", 5), ("linear_ce_bwd", 7), ("distill_fwd", 6), ("distill_bwd", 8)):
+        f = getattr(lib, "resbm_" + name)
+        f.restype = i32
+        f.argtypes = [ctypes.POINTER(resbm_vocab_desc)] + [vp] * tensors + [vp, sz, vp]
+    lib.resbm_embed_fwd.restype = i32
+    lib.resbm_embed_fwd.argtypes = [ctypes.POINTER(resbm_embed_desc)] + [vp] * 4
+    lib.resbm_embed_bwd.restype = i32
+    lib.resbm_embed_bwd.argtypes = [ctypes.POINTER(resbm_embed_desc)] + [vp] * 3 + [vp, sz, vp]
     if path is None:
         _lib = lib
     return lib
@@ -603,3 +628,129 @@ def resbm_grad_norm(plans, max_norm, out, ws, stream=None):
     st = load().resbm_grad_norm(array, len(plans), max_norm, out.data_ptr(), ws.data_ptr(), _nbytes(ws), _stream(stream))
     if st != RESBM_OK:
         _check("resbm_grad_norm", st)
+
+
+# ---- the vocabulary's operators (include/resbm_vocab.h) ------------------------------------------------
+def resbm_vocab_workspace_bytes(op, T, V, d, dtype="bf16", K=0) -> int:
+    """Bytes of the workspace of an op (RESBM_VOCAB_*) over T tokens, V words, width d; distillation: K entries a token."""
+    dt = DTYPES[dtype] if isinstance(dtype, str) else int(dtype)
+    out = ctypes.c_size_t(0)
+    desc = resbm_vocab_desc(int(T), int(V), int(d), int(d), int(d), int(K), dt, dt, 1.0, 0, 0)
+    _check("resbm_vocab_workspace_bytes", load().resbm_vocab_workspace_bytes(ctypes.byref(desc), int(op), ctypes.byref(out)))
+    return int(out.value)
+
+
+def vocab_workspace(op, T, V, d, dtype="bf16", K=0, device="cuda") -> torch.Tensor:
+    return torch.empty(max(resbm_vocab_workspace_bytes(op, T, V, d, dtype, K), 1), dtype=torch.uint8, device=device)
+
+
+def _dense(t, shape, dtypes, device, what):
+    if t.shape != shape or t.dtype not in dtypes or not t.is_contiguous():
+        raise ValueError("%s must be %s, dense, %s" % (what, tuple(shape), " or ".join(map(str, dtypes))))
+    _here(t, device, what)
+
+
+_F32, _I64 = (torch.float32,), (torch.int64,)
+
+
+def _loss_desc(X, W, target, teacher, temperature, device):
+    """The descriptor of a loss over the vocabulary, of checked inputs"""
+    if X.dim() != 2 or W.dim() != 2 or X.dtype not in _DT or X.shape[1] < 1 or W.shape[0] < 1:
+        raise ValueError("X must be (T, d) and W (V, d), fp32 or bf16")
+    (T, d), V, dtype = X.shape, W.shape[0], X.dtype
+    ldx = _row_stride(X, (T, d), dtype, device, "X")
+    ldw = _row_stride(W, (V, d), dtype, device, "W")
+    K, tdt = 0, RESBM_F32
+    if teacher is None:
+        _dense(target, (T,), _I64, device, "labels")
+    else:
+        if target.dim() != 2 or not 1 <= target.shape[1] <= 1024:
+            raise ValueError("index must be (T, K) with K from 1 to 1024")
+        K = target.shape[1]
+        _dense(target, (T, K), _I64, device, "index")
+        _dense(teacher, (T, K), tuple(_DT), device, "teacher")
+        tdt = _DT[teacher.dtype]
+    return resbm_vocab_desc(T, V, d, ldx if T > 1 else d, ldw if V > 1 else d, K, _DT[dtype], tdt, temperature, 0, 0)
+
+
+def _loss_fwd(fn, X, W, target, teacher, temperature, loss, lse, ws, stream):
+    device = _device()
+    desc = _loss_desc(X, W, target, teacher, temperature, device)
+    _dense(loss, (desc.T,), _F32, device, "loss")
+    _dense(lse, (desc.T,), _F32, device, "lse")
+    _workspace_here(ws, device)
+    args = [_p(X), _p(W), _p(target)] + ([] if teacher is None else [_p(teacher)])
+    _check(fn, getattr(_lib or load(), fn)(desc, *args, _p(loss), _p(lse), _p(ws), _nbytes(ws), _stream(stream)))
+
+
+def _loss_bwd(fn, X, W, target, teacher, temperature, lse, dloss, dX, dW, ws, stream):
+    device = _device()
+    desc = _loss_desc(X, W, target, teacher, temperature, device)
+    _dense(lse, (desc.T,), _F32, device, "lse")
+    if dloss.dtype != torch.float32 or dloss.shape not in ((), (1,), (desc.T,)) or not dloss.is_contiguous():
+        raise ValueError("dloss must be (%d,) or one element, fp32, dense" % desc.T)
+    _here(dloss, device, "dloss")
+    desc.dloss_each = int(dloss.shape == (desc.T,))
+    if dX is not None:
+        _dense(dX, X.shape, (X.dtype,), device, "dX")
+    if dW is not None:
+        _dense(dW, W.shape, (W.dtype,), device, "dW")
+    _workspace_here(ws, device)
+    args = [_p(X), _p(W), _p(target)] + ([] if teacher is None else [_p(teacher)])
+    _check(fn, getattr(_lib or load(), fn)(desc, *args, _p(lse), _p(dloss), _p(dX), _p(dW), _p(ws), _nbytes(ws), _stream(stream)))
+
+
+def _workspace_here(ws, device):
+    if ws is not None:
+        _here(ws, device, "ws")
+        _want(ws.is_contiguous(), "ws must be dense")   # (an expanded one is smaller than its elements)
+
+
+def resbm_linear_ce_fwd(X, W, labels, loss, lse, ws, stream=None):
+    """loss and lse (T fp32): the cross entropy of the logits X . W^T against labels (T int64; negative: no label), without the
+    logits. X (T, d) and W (V, d) of one type, unit stride along d, any row stride."""
+    _loss_fwd("resbm_linear_ce_fwd", X, W, labels, None, 1.0, loss, lse, ws, stream)
+
+
+def resbm_linear_ce_bwd(X, W, labels, lse, dloss, dX, dW, ws, stream=None):
+    """dX (T, d) and dW (V, d), dense, either may be None: the gradients for dloss (T fp32, or one for all)."""
+    _loss_bwd("resbm_linear_ce_bwd", X, W, labels, None, 1.0, lse, dloss, dX, dW, ws, stream)
+
+
+def resbm_distill_fwd(X, W, index, teacher, temperature, loss, lse, ws, stream=None):
+    """loss and lse (T fp32): temperature^2 times the divergence of softmax(X . W^T / temperature) from the softmax of the
+    teacher's logits (T, K; fp32 or bf16) at the words index (T, K int64; negative: no entry)."""
+    _loss_fwd("resbm_distill_fwd", X, W, index, teacher, temperature, loss, lse, ws, stream)
+
+
+def resbm_distill_bwd(X, W, index, teacher, temperature, lse, dloss, dX, dW, ws, stream=None):
+    _loss_bwd("resbm_distill_bwd", X, W, index, teacher, temperature, lse, dloss, dX, dW, ws, stream)
+
+
+def _embed_desc(ids, V, rows, scale, padding, device, what):
+    if rows.dim() != 2 or rows.dtype not in _DT or ids.dim() != 1 or rows.shape[1] < 1 or V < 1:
+        raise ValueError("ids must be (T,), %s (T, d), fp32 or bf16" % what)
+    T, d = ids.shape[0], rows.shape[1]
+    _dense(ids, (T,), _I64, device, "ids")
+    ldo = _row_stride(rows, (T, d), rows.dtype, device, what)
+    return resbm_embed_desc(T, V, d, d, ldo if T > 1 else d, padding, _DT[rows.dtype], scale, 0)
+
+
+def resbm_embed_fwd(ids, table, scale, out, stream=None):
+    """out (T, d) = scale * table[ids]; table (V, d); ids (T int64). Unit stride along d, any row stride. An id outside the
+    table gives a row of NaN."""
+    device = _device()
+    desc = _embed_desc(ids, table.shape[0], out, scale, -1, device, "out")
+    ldt = _row_stride(table, (desc.V, desc.d), out.dtype, device, "table")
+    desc.ldt = ldt if desc.V > 1 else desc.d
+    _check("resbm_embed_fwd", (_lib or load()).resbm_embed_fwd(desc, _p(ids), _p(table), _p(out), _stream(stream)))
+
+
+def resbm_embed_bwd(ids, dout, scale, dtable, ws, padding=-1, stream=None):
+    """dtable (V, d), dense = scale * the sum of dout's rows (T, d) over each word's tokens; zero for padding (an id; negative:
+    none)."""
+    device = _device()
+    desc = _embed_desc(ids, dtable.shape[0], dout, scale, padding, device, "dout")
+    _dense(dtable, (desc.V, desc.d), (dout.dtype,), device, "dtable")
+    _workspace_here(ws, device)
+    _check("resbm_embed_bwd", (_lib or load()).resbm_embed_bwd(desc, _p(ids), _p(dout), _p(dtable), _p(ws), _nbytes(ws), _stream(stream)))

@@ -98,23 +98,33 @@ __global__ void __launch_bounds__(256) k_embed_fwd(const int64_t *__restrict__ i
 // ---- tokens sorted by id -------------------------------------------------------------------------------
 constexpr int kSortCtas = 8, kSortThreads = 1024, kMaxBins = 512;
 
+// The first cluster sorts, the others write zeros over dtable meanwhile: most words have no tokens, and the sums
+// overwrite the rows of those that have (16384 tokens of 32000 words: 22 MB of 131).
+//
 // Stable: one cluster of eight CTAs, a radix sort of the ids from their lowest digit on. Each warp has a contiguous run of the
 // positions; its equal digits are found 32 at a time by a match, so that ranks need no atomics and keep the order. Ids that
-// count for nothing become V and sort behind the others. Then a bit for every word that has tokens. T = 16384 tokens of 32000
-// words are two passes of 8 bits. (A sort over the whole GPU would be several launches; this one's time is their latency.)
+// count for nothing become V and sort behind the others. T = 16384 tokens of 32000 words are two passes of 8 bits. (A sort over the whole GPU would be several launches; this one's time is their latency.)
 __global__ void __cluster_dims__(kSortCtas) __launch_bounds__(kSortThreads, 1)
-    k_sort(const int64_t *__restrict__ ids, int T, int V, int64_t padding, int passes, int bits, int32_t *keys, int32_t *vals, uint32_t *present)
+    k_sort(const int64_t *__restrict__ ids, int T, int V, int64_t padding, int passes, int bits, int32_t *keys, int32_t *vals, uint8_t *dtable, int64_t bytes)
 {
     extern __shared__ int32_t cnt[];   // 32 warps x bins: counts, then places
     __shared__ int32_t total[kMaxBins], wsum[32];
     griddep_wait();
     griddep_launch_dependents();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tid = threadIdx.x;
+    if (cluster_index() > 0) {
+        const int64_t head = min((int64_t)((16 - (reinterpret_cast<uintptr_t>(dtable) & 15)) & 15), bytes), vecs = (bytes - head) / 16;
+        uint4 *v = reinterpret_cast<uint4 *>(dtable + head);
+        const int64_t at = (int64_t)(blockIdx.x - kSortCtas) * kSortThreads + tid, step = (int64_t)(gridDim.x - kSortCtas) * kSortThreads;
+        for (int64_t i = at; i < vecs; i += step) v[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (at < head) dtable[at] = 0;
+        if (at < bytes - head - 16 * vecs) dtable[head + 16 * vecs + at] = 0;
+        return;
+    }
     const int rank = (int)cluster_rank(), bins = 1 << bits;
     const int per_warp = ((T + kSortCtas * 32 - 1) / (kSortCtas * 32) + 31) / 32 * 32;
     const int64_t first = ((int64_t)rank * 32 + warp) * per_warp;
     const int p0 = (int)(first < T ? first : T), p1 = (int)(first + per_warp < T ? first + per_warp : T);
-    for (int i = rank * kSortThreads + tid; i < (V + 31) / 32; i += kSortCtas * kSortThreads) present[i] = 0u;
     int32_t *mine = cnt + warp * bins;
     for (int pass = 0; pass < passes; ++pass) {
         const int32_t *kin = keys + (int64_t)((pass & 1) ^ 1) * T, *vin = vals + (int64_t)((pass & 1) ^ 1) * T;
@@ -184,11 +194,6 @@ __global__ void __cluster_dims__(kSortCtas) __launch_bounds__(kSortThreads, 1)
         __threadfence();
         cluster_sync();   // (and no CTA reads another's totals any more)
     }
-    const int32_t *sorted = keys + (int64_t)((passes - 1) & 1) * T;
-    for (int p = rank * kSortThreads + tid; p < T; p += kSortCtas * kSortThreads) {
-        const int32_t k = __ldcg(sorted + p);
-        if (k < V && (p == 0 || __ldcg(sorted + p - 1) != k)) atomicOr(&present[k >> 5], 1u << (k & 31));
-    }
 }
 
 // ---- sums ------------------------------------------------------------------------------------------------
@@ -196,35 +201,21 @@ constexpr int kRun = 32;   // sorted positions a block
 
 struct SumArgs {
     const int32_t *keys, *vals;   // sorted
-    const uint32_t *present;
     const void *dout;
     void *dtable;
     float *part;                  // (block, head or tail, column)
     int64_t ldo, d;
-    int T, V, sum_ctas, log_tx;
+    int T, V, log_tx;
     float scale;
 };
 
-// CTAs below sum_ctas: blocks of kRun sorted positions, 2^log_tx threads along a row, which add the rows of each word up in
-// order. A word whose tokens all lie in the block is finished; the block's first and last runs may be pieces of longer ones,
-// and leave a partial sum (k_embed_join). So the work is even whatever the ids are. The other CTAs write the zero rows.
+// Blocks of kRun sorted positions, 2^log_tx threads along a row, which add the rows of each word up in order, sixteen in
+// flight. A word whose tokens all lie in the block is finished; the block's first and last runs may be pieces of longer ones, and
+// leave a partial sum (k_embed_join). So the work is even whatever the ids are.
 template <typename E, int VEC> __global__ void __launch_bounds__(256) k_embed_sum(const SumArgs a)
 {
     griddep_wait();
     griddep_launch_dependents();
-    if ((int)blockIdx.x >= a.sum_ctas) {
-        if (blockIdx.y) return;
-        const int lane = threadIdx.x & 31;
-        const int step = (gridDim.x - a.sum_ctas) * 8;
-        Cols<E, VEC> zero;
-        zero.fill(0.0f);
-        for (int64_t v = (blockIdx.x - a.sum_ctas) * 8 + (threadIdx.x >> 5); v < a.V; v += step) {
-            if (a.present[v >> 5] >> (v & 31) & 1) continue;
-            E *row = static_cast<E *>(a.dtable) + v * a.d;
-            for (int64_t c = lane * VEC; c < a.d; c += 32 * VEC) zero.store(row + c, 0.0f);
-        }
-        return;
-    }
     const int per_cta = 256 >> a.log_tx;
     const int b = blockIdx.x * per_cta + (threadIdx.x >> a.log_tx);
     const int64_t col = (((int64_t)blockIdx.y << a.log_tx) + (threadIdx.x & ((1 << a.log_tx) - 1))) * VEC;
@@ -236,21 +227,26 @@ template <typename E, int VEC> __global__ void __launch_bounds__(256) k_embed_su
     const bool tail = p0 + len < a.T && key[len] == key[len - 1];        // the last one goes on
     const E *dout = static_cast<const E *>(a.dout) + col;
     float *part = a.part + (int64_t)b * 2 * a.d + col;
+    constexpr int F = VEC == 1 ? 16 : 8;   // rows in flight
     Cols<E, VEC> sum;
     sum.fill(0.0f);
     bool first_run = true;
-    int32_t k = key[0];
-    for (int i = 0; i < len && k < a.V; i += 8) {
-        Cols<E, VEC> v[8];
-        int32_t ks[9];
+#pragma unroll 1
+    for (int i = 0; i < len; i += F) {
+        Cols<E, VEC> v[F];
+        int32_t ks[F + 1], at[F];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < F; ++j) {
             ks[j] = i + j < len ? key[i + j] : a.V;
-            if (ks[j] < a.V) v[j].load(dout + (int64_t)val[i + j] * a.ldo);
+            at[j] = i + j < len ? val[i + j] : 0;
         }
-        ks[8] = i + 8 < len ? key[i + 8] : INT32_MAX;
+        ks[F] = i + F < len ? key[i + F] : INT32_MAX;
+        if (ks[0] >= a.V) break;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < F; ++j)
+            if (ks[j] < a.V) v[j].load(dout + (int64_t)at[j] * a.ldo);
+#pragma unroll
+        for (int j = 0; j < F; ++j) {
             if (ks[j] >= a.V) break;
             sum.add(v[j]);
             const bool end = i + j + 1 == len;
@@ -266,7 +262,6 @@ template <typename E, int VEC> __global__ void __launch_bounds__(256) k_embed_su
             sum.fill(0.0f);
             first_run = false;
         }
-        k = ks[8] == INT32_MAX ? a.V : ks[8];
     }
 }
 
@@ -282,32 +277,29 @@ template <typename E, int VEC> __global__ void __launch_bounds__(256) k_embed_jo
     if (col >= a.d || b + 1 >= blocks) return;
     const int32_t k = a.keys[p0 + kRun - 1];
     if (k >= a.V || a.keys[p0 + kRun] != k || (b > 0 && a.keys[p0 - 1] == k)) return;
-    // the last block with tokens of the word: keys ascend
-    int64_t lo = b + 1, hi = blocks - 1;
-    while (lo < hi) {
-        const int64_t mid = (lo + hi + 1) >> 1;
-        if (a.keys[mid * kRun] == k) lo = mid;
-        else hi = mid - 1;
-    }
     Cols<E, VEC> sum;
     const float *tail = a.part + (b * 2 + 1) * a.d + col;
 #pragma unroll
     for (int e = 0; e < VEC; ++e) sum.x[e] = tail[e];
-    for (int64_t i = b + 1; i <= lo; i += 4) {
-        float x[4][VEC];
+    bool more = true;
+    for (int64_t i = b + 1; more && i < blocks; i += 8) {   // (a block that has none of the word has no partial sum: loaded, not used)
+        float x[8][VEC];
+        bool has[8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (i + j <= lo) {
-                const float *head = a.part + (i + j) * 2 * a.d + col;
+        for (int j = 0; j < 8; ++j) {
+            const int64_t at = i + j < blocks ? i + j : blocks - 1;
+            has[j] = i + j < blocks && a.keys[at * kRun] == k;
+            const float *head = a.part + at * 2 * a.d + col;
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) x[j][e] = head[e];
-            }
+            for (int e = 0; e < VEC; ++e) x[j][e] = head[e];
+        }
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (i + j <= lo) {
+        for (int j = 0; j < 8; ++j)
+            if (has[j]) {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) sum.x[e] += x[j][e];
             }
+        more = has[7];
     }
     sum.store(static_cast<E *>(a.dtable) + (int64_t)k * a.d + col, a.scale);
 }
@@ -322,17 +314,15 @@ int log_threads(int64_t vectors)
 
 struct EmbedWs {
     int32_t *keys, *vals;
-    uint32_t *present;
     float *part;
     size_t bytes;
 };
-EmbedWs carve(void *ws, int64_t T, int64_t V, int64_t d)
+EmbedWs carve(void *ws, int64_t T, int64_t d)
 {
     WsCarver w(ws);
     EmbedWs e;
     e.keys = w.take<int32_t>(2 * T);
     e.vals = w.take<int32_t>(2 * T);
-    e.present = w.take<uint32_t>((V + 31) / 32);
     e.part = w.take<float>((T + kRun - 1) / kRun * 2 * d);
     e.bytes = w.used;
     return e;
@@ -379,19 +369,24 @@ template <typename E> cudaError_t run_bwd(const resbm_embed_desc &d, const int64
     static std::atomic<uint8_t> done[kMaxDev];
     cudaError_t e = ensure_smem(k_sort, 32 * 4 * kMaxBins, c.device, done);
     // (the cluster's size is the kernel's own)
-    if (e == cudaSuccess) e = launch(k_sort, dim3(kSortCtas), dim3(kSortThreads), smem, c.stream, ids, (int)d.T, (int)d.V, d.padding, passes, bits, w.keys, w.vals, w.present);
+    // the rest of the SMs write zeros, 64 KB a CTA at least
+    const int64_t bytes = d.V * d.d * (int64_t)sizeof(E);
+    const int64_t zeros = std::min<int64_t>((bytes + 65535) / 65536, std::max(kSortCtas, c.sm_count - kSortCtas));
+    const unsigned grid = (unsigned)(kSortCtas + (zeros + kSortCtas - 1) / kSortCtas * kSortCtas);
+    if (e == cudaSuccess) e = launch(k_sort, dim3(grid), dim3(kSortThreads), smem, c.stream, ids, (int)d.T, (int)d.V, d.padding, passes, bits, w.keys, w.vals,
+                                     static_cast<uint8_t *>(dtable), bytes);
     if (e != cudaSuccess) return e;
     constexpr int V16 = 16 / (int)sizeof(E);
     const bool vec = d.d % V16 == 0 && al16(dout) && al16(dtable) && (d.T == 1 || d.ldo % V16 == 0);
     const int64_t n = vec ? d.d / V16 : d.d;
     const int log_tx = log_threads(n);
     const int64_t per = 256 >> log_tx, blocks = (d.T + kRun - 1) / kRun, cols = (n + (int64_t(1) << log_tx) - 1) >> log_tx;
-    SumArgs a{w.keys + ((passes - 1) & 1) * d.T, w.vals + ((passes - 1) & 1) * d.T, w.present, dout, dtable, w.part, d.ldo, d.d, (int)d.T, (int)d.V,
-              (int)((blocks + per - 1) / per), log_tx, d.scale};
-    const int64_t zero = std::min<int64_t>((d.V + 7) / 8, 4 * c.sm_count);
+    SumArgs a{w.keys + ((passes - 1) & 1) * d.T, w.vals + ((passes - 1) & 1) * d.T, dout, dtable, w.part, d.ldo, d.d, (int)d.T, (int)d.V,
+              log_tx, d.scale};
+    const dim3 ctas((unsigned)((blocks + per - 1) / per), (unsigned)cols);
     auto go = [&](auto sum, auto join) {
-        cudaError_t e = launch(sum, dim3((unsigned)(a.sum_ctas + zero), (unsigned)cols), dim3(256), 0, c.stream, a);
-        if (e == cudaSuccess && blocks > 1) e = launch(join, dim3((unsigned)a.sum_ctas, (unsigned)cols), dim3(256), 0, c.stream, a);
+        cudaError_t e = launch(sum, ctas, dim3(256), 0, c.stream, a);
+        if (e == cudaSuccess && blocks > 1) e = launch(join, ctas, dim3(256), 0, c.stream, a);
         return e;
     };
     e = vec ? go(k_embed_sum<E, V16>, k_embed_join<E, V16>) : go(k_embed_sum<E, 1>, k_embed_join<E, 1>);
@@ -401,7 +396,7 @@ template <typename E> cudaError_t run_bwd(const resbm_embed_desc &d, const int64
 
 }  // namespace
 
-size_t embed_bwd_ws_bytes(int64_t T, int64_t V, int64_t d) { return carve(nullptr, T, V, d).bytes; }
+size_t embed_bwd_ws_bytes(int64_t T, int64_t d) { return carve(nullptr, T, d).bytes; }
 
 }  // namespace resbm
 
@@ -436,12 +431,12 @@ resbm_status resbm_embed_bwd(const resbm_embed_desc *desc, const int64_t *ids, c
     const Range outs[] = {rng(dtable, d.V * d.d, es), rng(ws, (int64_t)std::min<size_t>(ws_bytes, INT64_MAX), 1)};
     const Range ins[] = {rows_of(dout, d.T, d.ldo, d.d, es), rng(ids, d.T, 8)};
     if (any_overlap(outs, ins, 2)) return RESBM_ERR_INVALID_ARG;
-    if (d.T > 0 && (!ws || ws_bytes < embed_bwd_ws_bytes(d.T, d.V, d.d))) return RESBM_ERR_WORKSPACE;
+    if (d.T > 0 && (!ws || ws_bytes < embed_bwd_ws_bytes(d.T, d.d))) return RESBM_ERR_WORKSPACE;
     Ctx c;
     st = make_ctx(stream, &c);
     if (st != RESBM_OK) return st;
     if (d.T == 0) return finish(cudaMemsetAsync(dtable, 0, (size_t)(d.V * d.d * es), c.stream));
-    const EmbedWs w = carve(ws, d.T, d.V, d.d);
+    const EmbedWs w = carve(ws, d.T, d.d);
     const cudaError_t e = d.dtype == RESBM_F32 ? run_bwd<float>(d, ids, dout, dtable, w, c) : run_bwd<__nv_bfloat16>(d, ids, dout, dtable, w, c);
     if (e != cudaSuccess) cudaGetLastError();
     return finish(e);

@@ -89,48 +89,50 @@ __global__ void __launch_bounds__(256) k_targets(const int64_t *__restrict__ ind
 }
 
 // ---- the tokens in use -----------------------------------------------------------------------------
-// token[r] = the r-th token with a target, row[t] = its r or -1, *n = how many. One CTA, eight tokens a thread and round.
-__global__ void __launch_bounds__(1024) k_scan(const int64_t *__restrict__ label, const int32_t *__restrict__ count, int T,
-                                               int32_t *__restrict__ n, int32_t *__restrict__ token, int32_t *__restrict__ row)
+// token[r] = the r-th token with a target, row[t] = its r or -1, *n = how many. One cluster of eight CTAs, a contiguous run of the
+// tokens a warp, counted and then written. (One CTA with eight loads a thread, one after the other: 27 us at T = 16384; this 5.)
+constexpr int kScanCtas = 8;
+__global__ void __cluster_dims__(kScanCtas) __launch_bounds__(1024) k_scan(const int64_t *__restrict__ label, const int32_t *__restrict__ count, int T,
+                                                                           int32_t *__restrict__ n, int32_t *__restrict__ token, int32_t *__restrict__ row)
 {
-    __shared__ int sums[32];
+    __shared__ int sums[32], total;
     griddep_wait();
     griddep_launch_dependents();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int base = 0;
-    for (int t0 = 0; t0 < T; t0 += 8192) {
-        const int t = t0 + 8 * (int)threadIdx.x;
-        uint32_t has = 0;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rank = (int)cluster_rank();
+    const int per = ((T + kScanCtas * 32 - 1) / (kScanCtas * 32) + 31) / 32 * 32;
+    const int64_t first = ((int64_t)rank * 32 + warp) * per;
+    const int p0 = (int)(first < T ? first : T), p1 = (int)(first + per < T ? first + per : T);
+    auto has = [&](int t) { return t < p1 && (label ? label[t] >= 0 : count[t] > 0); };
+    int mine = 0;
+#pragma unroll 4
+    for (int p = p0; p < p1; p += 32) mine += __popc(__ballot_sync(0xffffffffu, has(p + lane)));
+    if (lane == 0) sums[warp] = mine;
+    __syncthreads();
+    int before = 0, all = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (t + i < T && (label ? label[t + i] >= 0 : count[t + i] > 0)) has |= 1u << i;
-        const int mine = __popc(has);
-        int upto = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int v = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += v;
-        }
-        if (lane == 31) sums[warp] = upto;
-        __syncthreads();
-        int before = 0, all = 0;
-#pragma unroll
-        for (int w = 0; w < 32; ++w) {
-            before += w < warp ? sums[w] : 0;
-            all += sums[w];
-        }
-        int at = base + before + upto - mine;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (t + i < T) {
-                const bool h = has >> i & 1;
-                row[t + i] = h ? at : -1;
-                if (h) token[at++] = t + i;
-            }
-        base += all;
-        __syncthreads();
+    for (int w = 0; w < 32; ++w) {
+        before += w < warp ? sums[w] : 0;
+        all += sums[w];
     }
-    if (threadIdx.x == 0) *n = base;
+    if (threadIdx.x == 0) total = all;
+    cluster_sync();
+    int whole = 0;
+    for (int c = 0; c < kScanCtas; ++c) {
+        int v;
+        asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(map_shared(smem_addr(&total), (uint32_t)c)));
+        if (c < rank) before += v;
+        whole += v;
+    }
+    for (int p = p0; p < p1; p += 32) {
+        const bool h = has(p + lane);
+        const uint32_t who = __ballot_sync(0xffffffffu, h);
+        const int at = before + __popc(who & ((1u << lane) - 1));
+        if (p + lane < p1) row[p + lane] = h ? at : -1;
+        if (h) token[at] = p + lane;
+        before += __popc(who);
+    }
+    if (rank == 0 && threadIdx.x == 0) *n = whole;
+    cluster_sync();   // no CTA leaves while another reads its total
 }
 
 // ---- operands with 16-byte rows --------------------------------------------------------------------
@@ -328,6 +330,7 @@ struct Plan {
     float *weight, *ent, *bad, *zt, *dxs, *dws;
     float2 *stat;
     __nv_bfloat16 *xp, *wp, *dz;
+    float *few;
 };
 
 int64_t piece_words(const Shape &s, const Plan &p, int i) { return std::min(p.vc, s.V - i * p.vc); }
@@ -354,6 +357,13 @@ Plan make_plan(const Shape &s, void *ws)
         p.ent = w.take<float>(s.T);
         p.bad = w.take<float>(s.T);
         p.count = w.take<int32_t>(s.T);
+    }
+    if (few_tokens(s.T, s.d, s.split == 3 ? 4 : 2, s.bwd)) {   // (the other path's buffers are not used)
+        p.stat = w.take<float2>(kFewSlots * s.T);
+        p.zt = w.take<float>(kFewSlots * s.T);
+        if (s.bwd) p.few = w.take<float>(kFewSlots * s.T * p.dp);
+        p.bytes = w.used;
+        return p;
     }
     p.xp = w.take<__nv_bfloat16>(s.split * p.tp * p.dp);
     if (s.pack_w) p.wp = w.take<__nv_bfloat16>(s.split * p.vc * p.dp);
@@ -443,11 +453,25 @@ template <typename E, int SPLIT> void run_loss(Run &r, const Shape &s, const Pla
         if (d.teacher_dtype == RESBM_F32) go(k_targets<float>, static_cast<const float *>(a.teacher));
         else go(k_targets<__nv_bfloat16>, static_cast<const __nv_bfloat16 *>(a.teacher));
     }
+    auto join = [&](const int32_t *row, int slots, int64_t tp) {
+        JoinArgs j{p.stat, p.zt, slots, tp, row, p.count, label, p.ent, T, V, kLog2e / tau, tau, a.loss, a.lse_out};
+        if (T < 1024) r.go(k_join<1>, dim3((unsigned)T), dim3(256), 0, 1, j);
+        else r.go(k_join<32>, dim3((unsigned)((T + 31) / 32)), dim3(256), 0, 1, j);
+    };
+    if (few_tokens(T, s.d, sizeof(E), s.bwd)) {
+        FewArgs f{s.bwd, a.X, a.W, d.ldx, d.ldw, V, (int)T, (int)s.d, (int)p.dp, label, p.list, p.count, p.weight, p.bad, (int)s.K, kLog2e / tau, tau,
+                  p.stat, p.zt, T, a.lse, a.dloss, d.dloss_each, a.dX, a.dW, p.few};
+        int launches = 0;
+        if (r.e == cudaSuccess) r.e = few_run(f, F32, c, &launches);
+        r.launches += launches;
+        if (!s.bwd) join(nullptr, few_slots(V, false, c.sm_count), T);
+        return;
+    }
     const bool x_fits = al16(a.X) && d.ldx * (int64_t)sizeof(E) % 16 == 0;
     // one row block: the tokens without a target cost nothing more (but their rows must not enter dW)
     const bool direct = !s.bwd && !F32 && x_fits && T <= 256;
     if (!direct) {
-        r.go(k_scan, dim3(1), dim3(1024), 0, 1, label, p.count, (int)T, p.n, p.token, p.row);
+        r.go(k_scan, dim3(kScanCtas), dim3(1024), 0, 1, label, p.count, (int)T, p.n, p.token, p.row);
         r.go(k_pack<E, SPLIT>, dim3(row_grid(c, p.tp, 8)), dim3(256), 0, 1, static_cast<const E *>(a.X), d.ldx, x_fits, p.token, p.n, 0, (int)s.d,
              (int)p.dp, p.xp, p.tp * p.dp);
     }
@@ -563,9 +587,7 @@ template <typename E, int SPLIT> void run_loss(Run &r, const Shape &s, const Pla
                  static_cast<const int32_t *>(p.row), T, (int)s.d, static_cast<E *>(a.dX), al16(a.dX) && s.d * (int64_t)sizeof(E) % 16 == 0);
         return;
     }
-    JoinArgs j{p.stat, p.zt, p.slots, p.tp, direct ? nullptr : p.row, p.count, label, p.ent, T, V, g.c, tau, a.loss, a.lse_out};
-    if (T < 1024) r.go(k_join<1>, dim3((unsigned)T), dim3(256), 0, 1, j);
-    else r.go(k_join<32>, dim3((unsigned)((T + 31) / 32)), dim3(256), 0, 1, j);
+    join(direct ? nullptr : p.row, p.slots, p.tp);
 }
 
 // ---- checks --------------------------------------------------------------------------------------------
@@ -657,7 +679,7 @@ resbm_status resbm_vocab_workspace_bytes(const resbm_vocab_desc *desc, int op, s
     const bool distill = op == RESBM_VOCAB_DISTILL_FWD || op == RESBM_VOCAB_DISTILL_BWD;
     const resbm_status st = check_shape(desc, distill);
     if (st != RESBM_OK) return st;
-    *bytes = op == RESBM_VOCAB_EMBED_BWD ? embed_bwd_ws_bytes(desc->T, desc->V, desc->d)
+    *bytes = op == RESBM_VOCAB_EMBED_BWD ? embed_bwd_ws_bytes(desc->T, desc->d)
                                          : plan_bytes(shape_of(*desc, distill, op == RESBM_VOCAB_CE_BWD || op == RESBM_VOCAB_DISTILL_BWD));
     return RESBM_OK;
 }

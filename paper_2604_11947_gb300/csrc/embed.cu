@@ -16,13 +16,15 @@
 namespace resbm {
 namespace {
 
-// VEC columns of a row (16 bytes, or one element off the 16-byte grid) as fp32
-template <typename E, int VEC> struct Cols {
+// A thread's columns of a row as fp32: VEC neighbours (16 bytes), or off the 16-byte grid (STEP > 0) VEC single ones STEP apart
+template <typename E, int VEC, int STEP> struct Cols {
     float x[VEC];
-    __device__ __forceinline__ void load(const E *p)
+    // left: columns from p on that exist
+    __device__ __forceinline__ void load(const E *p, int64_t left)
     {
-        if constexpr (VEC == 1) {
-            x[0] = to_f32(__ldg(p));
+        if constexpr (STEP > 0) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) x[i] = i * STEP < left ? to_f32(__ldg(p + i * STEP)) : 0.0f;
         } else {
             const uint4 u = __ldg(reinterpret_cast<const uint4 *>(p));
             const uint32_t w[4] = {u.x, u.y, u.z, u.w};
@@ -37,10 +39,12 @@ template <typename E, int VEC> struct Cols {
             }
         }
     }
-    __device__ __forceinline__ void store(E *p, float scale) const
+    __device__ __forceinline__ void store(E *p, int64_t left, float scale) const
     {
-        if constexpr (VEC == 1) {
-            *p = from_f32<E>(x[0] * scale);
+        if constexpr (STEP > 0) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                if (i * STEP < left) p[i * STEP] = from_f32<E>(x[i] * scale);
         } else {
             uint32_t w[4];
 #pragma unroll
@@ -55,6 +59,18 @@ template <typename E, int VEC> struct Cols {
             *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
         }
     }
+    // fp32 partial sums (rows of any alignment)
+    __device__ __forceinline__ void put(float *p, int64_t left) const
+    {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i)
+            if (STEP == 0 || i * STEP < left) p[STEP ? i * STEP : i] = x[i];
+    }
+    __device__ __forceinline__ void get(const float *p, int64_t left)
+    {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) x[i] = STEP == 0 || i * STEP < left ? p[STEP ? i * STEP : i] : 0.0f;
+    }
     __device__ __forceinline__ void fill(float v)
     {
 #pragma unroll
@@ -67,31 +83,39 @@ template <typename E, int VEC> struct Cols {
     }
 };
 
+// The columns of a thread: 2^log_tx threads along a row, those of blockIdx.y
+template <int VEC, int STEP> __device__ __forceinline__ int64_t first_col(int log_tx)
+{
+    const int x = threadIdx.x & ((1 << log_tx) - 1);
+    if (STEP) return (int64_t)blockIdx.y * (VEC * STEP) + x;   // (STEP threads along a row)
+    return (((int64_t)blockIdx.y << log_tx) + x) * VEC;
+}
+
 // ---- forward -----------------------------------------------------------------------------------------
 // 2^log_tx threads along a row, 256 >> log_tx rows a CTA at a time, four rows in flight a thread
-template <typename E, int VEC>
+template <typename E, int VEC, int STEP>
 __global__ void __launch_bounds__(256) k_embed_fwd(const int64_t *__restrict__ ids, const E *__restrict__ table, int64_t ldt, E *__restrict__ out,
                                                    int64_t ldo, int64_t T, int64_t V, int64_t d, float scale, int log_tx)
 {
     griddep_wait();
     griddep_launch_dependents();
-    const int64_t col = (((int64_t)blockIdx.y << log_tx) + (threadIdx.x & ((1 << log_tx) - 1))) * VEC;
-    if (col >= d) return;
+    const int64_t col = first_col<VEC, STEP>(log_tx), left = d - col;
+    if (left <= 0) return;
     const int rows = 256 >> log_tx;
     const int64_t step = (int64_t)gridDim.x * rows;
     for (int64_t t = (int64_t)blockIdx.x * rows + (threadIdx.x >> log_tx); t < T; t += 4 * step) {
         int64_t id[4];
-        Cols<E, VEC> v[4];
+        Cols<E, VEC, STEP> v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) id[i] = t + i * step < T ? ids[t + i * step] : -1;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            if (id[i] >= 0 && id[i] < V) v[i].load(table + id[i] * ldt + col);
+            if (id[i] >= 0 && id[i] < V) v[i].load(table + id[i] * ldt + col, left);
             else v[i].fill(NAN);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (t + i * step < T) v[i].store(out + (t + i * step) * ldo + col, scale);
+            if (t + i * step < T) v[i].store(out + (t + i * step) * ldo + col, left, scale);
     }
 }
 
@@ -107,18 +131,30 @@ constexpr int kSortCtas = 8, kSortThreads = 1024, kMaxBins = 512;
 __global__ void __cluster_dims__(kSortCtas) __launch_bounds__(kSortThreads, 1)
     k_sort(const int64_t *__restrict__ ids, int T, int V, int64_t padding, int passes, int bits, int32_t *keys, int32_t *vals, uint8_t *dtable, int64_t bytes)
 {
-    extern __shared__ int32_t cnt[];   // 32 warps x bins: counts, then places
+    extern __shared__ __align__(128) int32_t cnt[];   // 32 warps x bins: counts, then places
     __shared__ int32_t total[kMaxBins], wsum[32];
     griddep_wait();
     griddep_launch_dependents();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tid = threadIdx.x;
     if (cluster_index() > 0) {
-        const int64_t head = min((int64_t)((16 - (reinterpret_cast<uintptr_t>(dtable) & 15)) & 15), bytes), vecs = (bytes - head) / 16;
-        uint4 *v = reinterpret_cast<uint4 *>(dtable + head);
-        const int64_t at = (int64_t)(blockIdx.x - kSortCtas) * kSortThreads + tid, step = (int64_t)(gridDim.x - kSortCtas) * kSortThreads;
-        for (int64_t i = at; i < vecs; i += step) v[i] = make_uint4(0u, 0u, 0u, 0u);
-        if (at < head) dtable[at] = 0;
-        if (at < bytes - head - 16 * vecs) dtable[head + 16 * vecs + at] = 0;
+        // (bulk copies out of shared memory: plain 16-byte stores of these CTAs reached 4.6 TB/s)
+        constexpr int64_t chunk = 32768;
+        const int64_t head = min((int64_t)((16 - (reinterpret_cast<uintptr_t>(dtable) & 15)) & 15), bytes), body = (bytes - head) / 16 * 16;
+        const int64_t first = blockIdx.x - kSortCtas, step = gridDim.x - kSortCtas;
+        for (int i = tid; i < chunk / 16; i += kSortThreads) reinterpret_cast<uint4 *>(cnt)[i] = make_uint4(0u, 0u, 0u, 0u);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncthreads();
+        if (tid == 0) {
+            for (int64_t at = first * chunk; at < body; at += step * chunk) {
+                const uint32_t size = (uint32_t)(body - at < chunk ? body - at : chunk);
+                asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dtable + head + at), "r"(smem_addr(cnt)), "r"(size) : "memory");
+                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                asm volatile("cp.async.bulk.wait_group.read 4;" ::: "memory");
+            }
+            asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        }
+        if (first == 0 && tid >= 32 && tid < 32 + head) dtable[tid - 32] = 0;
+        if (first == 0 && tid >= 64 && tid < 64 + bytes - head - body) dtable[head + body + tid - 64] = 0;
         return;
     }
     const int rank = (int)cluster_rank(), bins = 1 << bits;
@@ -212,52 +248,47 @@ struct SumArgs {
 // Blocks of kRun sorted positions, 2^log_tx threads along a row, which add the rows of each word up in order, sixteen in
 // flight. A word whose tokens all lie in the block is finished; the block's first and last runs may be pieces of longer ones, and
 // leave a partial sum (k_embed_join). So the work is even whatever the ids are.
-template <typename E, int VEC> __global__ void __launch_bounds__(256) k_embed_sum(const SumArgs a)
+template <typename E, int VEC, int STEP> __global__ void __launch_bounds__(256) k_embed_sum(const SumArgs a)
 {
     griddep_wait();
     griddep_launch_dependents();
-    const int per_cta = 256 >> a.log_tx;
-    const int b = blockIdx.x * per_cta + (threadIdx.x >> a.log_tx);
-    const int64_t col = (((int64_t)blockIdx.y << a.log_tx) + (threadIdx.x & ((1 << a.log_tx) - 1))) * VEC;
-    const int64_t p0 = (int64_t)b * kRun;
-    if (col >= a.d || p0 >= a.T) return;
+    const int lane = threadIdx.x & 31;
+    const int64_t b = (int64_t)blockIdx.x * (256 >> a.log_tx) + (threadIdx.x >> a.log_tx);   // (the same for a warp)
+    const int64_t col = first_col<VEC, STEP>(a.log_tx), left = a.d - col;
+    const int64_t p0 = b * kRun;
+    if (p0 >= a.T) return;
     const int len = a.T - p0 < kRun ? (int)(a.T - p0) : kRun;
-    const int32_t *key = a.keys + p0, *val = a.vals + p0;
-    const bool head = b > 0 && key[-1] == key[0];                        // the first run began before
-    const bool tail = p0 + len < a.T && key[len] == key[len - 1];        // the last one goes on
+    // the block's keys and tokens, one a lane
+    const int32_t k = lane < len ? a.keys[p0 + lane] : a.V, tok = lane < len ? a.vals[p0 + lane] : 0;
+    const int32_t before = p0 > 0 ? a.keys[p0 - 1] : -1, after = p0 + len < a.T ? a.keys[p0 + len] : -1;
+    const bool head = __shfl_sync(0xffffffffu, k, 0) == before;          // the first run began before
+    const bool tail = __shfl_sync(0xffffffffu, k, len - 1) == after;     // the last one goes on
+    const int used = __popc(__ballot_sync(0xffffffffu, k < a.V));        // (keys ascend)
     const E *dout = static_cast<const E *>(a.dout) + col;
-    float *part = a.part + (int64_t)b * 2 * a.d + col;
-    constexpr int F = VEC == 1 ? 16 : 8;   // rows in flight
-    Cols<E, VEC> sum;
+    float *part = a.part + b * 2 * a.d + col;
+    constexpr int F = STEP ? 4 : 8;   // rows in flight
+    Cols<E, VEC, STEP> sum;
     sum.fill(0.0f);
     bool first_run = true;
 #pragma unroll 1
-    for (int i = 0; i < len; i += F) {
-        Cols<E, VEC> v[F];
-        int32_t ks[F + 1], at[F];
+    for (int i = 0; i < used; i += F) {
+        Cols<E, VEC, STEP> v[F];
 #pragma unroll
         for (int j = 0; j < F; ++j) {
-            ks[j] = i + j < len ? key[i + j] : a.V;
-            at[j] = i + j < len ? val[i + j] : 0;
+            const int32_t t = __shfl_sync(0xffffffffu, tok, (i + j) & 31);
+            if (i + j < used && left > 0) v[j].load(dout + (int64_t)t * a.ldo, left);
         }
-        ks[F] = i + F < len ? key[i + F] : INT32_MAX;
-        if (ks[0] >= a.V) break;
-#pragma unroll
-        for (int j = 0; j < F; ++j)
-            if (ks[j] < a.V) v[j].load(dout + (int64_t)at[j] * a.ldo);
 #pragma unroll
         for (int j = 0; j < F; ++j) {
-            if (ks[j] >= a.V) break;
+            const int32_t kj = __shfl_sync(0xffffffffu, k, (i + j) & 31), kn = __shfl_sync(0xffffffffu, k, (i + j + 1) & 31);
+            if (i + j >= used) continue;
             sum.add(v[j]);
             const bool end = i + j + 1 == len;
-            if (!end && ks[j + 1] == ks[j]) continue;
+            if (!end && kn == kj) continue;
             // a run ends here, or the block does
-            if ((first_run && head) || (end && tail)) {
-                float *dst = part + (first_run && head ? 0 : a.d);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) dst[e] = sum.x[e];
-            } else {
-                sum.store(static_cast<E *>(a.dtable) + (int64_t)ks[j] * a.d + col, a.scale);
+            if (left > 0) {
+                if ((first_run && head) || (end && tail)) sum.put(part + (first_run && head ? 0 : a.d), left);
+                else sum.store(static_cast<E *>(a.dtable) + (int64_t)kj * a.d + col, left, a.scale);
             }
             sum.fill(0.0f);
             first_run = false;
@@ -266,50 +297,56 @@ template <typename E, int VEC> __global__ void __launch_bounds__(256) k_embed_su
 }
 
 // Words whose tokens span blocks: the partial sums in order, by the threads of the block where the word begins
-template <typename E, int VEC> __global__ void __launch_bounds__(256) k_embed_join(const SumArgs a)
+template <typename E, int VEC, int STEP> __global__ void __launch_bounds__(256) k_embed_join(const SumArgs a)
 {
     griddep_wait();
     griddep_launch_dependents();
-    const int per_cta = 256 >> a.log_tx;
-    const int64_t b = (int64_t)blockIdx.x * per_cta + (threadIdx.x >> a.log_tx);
-    const int64_t col = (((int64_t)blockIdx.y << a.log_tx) + (threadIdx.x & ((1 << a.log_tx) - 1))) * VEC;
+    const int64_t b = (int64_t)blockIdx.x * (256 >> a.log_tx) + (threadIdx.x >> a.log_tx);
+    const int64_t col = first_col<VEC, STEP>(a.log_tx), left = a.d - col;
     const int64_t blocks = ((int64_t)a.T + kRun - 1) / kRun, p0 = b * kRun;
-    if (col >= a.d || b + 1 >= blocks) return;
-    const int32_t k = a.keys[p0 + kRun - 1];
-    if (k >= a.V || a.keys[p0 + kRun] != k || (b > 0 && a.keys[p0 - 1] == k)) return;
-    Cols<E, VEC> sum;
-    const float *tail = a.part + (b * 2 + 1) * a.d + col;
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) sum.x[e] = tail[e];
+    if (left <= 0 || b + 1 >= blocks) return;
+    const int32_t k = a.keys[p0 + kRun - 1], next = a.keys[p0 + kRun], prev = b > 0 ? a.keys[p0 - 1] : -1;
+    if (k >= a.V || next != k || prev == k) return;
+    Cols<E, VEC, STEP> sum;
+    sum.get(a.part + (b * 2 + 1) * a.d + col, left);
+    constexpr int F = 8;
     bool more = true;
-    for (int64_t i = b + 1; more && i < blocks; i += 8) {   // (a block that has none of the word has no partial sum: loaded, not used)
-        float x[8][VEC];
-        bool has[8];
+    for (int64_t i = b + 1; more && i < blocks; i += F) {   // (a block that has none of the word has no partial sum: loaded, not used)
+        Cols<E, VEC, STEP> x[F];
+        bool has[F];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < F; ++j) {
             const int64_t at = i + j < blocks ? i + j : blocks - 1;
             has[j] = i + j < blocks && a.keys[at * kRun] == k;
-            const float *head = a.part + at * 2 * a.d + col;
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) x[j][e] = head[e];
+            x[j].get(a.part + at * 2 * a.d + col, left);
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (has[j]) {
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) sum.x[e] += x[j][e];
-            }
-        more = has[7];
+        for (int j = 0; j < F; ++j)
+            if (has[j]) sum.add(x[j]);
+        more = has[F - 1];
     }
-    sum.store(static_cast<E *>(a.dtable) + (int64_t)k * a.d + col, a.scale);
+    sum.store(static_cast<E *>(a.dtable) + (int64_t)k * a.d + col, left, a.scale);
 }
 
-// threads along a row: a power of two, up to 256
-int log_threads(int64_t vectors)
+// How threads cover a row: whole vectors, 2^log threads along it (32 at least: a warp's threads share their rows), or four
+// single columns a thread, 256 apart, or 32 apart in rows of up to 128
+struct Cover {
+    int log_tx;
+    unsigned cols;   // CTAs along a row
+};
+template <int V16> Cover cover(int64_t d, bool vec, int least)
 {
-    int log = 0;
-    while (log < 8 && (int64_t(1) << log) < vectors) ++log;
-    return log;
+    Cover c;
+    if (!vec) {
+        c.log_tx = d <= 128 ? 5 : 8;
+        c.cols = (unsigned)((d + (4 << c.log_tx) - 1) >> (c.log_tx + 2));
+        return c;
+    }
+    const int64_t n = d / V16;
+    c.log_tx = least;
+    while (c.log_tx < 8 && (int64_t(1) << c.log_tx) < n) ++c.log_tx;
+    c.cols = (unsigned)((n + (int64_t(1) << c.log_tx) - 1) >> c.log_tx);
+    return c;
 }
 
 struct EmbedWs {
@@ -349,14 +386,13 @@ template <typename E> cudaError_t run_fwd(const resbm_embed_desc &d, const int64
 {
     constexpr int V16 = 16 / (int)sizeof(E);
     const bool vec = d.d % V16 == 0 && al16(table) && al16(out) && (d.V == 1 || d.ldt % V16 == 0) && (d.T == 1 || d.ldo % V16 == 0);
-    const int64_t n = vec ? d.d / V16 : d.d;
-    const int log_tx = log_threads(n);
-    const int64_t rows = 256 >> log_tx, ctas = (d.T + rows - 1) / rows, cols = (n + (int64_t(1) << log_tx) - 1) >> log_tx;
-    const dim3 grid((unsigned)std::min<int64_t>(ctas, std::max<int64_t>(1, 16 * c.sm_count / cols)), (unsigned)cols);
+    const Cover v = cover<V16>(d.d, vec, 0);
+    const int64_t rows = 256 >> v.log_tx, ctas = (d.T + rows - 1) / rows;
+    const dim3 grid((unsigned)std::min<int64_t>(ctas, std::max<int64_t>(1, 16 * c.sm_count / (int64_t)v.cols)), v.cols);
     auto go = [&](auto kernel) {
-        return launch(kernel, grid, dim3(256), 0, c.stream, ids, static_cast<const E *>(table), d.ldt, static_cast<E *>(out), d.ldo, d.T, d.V, d.d, d.scale, log_tx);
+        return launch(kernel, grid, dim3(256), 0, c.stream, ids, static_cast<const E *>(table), d.ldt, static_cast<E *>(out), d.ldo, d.T, d.V, d.d, d.scale, v.log_tx);
     };
-    return vec ? go(k_embed_fwd<E, V16>) : go(k_embed_fwd<E, 1>);
+    return vec ? go(k_embed_fwd<E, V16, 0>) : v.log_tx == 5 ? go(k_embed_fwd<E, 4, 32>) : go(k_embed_fwd<E, 4, 256>);
 }
 
 template <typename E> cudaError_t run_bwd(const resbm_embed_desc &d, const int64_t *ids, const void *dout, void *dtable, const EmbedWs &w, const Ctx &c)
@@ -365,7 +401,7 @@ template <typename E> cudaError_t run_bwd(const resbm_embed_desc &d, const int64
     int width = 1;
     while (width < 31 && (int64_t(1) << width) <= d.V) ++width;
     const int passes = (width + 8) / 9, bits = (width + passes - 1) / passes;
-    const uint32_t smem = 32u * 4u << bits;
+    const uint32_t smem = std::max(32768u, 32u * 4u << bits);   // (the zeros: 32 KB)
     static std::atomic<uint8_t> done[kMaxDev];
     cudaError_t e = ensure_smem(k_sort, 32 * 4 * kMaxBins, c.device, done);
     // (the cluster's size is the kernel's own)
@@ -378,18 +414,17 @@ template <typename E> cudaError_t run_bwd(const resbm_embed_desc &d, const int64
     if (e != cudaSuccess) return e;
     constexpr int V16 = 16 / (int)sizeof(E);
     const bool vec = d.d % V16 == 0 && al16(dout) && al16(dtable) && (d.T == 1 || d.ldo % V16 == 0);
-    const int64_t n = vec ? d.d / V16 : d.d;
-    const int log_tx = log_threads(n);
-    const int64_t per = 256 >> log_tx, blocks = (d.T + kRun - 1) / kRun, cols = (n + (int64_t(1) << log_tx) - 1) >> log_tx;
-    SumArgs a{w.keys + ((passes - 1) & 1) * d.T, w.vals + ((passes - 1) & 1) * d.T, dout, dtable, w.part, d.ldo, d.d, (int)d.T, (int)d.V,
-              log_tx, d.scale};
-    const dim3 ctas((unsigned)((blocks + per - 1) / per), (unsigned)cols);
+    const Cover v = cover<V16>(d.d, vec, 5);
+    const int64_t per = 256 >> v.log_tx, blocks = (d.T + kRun - 1) / kRun;
+    SumArgs a{w.keys + ((passes - 1) & 1) * d.T, w.vals + ((passes - 1) & 1) * d.T, dout, dtable, w.part, d.ldo, d.d, (int)d.T, (int)d.V, v.log_tx, d.scale};
+    const dim3 ctas((unsigned)((blocks + per - 1) / per), v.cols);
     auto go = [&](auto sum, auto join) {
         cudaError_t e = launch(sum, ctas, dim3(256), 0, c.stream, a);
         if (e == cudaSuccess && blocks > 1) e = launch(join, ctas, dim3(256), 0, c.stream, a);
         return e;
     };
-    e = vec ? go(k_embed_sum<E, V16>, k_embed_join<E, V16>) : go(k_embed_sum<E, 1>, k_embed_join<E, 1>);
+    e = vec ? go(k_embed_sum<E, V16, 0>, k_embed_join<E, V16, 0>)
+        : v.log_tx == 5 ? go(k_embed_sum<E, 4, 32>, k_embed_join<E, 4, 32>) : go(k_embed_sum<E, 4, 256>, k_embed_join<E, 4, 256>);
     if (e == cudaSuccess) count_launches(blocks > 1 ? 3 : 2);
     return e;
 }

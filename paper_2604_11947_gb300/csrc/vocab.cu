@@ -242,39 +242,51 @@ template <int TX> __global__ void __launch_bounds__(256) k_join(const JoinArgs a
 }
 
 // ---- rows of fp32 slots, summed in order and rounded -----------------------------------------------
-// out[t] = the sum of the slots' rows row[t] (or t), zeros where that is negative or there are no slots. A warp a row.
-template <typename E>
-__global__ void __launch_bounds__(256) k_finish(const float *__restrict__ slot, int slots, int64_t stride, int dp,
-                                                const int32_t *__restrict__ row, int64_t T, int d, E *__restrict__ out, bool vec)
+// out[t] = the sum of the slots' rows row[t] (or t), zeros where that is negative or there are no slots. Eight columns a thread;
+// up to two matrices in a launch.
+struct FinishJob {
+    const float *slot;
+    int slots;
+    int64_t stride;
+    const int32_t *row;
+    int64_t T;
+    void *out;
+    bool vec;
+};
+template <typename E> __global__ void __launch_bounds__(256) k_finish(const FinishJob j0, const FinishJob j1, int d, int dp)
 {
     griddep_wait();
     griddep_launch_dependents();
-    const int lane = threadIdx.x & 31;
-    for (int64_t t = blockIdx.x * (int64_t)8 + (threadIdx.x >> 5); t < T; t += (int64_t)gridDim.x * 8) {
-        const int64_t r = row ? row[t] : t;
-        const int count = r < 0 ? 0 : slots;
-        E *dst = out + t * d;
-        for (int c = lane * 8; c < d; c += 256) {
-            float x[8] = {};
-            for (int s = 0; s < count; ++s) {
-                const float4 *p = reinterpret_cast<const float4 *>(slot + s * stride + r * dp + c);
-                const float4 a = p[0], b = p[1];
-                x[0] += a.x; x[1] += a.y; x[2] += a.z; x[3] += a.w;
-                x[4] += b.x; x[5] += b.y; x[6] += b.z; x[7] += b.w;
-            }
-            if (vec && c + 8 <= d) {
-                if constexpr (sizeof(E) == 2) {
-                    *reinterpret_cast<uint4 *>(dst + c) =
-                        make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
-                } else {
-                    *reinterpret_cast<float4 *>(dst + c) = make_float4(x[0], x[1], x[2], x[3]);
-                    *reinterpret_cast<float4 *>(dst + c + 4) = make_float4(x[4], x[5], x[6], x[7]);
-                }
+    const FinishJob &j = blockIdx.y ? j1 : j0;
+    const int per = (d + 7) / 8;
+    const int64_t vectors = j.T * per;
+    for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < vectors; i += (int64_t)gridDim.x * 256) {
+        const int64_t t = i / per;
+        const int c = (int)(i - t * per) * 8;
+        const int64_t r = j.row ? j.row[t] : t;
+        const int count = r < 0 ? 0 : j.slots;
+        const float *src = j.slot + r * dp + c;
+        float x[8] = {};
+#pragma unroll 4
+        for (int s = 0; s < count; ++s) {
+            const float4 *p = reinterpret_cast<const float4 *>(src + s * j.stride);
+            const float4 a = p[0], b = p[1];
+            x[0] += a.x; x[1] += a.y; x[2] += a.z; x[3] += a.w;
+            x[4] += b.x; x[5] += b.y; x[6] += b.z; x[7] += b.w;
+        }
+        E *dst = static_cast<E *>(j.out) + t * d + c;
+        if (j.vec && c + 8 <= d) {
+            if constexpr (sizeof(E) == 2) {
+                *reinterpret_cast<uint4 *>(dst) =
+                    make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
             } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (c + i < d) dst[c + i] = from_f32<E>(x[i]);
+                *reinterpret_cast<float4 *>(dst) = make_float4(x[0], x[1], x[2], x[3]);
+                *reinterpret_cast<float4 *>(dst + 4) = make_float4(x[4], x[5], x[6], x[7]);
             }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (c + k < d) dst[k] = from_f32<E>(x[k]);
         }
     }
 }
@@ -330,20 +342,23 @@ struct Plan {
     float *weight, *ent, *bad, *zt, *dxs, *dws;
     float2 *stat;
     __nv_bfloat16 *xp, *wp, *dz;
-    float *few;
 };
 
 int64_t piece_words(const Shape &s, const Plan &p, int i) { return std::min(p.vc, s.V - i * p.vc); }
+
+// Whether a W of dense rows goes through the workspace. (Rows of whole 16 bytes that straddle 128-byte lines do not: with V = 30011,
+// d = 1000 the copy cost more than it gave up to T = 4096, 153 against 164 us forward, and nothing at 8192.)
+bool packs_w(const Shape &s) { return s.split == 3 || s.d % 8 != 0; }
 
 Plan make_plan(const Shape &s, void *ws)
 {
     Plan p = {};
     p.tp = std::max<int64_t>(up(s.T, 256), 256);
-    p.dp = up(s.d, 8);
+    p.dp = up(s.d, 64);   // (whole 128-byte lines: rows that straddle them load at half the rate)
     // dz of a piece: 2^27 elements (268 MB in bf16), but no fewer than 4096 words
     int64_t vc = up(s.V, 256);
     if (s.bwd) vc = std::min(vc, std::max(kPackRows, (int64_t(1) << (s.split == 3 ? 26 : 27)) / p.tp / 256 * 256));
-    if (s.pack_w) vc = std::min(vc, std::max(kPackRows, s.split == 1 && s.d % 8 == 0 ? 0 : (int64_t(1) << 26) / p.dp / 256 * 256));
+    if (s.pack_w) vc = std::min(vc, std::max(kPackRows, packs_w(s) ? (int64_t(1) << 26) / p.dp / 256 * 256 : 0));
     p.pieces = (int)((s.V + vc - 1) / vc);
     p.vc = up((s.V + p.pieces - 1) / p.pieces, 256);
     p.pieces = (int)((s.V + p.vc - 1) / p.vc);
@@ -357,13 +372,6 @@ Plan make_plan(const Shape &s, void *ws)
         p.ent = w.take<float>(s.T);
         p.bad = w.take<float>(s.T);
         p.count = w.take<int32_t>(s.T);
-    }
-    if (few_tokens(s.T, s.d, s.split == 3 ? 4 : 2, s.bwd)) {   // (the other path's buffers are not used)
-        p.stat = w.take<float2>(kFewSlots * s.T);
-        p.zt = w.take<float>(kFewSlots * s.T);
-        if (s.bwd) p.few = w.take<float>(kFewSlots * s.T * p.dp);
-        p.bytes = w.used;
-        return p;
     }
     p.xp = w.take<__nv_bfloat16>(s.split * p.tp * p.dp);
     if (s.pack_w) p.wp = w.take<__nv_bfloat16>(s.split * p.vc * p.dp);
@@ -387,7 +395,7 @@ size_t plan_bytes(Shape s)
 {
     s.pack_w = true;
     const size_t a = make_plan(s, nullptr).bytes;
-    s.pack_w = s.split == 3 || s.d % 8 != 0;
+    s.pack_w = packs_w(s);
     return std::max(a, make_plan(s, nullptr).bytes);
 }
 
@@ -409,14 +417,12 @@ struct Run {
     }
 };
 
-template <int MODE, int SPLIT, int PIECE>
-void run_gemm(Run &r, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &o, const VocabGemm &g, int64_t rows)
+template <int MODE, int SPLIT, int PIECE, int JOBS> void run_gemm(Run &r, const VocabJobs<JOBS> &jobs, int64_t units)
 {
     static std::atomic<uint8_t> done[kMaxDev];
-    if (r.e == cudaSuccess) r.e = ensure_smem(k_vocab_gemm<MODE, SPLIT, PIECE>, VocabCfg::SMEM, r.c.device, done);
-    const int64_t units = (rows + 255) / 256 * g.nn * g.splits, pairs = std::max(1, r.c.sm_count / 2);
-    if (units == 0) return;
-    r.go(k_vocab_gemm<MODE, SPLIT, PIECE>, dim3((unsigned)(2 * std::min(units, pairs))), dim3(VocabCfg::THREADS), VocabCfg::SMEM, 2, a, b, o, g);
+    if (r.e == cudaSuccess) r.e = ensure_smem(k_vocab_gemm<MODE, SPLIT, PIECE, JOBS>, VocabCfg::SMEM, r.c.device, done);
+    const int64_t pairs = std::max(1, r.c.sm_count / 2);
+    r.go(k_vocab_gemm<MODE, SPLIT, PIECE, JOBS>, dim3((unsigned)(2 * std::min(units, pairs))), dim3(VocabCfg::THREADS), VocabCfg::SMEM, 2, jobs);
 }
 
 unsigned row_grid(const Ctx &c, int64_t rows, int per) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>((rows + per - 1) / per, 16 * c.sm_count)); }
@@ -436,8 +442,9 @@ struct Call {
 template <typename E, int SPLIT> void run_loss(Run &r, const Shape &s, const Plan &p, const Call &a)
 {
     constexpr bool F32 = SPLIT == 3;
-    // slices of a piece of a sum: 256 deep (128 of three parts), which leaves the truncation of 16 MMAs (48)
-    constexpr int P = F32 ? 2 : 4;
+    // Slices of a piece of a sum: 512 deep (128 of three parts), which leaves the truncation of 32 MMAs (48). T = 777, V = 50001,
+    // d = 1000: losses 3.8e-7 off (256 deep 1.8e-7, 1024 8e-7); T = 16384, V = 32000, d = 2048: 1104 us (1194, 1090).
+    constexpr int P = F32 ? 2 : 8;
     const resbm_vocab_desc &d = *a.d;
     const int64_t T = s.T, V = s.V;
     const float tau = s.distill ? d.temperature : 1.0f;
@@ -458,15 +465,6 @@ template <typename E, int SPLIT> void run_loss(Run &r, const Shape &s, const Pla
         if (T < 1024) r.go(k_join<1>, dim3((unsigned)T), dim3(256), 0, 1, j);
         else r.go(k_join<32>, dim3((unsigned)((T + 31) / 32)), dim3(256), 0, 1, j);
     };
-    if (few_tokens(T, s.d, sizeof(E), s.bwd)) {
-        FewArgs f{s.bwd, a.X, a.W, d.ldx, d.ldw, V, (int)T, (int)s.d, (int)p.dp, label, p.list, p.count, p.weight, p.bad, (int)s.K, kLog2e / tau, tau,
-                  p.stat, p.zt, T, a.lse, a.dloss, d.dloss_each, a.dX, a.dW, p.few};
-        int launches = 0;
-        if (r.e == cudaSuccess) r.e = few_run(f, F32, c, &launches);
-        r.launches += launches;
-        if (!s.bwd) join(nullptr, few_slots(V, false, c.sm_count), T);
-        return;
-    }
     const bool x_fits = al16(a.X) && d.ldx * (int64_t)sizeof(E) % 16 == 0;
     // one row block: the tokens without a target cost nothing more (but their rows must not enter dW)
     const bool direct = !s.bwd && !F32 && x_fits && T <= 256;
@@ -484,6 +482,7 @@ template <typename E, int SPLIT> void run_loss(Run &r, const Shape &s, const Pla
     g.n_rows = (int)T;
     g.splits = 1;
     g.group = 8;
+    g.a_rows = T <= 120 ? (int)up(T, 8) : 128;
     g.a_off = (int)p.tp;
     g.b_off = (int)p.vc;
     g.token = direct ? nullptr : p.token;
@@ -513,7 +512,7 @@ template <typename E, int SPLIT> void run_loss(Run &r, const Shape &s, const Pla
             ldw = p.dp;
             w_rows = SPLIT * p.vc;
         }
-        CUtensorMap ma, mb, mo;
+        const int64_t row_blocks = (T + 255) / 256;
         // z = X . W^T
         const Units u = choose_units(T, vn, p.dp * (F32 ? 6 : 1), 1, 0);
         g.v0 = (int)v0;
@@ -522,32 +521,46 @@ template <typename E, int SPLIT> void run_loss(Run &r, const Shape &s, const Pla
         g.depth = (int)s.d;
         g.bn = u.bn;
         g.nn = u.nn;
-        r.map(&ma, x, s.d, x_rows, ldx * 2, 64, 128, k128);
-        r.map(&mb, w, s.d, w_rows, ldw * 2, 64, (uint32_t)u.bn / 2, k128);
+        g.slot_rows = (int)p.tp;
+        VocabJobs<1> z;
+        r.map(&z.a[0], x, s.d, x_rows, ldx * 2, 64, (uint32_t)g.a_rows, k128);
+        r.map(&z.b[0], w, s.d, w_rows, ldw * 2, 64, (uint32_t)u.bn / 2, k128);
+        z.o[0] = z.a[0];
+        z.g[0] = g;
         if (!s.bwd) {
-            run_gemm<VG_FWD, SPLIT, P>(r, ma, mb, ma, g, T);
+            run_gemm<VG_FWD, SPLIT, P, 1>(r, z, row_blocks * u.nn);
             g.slot0 += 2 * u.nn;
             continue;
         }
-        r.map(&mo, p.dz, vn, SPLIT * p.tp, p.vc * 2, 32, 32, k64);
-        g.slot_rows = (int)p.tp;
-        run_gemm<VG_DZ, SPLIT, F32 ? P : 0>(r, ma, mb, mo, g, T);
+        r.map(&z.o[0], p.dz, vn, SPLIT * p.tp, p.vc * 2, 32, 32, k64);
+        run_gemm<VG_DZ, SPLIT, F32 ? P : 0, 1>(r, z, row_blocks * u.nn);
+
+        VocabJobs<2> gr;
+        FinishJob fin[2] = {};
+        int jobs = 0, fins = 0;
+        int64_t units = 0, depth[2] = {};
         if (a.dX) {   // dz . W, added over the pieces
-            VocabGemm h = g;
+            VocabGemm &h = gr.g[jobs];
+            h = g;
+            h.mode = VG_DX;
             h.cols = (int)s.d;
             h.depth = (int)vn;
             h.bn = p.dx.bn;
             h.nn = p.dx.nn;
             h.splits = p.dx.splits;
-            h.slot_rows = (int)p.tp;
             h.add = i > 0;
-            r.map(&ma, p.dz, vn, SPLIT * p.tp, p.vc * 2, 64, 128, k128);
-            r.map(&mb, w, s.d, w_rows, ldw * 2, 64, 64, k128);
-            r.map(&mo, p.dxs, p.dp, h.splits * p.tp, p.dp * 4, 32, 32, k128, CU_TENSOR_MAP_DATA_TYPE_FLOAT32);
-            run_gemm<VG_DX, SPLIT, F32 ? P : 0>(r, ma, mb, mo, h, T);
+            r.map(&gr.a[jobs], p.dz, vn, SPLIT * p.tp, p.vc * 2, 64, (uint32_t)g.a_rows, k128);
+            r.map(&gr.b[jobs], w, s.d, w_rows, ldw * 2, 64, 64, k128);
+            r.map(&gr.o[jobs], p.dxs, p.dp, h.splits * p.tp, p.dp * 4, 32, 32, k128, CU_TENSOR_MAP_DATA_TYPE_FLOAT32);
+            depth[jobs++] = vn / h.splits;
+            units += row_blocks * h.nn * h.splits;
+            if (i + 1 == p.pieces)
+                fin[fins++] = FinishJob{p.dxs, h.splits, p.tp * p.dp, p.row, T, a.dX, al16(a.dX) && s.d * (int64_t)sizeof(E) % 16 == 0};
         }
         if (a.dW) {   // dz^T . X
-            VocabGemm h = g;
+            VocabGemm &h = gr.g[jobs];
+            h = g;
+            h.mode = VG_DW;
             h.rows = (int)vn;
             h.cols = (int)s.d;
             h.bn = p.dw.bn;
@@ -555,39 +568,53 @@ template <typename E, int SPLIT> void run_loss(Run &r, const Shape &s, const Pla
             h.splits = p.dw.splits;
             h.slot_rows = (int)p.vc;
             h.b_off = (int)p.tp;
+            h.b_y = 0;
             h.out_f32 = F32;
-            r.map(&ma, p.dz, vn, SPLIT * p.tp, p.vc * 2, 64, 64, k128);
-            r.map(&mb, p.xp, s.d, SPLIT * p.tp, p.dp * 2, 64, 64, k128);
+            r.map(&gr.a[jobs], p.dz, vn, SPLIT * p.tp, p.vc * 2, 64, 64, k128);
+            r.map(&gr.b[jobs], p.xp, s.d, SPLIT * p.tp, p.dp * 2, 64, 64, k128);
+            CUtensorMap *mo = &gr.o[jobs];
+            *mo = gr.a[jobs];
+            E *out = static_cast<E *>(a.dW) + v0 * s.d;
             if (h.splits > 1) {
                 h.out_f32 = 1;
-                r.map(&mo, p.dws, p.dp, h.splits * p.vc, p.dp * 4, 32, 32, k128, CU_TENSOR_MAP_DATA_TYPE_FLOAT32);
+                r.map(mo, p.dws, p.dp, h.splits * p.vc, p.dp * 4, 32, 32, k128, CU_TENSOR_MAP_DATA_TYPE_FLOAT32);
+                fin[fins++] = FinishJob{p.dws, h.splits, p.vc * p.dp, nullptr, vn, out, al16(out) && s.d * (int64_t)sizeof(E) % 16 == 0};
             } else {
                 h.out_y = (int)v0;
                 if (!al16(a.dW) || s.d * (int64_t)sizeof(E) % 16 != 0) {
                     h.out = a.dW;
                     h.ldo = s.d;
-                    mo = ma;
                 } else if (F32) {
-                    r.map(&mo, a.dW, s.d, V, s.d * 4, 32, 32, k128, CU_TENSOR_MAP_DATA_TYPE_FLOAT32);
+                    r.map(mo, a.dW, s.d, V, s.d * 4, 32, 32, k128, CU_TENSOR_MAP_DATA_TYPE_FLOAT32);
                 } else {
-                    r.map(&mo, a.dW, s.d, V, s.d * 2, 32, 32, k64);
+                    r.map(mo, a.dW, s.d, V, s.d * 2, 32, 32, k64);
                 }
             }
-            run_gemm<VG_DW, SPLIT, F32 ? P : 0>(r, ma, mb, mo, h, vn);
-            if (h.splits > 1) {
-                E *out = static_cast<E *>(a.dW) + v0 * s.d;
-                r.go(k_finish<E>, dim3(row_grid(c, vn, 8)), dim3(256), 0, 1, static_cast<const float *>(p.dws), h.splits, p.vc * p.dp, (int)p.dp,
-                     static_cast<const int32_t *>(nullptr), vn, (int)s.d, out, al16(out) && s.d * (int64_t)sizeof(E) % 16 == 0);
-            }
+            depth[jobs++] = T / h.splits;
+            units += (vn + 255) / 256 * h.nn * h.splits;
+        }
+        if (jobs < 2) {   // (only one of them is wanted: the other has no units)
+            gr.a[1] = gr.a[0];
+            gr.b[1] = gr.b[0];
+            gr.o[1] = gr.o[0];
+            gr.g[1] = gr.g[0];
+            gr.g[1].nn = 0;
+        } else if (depth[0] < depth[1]) {
+            std::swap(gr.a[0], gr.a[1]);
+            std::swap(gr.b[0], gr.b[1]);
+            std::swap(gr.o[0], gr.o[1]);
+            std::swap(gr.g[0], gr.g[1]);
+        }
+        run_gemm<VG_GRADS, SPLIT, F32 ? P : 0, 2>(r, gr, units);
+        if (fins) {
+            const int64_t most = std::max(fin[0].T, fin[1].T) * ((s.d + 7) / 8);
+            r.go(k_finish<E>, dim3(row_grid(c, most, 256), (unsigned)fins), dim3(256), 0, 1, fin[0], fin[1], (int)s.d, (int)p.dp);
         }
     }
-    if (s.bwd) {
-        if (a.dX)
-            r.go(k_finish<E>, dim3(row_grid(c, T, 8)), dim3(256), 0, 1, static_cast<const float *>(p.dxs), p.dx.splits, p.tp * p.dp, (int)p.dp,
-                 static_cast<const int32_t *>(p.row), T, (int)s.d, static_cast<E *>(a.dX), al16(a.dX) && s.d * (int64_t)sizeof(E) % 16 == 0);
-        return;
-    }
-    join(direct ? nullptr : p.row, p.slots, p.tp);
+    if (s.bwd) return;
+    JoinArgs j{p.stat, p.zt, p.slots, p.tp, direct ? nullptr : p.row, p.count, label, p.ent, T, V, g.c, tau, a.loss, a.lse_out};
+    if (T < 1024) r.go(k_join<1>, dim3((unsigned)T), dim3(256), 0, 1, j);
+    else r.go(k_join<32>, dim3((unsigned)((T + 31) / 32)), dim3(256), 0, 1, j);
 }
 
 // ---- checks --------------------------------------------------------------------------------------------

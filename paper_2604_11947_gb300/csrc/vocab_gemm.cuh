@@ -5,7 +5,7 @@
 //                                    targets' logits: 16 bytes a row and unit instead of the logits
 //   VG_DZ    z again, then           dz = g (softmax(z / tau) - q), stored for a piece of the vocabulary at a time
 //   VG_DX    dz . W                  fp32, added to what earlier pieces gave
-//   VG_DW    dz^T . X                complete for the piece's rows of W
+//   VG_DW    dz^T . X                complete for the piece's rows of W (in one launch with VG_DX)
 //
 // X: the n tokens that have a target, packed (n is on the device only); z and dz have a row for each of them.
 //
@@ -40,9 +40,10 @@
 namespace resbm {
 namespace tc {
 
-enum VocabMode : int { VG_FWD, VG_DZ, VG_DX, VG_DW };
+enum VocabMode : int { VG_FWD, VG_DZ, VG_DX, VG_DW, VG_GRADS };   // GRADS: units of DX and of DW in one launch
 
 struct VocabGemm {
+    int32_t mode;             // of VG_GRADS: VG_DX or VG_DW
     const int32_t *n_ptr;     // tokens in use: *n_ptr, or n_rows where it is null
     int32_t n_rows;
     int32_t rows;             // VG_DW: rows of the piece (words)
@@ -51,6 +52,7 @@ struct VocabGemm {
     int32_t bn, nn;           // columns a unit (a multiple of 32), units along the columns
     int32_t splits, group;
     int32_t a_off, b_off;     // rows from one of SPLIT's three operands to the next
+    int32_t a_rows;           // FWD, DZ, DX: rows of A a load: 128, or fewer where one load has all tokens
     int32_t b_y;              // FWD, DZ, DX: the piece's first row in B's tensor map
     int32_t out_y;            // DW: the piece's first row of dW
     int32_t slot_rows;        // DX, DW: rows of a slot
@@ -122,14 +124,13 @@ struct Targets {
         }
     }
     // those from column `first` of the tile that starts at word `base_` on
-    __device__ __forceinline__ void start(const VocabGemm &g, int64_t token, int base_, int first)
+    __device__ __forceinline__ void start(const VocabGemm &g, int64_t token, int64_t label, int base_, int first)
     {
         base = base_;
         if (g.label) {
-            const int64_t y = g.label[token];
             K = 0;
             q = 1.0f;
-            next = y >= (int64_t)base + first && y < g.V ? (int)(y - base) : INT_MAX;
+            next = label >= (int64_t)base + first && label < g.V ? (int)(label - base) : INT_MAX;
             return;
         }
         K = g.K;
@@ -155,14 +156,25 @@ struct Targets {
     }
 };
 
+// What a row's token brings along, loaded a unit ahead (three loads that wait for one another, 1500 cycles)
+struct RowIn {
+    int64_t token, label;
+    float lse, dloss, bad;
+};
+
 // MODE: what becomes of the accumulator; SPLIT: bf16 parts of an operand; PIECE: 64-deep slices of a piece of a sum (0: whole)
-template <int MODE, int SPLIT, int PIECE>
-__global__ void __launch_bounds__(VocabCfg::THREADS, 1)
-    k_vocab_gemm(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUtensorMap tmb,
-                 const __grid_constant__ CUtensorMap tmo, const VocabGemm g)
+// JOBS: 1, or the two of VG_GRADS, whose units follow one another (the one with the longer units first): apart, the last round of
+// each leaves pairs without work.
+template <int JOBS> struct VocabJobs {
+    CUtensorMap a[JOBS], b[JOBS], o[JOBS];
+    VocabGemm g[JOBS];
+};
+
+template <int MODE, int SPLIT, int PIECE, int JOBS = MODE == VG_GRADS ? 2 : 1>
+__global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __grid_constant__ VocabJobs<JOBS> jobs)
 {
     using C = VocabCfg;
-    constexpr bool AMN = MODE == VG_DW, BMN = MODE == VG_DX || MODE == VG_DW;
+    constexpr bool GRADS = MODE == VG_GRADS, BMN = GRADS;
     constexpr bool PIECES = PIECE > 0;
     constexpr int TERMS = SPLIT == 3 ? 6 : 1;
     extern __shared__ uint8_t smem_raw[];
@@ -194,43 +206,97 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1)
     const uint32_t tmem = tmem_base_sh;
 
     // the units, in every warp alike
-    const int n = g.n_ptr ? *g.n_ptr : g.n_rows;
-    const int rows = MODE == VG_DW ? g.rows : n;
-    const int depth = MODE == VG_DW ? n : g.depth;
-    const uint32_t nm = (uint32_t)((rows + 255) / 256), nn = (uint32_t)g.nn, per_split = nm * nn;
-    const uint32_t units = per_split * (uint32_t)g.splits;
-    const int slices = (depth + 63) / 64, per = (slices + g.splits - 1) / g.splits;
-    const uint32_t u_first = cluster_index(), u_step = gridDim.x / 2;
-    // unit -> its 128-row block of this CTA, column block, slices [k0, k0 + nk)
-    auto unit_of = [&](uint32_t u, int &mb, int &nb, int &ks, int &k0, int &nk) {
-        ks = (int)(u / per_split);
-        uint32_t r = u - (uint32_t)ks * per_split;
-        const uint32_t in_group = (uint32_t)g.group * nn, gi = r / in_group;
-        r -= gi * in_group;
-        const uint32_t left = nm - gi * (uint32_t)g.group, gr = left < (uint32_t)g.group ? left : (uint32_t)g.group;
-        nb = (int)(r / gr);
-        mb = 2 * (int)(gi * (uint32_t)g.group + r - (uint32_t)nb * gr) + (int)crank;
-        k0 = ks * per;
-        const int k1 = k0 + per < slices ? k0 + per : slices;
-        nk = k1 > k0 ? k1 - k0 : 0;
+    const int n = jobs.g[0].n_ptr ? *jobs.g[0].n_ptr : jobs.g[0].n_rows;
+    struct Job {
+        bool dw;
+        int rows, slices, per, nn;
+        uint32_t nm, per_split, units;
     };
-    const int half_b = g.bn / 2;   // this CTA's columns of B
+    auto job_of = [&](int j) {
+        const VocabGemm &g = jobs.g[j];
+        Job k;
+        k.dw = GRADS && g.mode == VG_DW;
+        k.rows = k.dw ? g.rows : n;
+        k.slices = ((k.dw ? n : g.depth) + 63) / 64;
+        k.per = (k.slices + g.splits - 1) / g.splits;
+        k.nm = (uint32_t)((k.rows + 255) / 256);
+        k.nn = g.nn;
+        k.per_split = k.nm * (uint32_t)g.nn;
+        k.units = k.per_split * (uint32_t)g.splits;
+        return k;
+    };
+    const Job job0 = job_of(0), job1 = job_of(JOBS - 1);
+    const uint32_t units = job0.units + (JOBS > 1 ? job1.units : 0);
+    // This pair's i-th unit. One job: every pairs-th one. Two: the pairs that got one unit of the first job fewer take `extra` of the
+    // second one's, about as much work, before all of them go on in turn. (In plain turns 104 units of 256 slices and then 504 of
+    // 52 leave some pairs 876 slices where the mean is 695; so 724.)
+    const uint32_t pair = cluster_index(), pairs = gridDim.x / 2;
+    const uint32_t mine0 = pair < job0.units ? (job0.units - pair + pairs - 1) / pairs : 0;
+    const int over = JOBS > 1 ? (int)(job0.units % pairs) : 0;
+    const uint32_t under = pairs - over;
+    const bool late = (int)pair >= over;
+    uint32_t extra = 0;
+    if (JOBS > 1 && over > 0) {
+        extra = (uint32_t)(2 * job0.per + job1.per) / (uint32_t)(2 * job1.per + 1);
+        if (extra > job1.units / under) extra = job1.units / under;
+    }
+    auto unit_at = [&](uint32_t i) -> uint32_t {
+        if (i < mine0) return pair + i * pairs;
+        if (JOBS == 1) return units;
+        i -= mine0;
+        uint32_t t;
+        if (late && i < extra) t = i * under + pair - over;
+        else t = extra * under + pair + (i - (late ? extra : 0)) * pairs;
+        return job0.units + t;   // (units or more: none)
+    };
+    // a unit: its job, 128-row block of this CTA, column block, split, slices [k0, k0 + nk)
+    struct Unit {
+        int job, mb, nb, ks, k0, nk;
+    };
+    auto unit_of = [&](uint32_t u) {
+        Unit x;
+        x.job = JOBS > 1 && u >= job0.units;
+        if (x.job) u -= job0.units;
+        const Job &k = x.job ? job1 : job0;
+        const uint32_t group = (uint32_t)jobs.g[0].group;
+        x.ks = (int)(u / k.per_split);
+        uint32_t r = u - (uint32_t)x.ks * k.per_split;
+        const uint32_t in_group = group * (uint32_t)k.nn, gi = r / in_group;
+        r -= gi * in_group;
+        const uint32_t left = k.nm - gi * group, gr = left < group ? left : group;
+        x.nb = (int)(r / gr);
+        x.mb = 2 * (int)(gi * group + r - (uint32_t)x.nb * gr) + (int)crank;
+        x.k0 = x.ks * k.per;
+        const int k1 = x.k0 + k.per < k.slices ? x.k0 + k.per : k.slices;
+        x.nk = k1 > x.k0 ? k1 - x.k0 : 0;
+        return x;
+    };
 
     if (warp == 0) {
         // ---------------- producer ----------------
         if (elect_one()) {
-            tma_prefetch_desc(&tma);
-            tma_prefetch_desc(&tmb);
-            const int loads_b = BMN ? (half_b + 63) / 64 : 1;
-            const uint32_t bytes = 2 * (C::A_STAGE + (BMN ? (uint32_t)loads_b * 8192u : (uint32_t)half_b * 128u));
+            for (int j = 0; j < JOBS; ++j) {
+                tma_prefetch_desc(&jobs.a[j]);
+                tma_prefetch_desc(&jobs.b[j]);
+            }
             uint32_t it = 0;
             bool ok = true;
-            for (uint32_t u = u_first; u < units && ok; u += u_step) {
-                int mb, nb, ks, k0, nk;
-                unit_of(u, mb, nb, ks, k0, nk);
-                const int piece = PIECES ? PIECE : nk;
-                for (int kp = 0; kp < nk && ok; kp += piece) {
-                    const int ke = nk - kp < piece ? nk : kp + piece;
+            for (uint32_t i = 0, u; (u = unit_at(i)) < units && ok; ++i) {
+                const Unit x = unit_of(u);
+                const VocabGemm &g = jobs.g[x.job];
+                const CUtensorMap *ma = &jobs.a[x.job], *mb = &jobs.b[x.job];
+                const bool dw = GRADS && (x.job ? job1.dw : job0.dw);
+                const int half_b = g.bn / 2;   // this CTA's columns of B
+                const int loads_b = BMN ? (half_b + 63) / 64 : 1;
+                // Few tokens: the rows of A behind them are not loaded (rows that the tensor map fills cost more than rows that it
+                // reads: T = 1 took 47 us where T = 32 took 32), and what stands there goes into rows of the product that nobody reads.
+                const bool few = !dw && g.a_rows < 128;
+                const uint32_t bytes_a = few ? (uint32_t)g.a_rows * 128u : 2 * C::A_STAGE;
+                const uint32_t bytes = bytes_a + 2 * (BMN ? (uint32_t)loads_b * 8192u : (uint32_t)half_b * 128u);
+                const int row = x.mb * 128, col = x.nb * g.bn + (int)crank * half_b;
+                const int piece = PIECES ? PIECE : x.nk;
+                for (int kp = 0; kp < x.nk && ok; kp += piece) {
+                    const int ke = x.nk - kp < piece ? x.nk : kp + piece;
                     for (int term = 0; term < TERMS && ok; ++term) {
                         // the partial products, smallest first: (2, 0) (1, 1) (0, 2) (1, 0) (0, 1) (0, 0)
                         const int sa = SPLIT == 1 ? 0 : term == 0 ? 2 : (term == 1 || term == 3) ? 1 : 0;
@@ -244,19 +310,17 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1)
                             if (crank == 0) mbar_expect_tx(smem_u32(&full[s]), bytes);   // both CTAs' bytes
                             const uint32_t bar = map_shared(smem_u32(&full[s]), 0);
                             const uint32_t ad = smem_u32(smem + s * C::STAGE), bd = ad + C::A_STAGE;
-                            const int k = 64 * (k0 + kb);
-                            if (!AMN) {
-                                tma_load_2d_pair(ad, &tma, k, sa * g.a_off + mb * 128, bar);
+                            const int k = 64 * (x.k0 + kb);
+                            if (!dw) {
+                                if (!few || crank == 0) tma_load_2d_pair(ad, ma, k, sa * g.a_off + row, bar);
                             } else {
-                                tma_load_2d_pair(ad, &tma, mb * 128, sa * g.a_off + k, bar);
-                                tma_load_2d_pair(ad + 8192, &tma, mb * 128 + 64, sa * g.a_off + k, bar);
+                                tma_load_2d_pair(ad, ma, row, sa * g.a_off + k, bar);
+                                tma_load_2d_pair(ad + 8192, ma, row + 64, sa * g.a_off + k, bar);
                             }
-                            const int col = nb * g.bn + (int)crank * half_b;
                             if (!BMN) {
-                                tma_load_2d_pair(bd, &tmb, k, sb * g.b_off + g.b_y + col, bar);
+                                tma_load_2d_pair(bd, mb, k, sb * g.b_off + g.b_y + col, bar);
                             } else {   // (what lies past the half is loaded and not read)
-                                for (int j = 0; j < loads_b; ++j)
-                                    tma_load_2d_pair(bd + j * 8192, &tmb, col + 64 * j, sb * g.b_off + (MODE == VG_DX ? g.b_y : 0) + k, bar);
+                                for (int j = 0; j < loads_b; ++j) tma_load_2d_pair(bd + j * 8192, mb, col + 64 * j, sb * g.b_off + g.b_y + k, bar);
                             }
                         }
                     }
@@ -272,23 +336,24 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1)
     } else if (warp == 1) {
         // ---------------- MMA issuer ----------------
         if (crank == 0 && elect_one()) {
-            const uint32_t idesc = idesc_bf16(256, (uint32_t)g.bn, AMN, BMN);
             const uint32_t a0 = smem_u32(smem), b0 = a0 + C::A_STAGE;
-            const uint64_t ad0 = AMN ? smem_desc(a0, 8192, 1024, kSwz128) : smem_desc(a0, 16, 1024, kSwz128);
             const uint64_t bd0 = BMN ? smem_desc(b0, 8192, 1024, kSwz128) : smem_desc(b0, 16, 1024, kSwz128);
-            constexpr uint64_t AK = (AMN ? 2048 : 32) >> 4, BK = (BMN ? 2048 : 32) >> 4;
+            constexpr uint64_t BK = (BMN ? 2048 : 32) >> 4;
             uint32_t it = 0, ti = 0;
             bool ok = true;
-            for (uint32_t u = u_first; u < units && ok; u += u_step) {
-                int mb, nb, ks, k0, nk;
-                unit_of(u, mb, nb, ks, k0, nk);
-                const int piece = PIECES ? PIECE : nk;
-                for (int kp = 0; kp < nk && ok; kp += piece) {
+            for (uint32_t i = 0, u; (u = unit_at(i)) < units && ok; ++i) {
+                const Unit x = unit_of(u);
+                const bool dw = GRADS && (x.job ? job1.dw : job0.dw);   // A: dz^T, a row of it along the lines of memory
+                const uint32_t idesc = idesc_bf16(256, (uint32_t)jobs.g[x.job].bn, dw, BMN);
+                const uint64_t ad0 = dw ? smem_desc(a0, 8192, 1024, kSwz128) : smem_desc(a0, 16, 1024, kSwz128);
+                const uint64_t AK = (dw ? 2048 : 32) >> 4;
+                const int piece = PIECES ? PIECE : x.nk;
+                for (int kp = 0; kp < x.nk && ok; kp += piece) {
                     const uint32_t ab = ti & 1;
                     ok = mbar_wait(smem_u32(&acc_empty[ab]), ((ti >> 1) & 1) ^ 1);
                     tc_fence_after();
                     if (!ok) break;
-                    const int steps = (nk - kp < piece ? nk - kp : piece) * TERMS;
+                    const int steps = (x.nk - kp < piece ? x.nk - kp : piece) * TERMS;
                     for (int i = 0; i < steps; ++i, ++it) {
                         const uint32_t s = it % C::NST, ph = (it / C::NST) & 1;
                         ok = mbar_wait(smem_u32(&full[s]), ph);
@@ -312,8 +377,6 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1)
         // ---------------- epilogue warps ----------------
         const int q = warp & 3, half = (warp - 2) >> 2;   // TMEM lane quarter, which half of the columns
         const uint32_t lane_base = (uint32_t)(q * 32) << 16;
-        const int groups = g.bn / 32, first_group = half ? (groups + 1) / 2 : 0;
-        const int my = half ? groups / 2 : (groups + 1) / 2;   // groups of 32 columns, up to 4
         uint8_t *const box = smem + C::OFF_BOX + (warp - 2) * C::BOX;
         uint32_t ti = 0, boxes = 0;
         bool ok = true;
@@ -324,7 +387,7 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1)
             if (lane == 0) mbar_arrive_remote(map_shared(smem_u32(&acc_empty[ab]), 0));
         };
         // 32 columns of this thread's row as bf16: the next of the two 2 KB boxes, stored at (col, row0)
-        auto store_bf16 = [&](const float (&v)[32], int col, int row0) {
+        auto store_bf16 = [&](const CUtensorMap *mo, const float (&v)[32], int col, int row0) {
             if (lane == 0) bulk_wait_read<1>();
             __syncwarp();
             uint8_t *b = box + (boxes++ & 1) * 2048;
@@ -336,11 +399,11 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1)
             fence_async_smem();
             __syncwarp();
             if (lane == 0) {
-                tma_store_2d(&tmo, col, row0, smem_u32(b));
+                tma_store_2d(mo, col, row0, smem_u32(b));
                 bulk_commit();
             }
         };
-        auto store_f32 = [&](const float (&v)[32], int col, int row0, bool add) {
+        auto store_f32 = [&](const CUtensorMap *mo, const float (&v)[32], int col, int row0, bool add) {
             if (lane == 0) bulk_wait_read<0>();
             __syncwarp();
 #pragma unroll
@@ -350,13 +413,13 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1)
             fence_async_smem();
             __syncwarp();
             if (lane == 0) {
-                if (add) tma_add_2d(&tmo, col, row0, smem_u32(box));
-                else tma_store_2d(&tmo, col, row0, smem_u32(box));
+                if (add) tma_add_2d(mo, col, row0, smem_u32(box));
+                else tma_store_2d(mo, col, row0, smem_u32(box));
                 bulk_commit();
             }
         };
         // DW into a matrix off the 16-byte grid: a row at a time, one element a lane
-        auto store_plain = [&](const float (&v)[32], int col, int row0) {
+        auto store_plain = [&](const VocabGemm &g, const float (&v)[32], int col, int row0) {
             __syncwarp();
 #pragma unroll
             for (int e = 0; e < 8; ++e)
@@ -373,58 +436,52 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1)
             }
         };
 
-        for (uint32_t u = u_first; u < units && ok; u += u_step) {
-            int mb, nb, ks, k0, nk;
-            unit_of(u, mb, nb, ks, k0, nk);
-            const int row0 = mb * 128 + q * 32, row = row0 + lane;
+        auto row_in = [&](uint32_t u) {
+            RowIn r = {};
+            if (GRADS || u >= units) return r;
+            const VocabGemm &g = jobs.g[0];
+            const int row = unit_of(u).mb * 128 + q * 32 + lane;
+            if (row >= n) return r;
+            r.token = g.token ? g.token[row] : row;
+            if (g.label) r.label = g.label[r.token];
+            if (MODE == VG_DZ) {
+                r.lse = g.lse[r.token];
+                r.dloss = g.dloss[r.token * g.dloss_step];
+                if (g.bad) r.bad = g.bad[r.token];
+            }
+            return r;
+        };
+        RowIn coming = row_in(unit_at(0));
+        for (uint32_t i = 0, u; (u = unit_at(i)) < units && ok; ++i) {
+            const Unit x = unit_of(u);
+            const VocabGemm &g = jobs.g[x.job];
+            const CUtensorMap *mo = &jobs.o[x.job];
+            const bool dw = GRADS && (x.job ? job1.dw : job0.dw);
+            const int rows = x.job ? job1.rows : job0.rows;
+            const int nb = x.nb, ks = x.ks, nk = x.nk;
+            const int groups = g.bn / 32, first_group = half ? (groups + 1) / 2 : 0;
+            const int my = half ? groups / 2 : (groups + 1) / 2;   // groups of 32 columns, up to 4
+            const int row0 = x.mb * 128 + q * 32, row = row0 + lane;
+            const RowIn in = coming;
+            coming = row_in(unit_at(i + 1));
             // this thread's row
             Targets t;
             t.next = INT_MAX;
             t.K = 0;
             float most = -INFINITY, sum_e = 0.0f, zt = 0.0f, lse2 = 0.0f, grad = 0.0f;
             bool hit = false;
-            if ((MODE == VG_FWD || MODE == VG_DZ) && row < n) {
-                const int64_t token = g.token ? g.token[row] : row;
-                t.start(g, token, g.v0 + nb * g.bn, first_group * 32);
+            if (!GRADS && row < n) {
+                t.start(g, in.token, in.label, g.v0 + nb * g.bn, first_group * 32);
                 if (MODE == VG_DZ) {
-                    lse2 = g.lse[token] * 1.4426950408889634f;
-                    grad = g.dloss[token * g.dloss_step] * g.tau;
-                    if (g.label ? g.label[token] >= g.V : false) grad = NAN;
-                    if (g.bad) grad += g.bad[token];
+                    lse2 = in.lse * 1.4426950408889634f;
+                    grad = in.dloss * g.tau + in.bad;
+                    if (g.label && in.label >= g.V) grad = NAN;
                 }
             }
             // what becomes of 32 columns of the row, from column `c` of the tile on
             auto process = [&](float (&v)[32], int c) {
                 const int col = nb * g.bn + c;
-                if (MODE == VG_FWD) {
-                    if (row0 >= n || col >= g.cols) return;
-                    if (col + 32 > g.cols) {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (col + j >= g.cols) v[j] = -INFINITY;
-                    }
-                    while (t.next < c + 32) {
-                        const int at = t.next - c;
-                        float x = 0.0f;
-#pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (j == at) x = v[j];
-                        zt = fmaf(t.q, x, zt);
-                        hit = true;
-                        t.advance();
-                    }
-                    float m[4] = {v[0], v[1], v[2], v[3]};
-#pragma unroll
-                    for (int j = 4; j < 32; ++j) m[j & 3] = max_nan(m[j & 3], v[j]);
-                    const float top = max_nan(max_nan(m[0], m[1]), max_nan(m[2], m[3])) * g.c;
-                    const float now = max_nan(most, top);
-                    if (now == -INFINITY) return;
-                    float s[4] = {sum_e * exp2_fast(most - now), 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) s[j & 3] += exp2_fast(fmaf(v[j], g.c, -now));
-                    sum_e = (s[0] + s[1]) + (s[2] + s[3]);
-                    most = now;
-                } else if (MODE == VG_DZ) {
+                if (MODE == VG_DZ) {
                     if (col >= g.cols) return;
                     if (row < n) {
 #pragma unroll
@@ -444,7 +501,7 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1)
                     }
 #pragma unroll
                     for (int part = 0; part < SPLIT; ++part) {
-                        store_bf16(v, col, part * g.slot_rows + row0);
+                        store_bf16(mo, v, col, part * g.slot_rows + row0);
                         if (part + 1 < SPLIT) {
 #pragma unroll
                             for (int j = 0; j < 32; ++j) v[j] -= __bfloat162float(__float2bfloat16_rn(v[j]));
@@ -452,14 +509,14 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1)
                     }
                 } else {
                     if (row0 >= rows || col >= g.cols) return;
-                    if (MODE == VG_DX) store_f32(v, col, ks * g.slot_rows + row0, g.add);
-                    else if (g.out) store_plain(v, col, row0);
-                    else if (g.out_f32) store_f32(v, col, g.out_y + ks * g.slot_rows + row0, false);
-                    else store_bf16(v, col, g.out_y + row0);
+                    if (!dw) store_f32(mo, v, col, ks * g.slot_rows + row0, g.add);
+                    else if (g.out) store_plain(g, v, col, row0);
+                    else if (g.out_f32) store_f32(mo, v, col, g.out_y + ks * g.slot_rows + row0, false);
+                    else store_bf16(mo, v, col, g.out_y + row0);
                 }
             };
             if (nk == 0) {   // nothing to add up: zeros (no token in use, or a split past the end)
-                if (MODE == VG_DX || MODE == VG_DW) {
+                if (GRADS) {
 #pragma unroll 1
                     for (int i = 0; i < my; ++i) {
                         float v[32];
@@ -482,26 +539,74 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1)
                     ok = mbar_wait(smem_u32(&acc_full[ab]), (ti >> 1) & 1);
                     tc_fence_after();
                     if (!ok) break;
+                    if (row0 < rows) {   // (the same for the whole warp)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if (i < my) {   // (the same for the whole warp)
+                        for (int i = 0; i < 4; ++i) {
+                            if (i < my) {
 #pragma unroll
-                            for (int h = 0; h < 2; ++h) {   // (32 at a time spill)
-                                float v[16];
-                                tmem_ld16(tmem + lane_base + ab * 256 + (first_group + i) * 32 + 16 * h, v);
-                                tmem_ld_wait();
-                                tmem_regs_ready(v);
+                                for (int h = 0; h < 2; ++h) {   // (32 at a time spill)
+                                    float v[16];
+                                    tmem_ld16(tmem + lane_base + ab * 256 + (first_group + i) * 32 + 16 * h, v);
+                                    tmem_ld_wait();
+                                    tmem_regs_ready(v);
 #pragma unroll
-                                for (int j = 0; j < 16; ++j) sum[i][16 * h + j] += v[j];
+                                    for (int j = 0; j < 16; ++j) sum[i][16 * h + j] += v[j];
+                                }
                             }
                         }
                     }
                     release_acc(ab);
                 }
                 if (!ok) break;
+                if constexpr (MODE == VG_FWD) {
+                    if (row < n) {
+                        // the targets' logits, then the maximum and the sum of exponentials over what columns exist
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (i < my) process(sum[i], (first_group + i) * 32);
+                        for (int i = 0; i < 4; ++i) {
+                            const int c = (first_group + i) * 32, left = i < my ? g.cols - nb * g.bn - c : 0;
+                            if (left < 32) {
+#pragma unroll
+                                for (int j = 0; j < 32; ++j)
+                                    if (j >= left) sum[i][j] = -INFINITY;
+                            }
+                            while (i < my && t.next < c + 32) {
+                                const int at = t.next - c;
+                                float x = 0.0f;
+#pragma unroll
+                                for (int j = 0; j < 32; ++j)
+                                    if (j == at) x = sum[i][j];
+                                zt = fmaf(t.q, x, zt);
+                                hit = true;
+                                t.advance();
+                            }
+                        }
+                        float m[8], s[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) m[j] = sum[0][j];
+#pragma unroll
+                        for (int j = 8; j < 128; ++j) m[j & 7] = max_nan(m[j & 7], sum[j >> 5][j & 31]);
+#pragma unroll
+                        for (int w = 4; w; w >>= 1)
+#pragma unroll
+                            for (int j = 0; j < w; ++j) m[j] = max_nan(m[j], m[j + w]);
+                        most = m[0] * g.c;
+                        if (!(most == -INFINITY)) {
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) s[j] = exp2_fast(fmaf(sum[0][j], g.c, -most));
+#pragma unroll
+                            for (int j = 8; j < 128; ++j) s[j & 7] += exp2_fast(fmaf(sum[j >> 5][j & 31], g.c, -most));
+                            sum_e = ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
+                        }
+                        const int64_t at = (int64_t)(g.slot0 + 2 * nb + half) * g.tp + row;   // (of a half without columns too)
+                        g.stat[at] = make_float2(most, sum_e);
+                        if (!g.label) g.zt[at] = zt;
+                        else if (hit) g.zt[row] = zt;
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (i < my) process(sum[i], (first_group + i) * 32);
+                }
             } else {
                 const uint32_t ab = ti & 1;
                 ok = mbar_wait(smem_u32(&acc_full[ab]), (ti >> 1) & 1);
@@ -518,15 +623,6 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1)
                 }
                 if (my == 0) release_acc(ab);
                 ++ti;
-            }
-            if (MODE == VG_FWD && row < n) {   // (a half without columns too: the sums are joined over all slots)
-                const int64_t at = (int64_t)(g.slot0 + 2 * nb + half) * g.tp + row;
-                g.stat[at] = make_float2(most, sum_e);
-                if (g.label) {
-                    if (hit) g.zt[row] = zt;
-                } else {
-                    g.zt[at] = zt;
-                }
             }
         }
     }

@@ -71,6 +71,11 @@ template <typename E, int VEC, int STEP> struct Cols {
 #pragma unroll
         for (int i = 0; i < VEC; ++i) x[i] = STEP == 0 || i * STEP < left ? p[STEP ? i * STEP : i] : 0.0f;
     }
+    __device__ __forceinline__ void ready()
+    {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) asm volatile("" : "+f"(x[i]));
+    }
     __device__ __forceinline__ void fill(float v)
     {
 #pragma unroll
@@ -120,7 +125,7 @@ __global__ void __launch_bounds__(256) k_embed_fwd(const int64_t *__restrict__ i
 }
 
 // ---- tokens sorted by id -------------------------------------------------------------------------------
-constexpr int kSortCtas = 8, kSortThreads = 1024, kMaxBins = 512;
+constexpr int kZeroClusters = 13, kSortCtas = 8, kSortThreads = 1024, kMaxBins = 512;
 
 // The first cluster sorts, the others write zeros over dtable meanwhile: most words have no tokens, and the sums
 // overwrite the rows of those that have (16384 tokens of 32000 words: 22 MB of 131).
@@ -321,6 +326,8 @@ template <typename E, int VEC, int STEP> __global__ void __launch_bounds__(256) 
             x[j].get(a.part + at * 2 * a.d + col, left);
         }
 #pragma unroll
+        for (int j = 0; j < F; ++j) x[j].ready();   // (all of them in flight, not one after the other)
+#pragma unroll
         for (int j = 0; j < F; ++j)
             if (has[j]) sum.add(x[j]);
         more = has[F - 1];
@@ -405,10 +412,12 @@ template <typename E> cudaError_t run_bwd(const resbm_embed_desc &d, const int64
     static std::atomic<uint8_t> done[kMaxDev];
     cudaError_t e = ensure_smem(k_sort, 32 * 4 * kMaxBins, c.device, done);
     // (the cluster's size is the kernel's own)
-    // the rest of the SMs write zeros, 64 KB a CTA at least
+    // Zeros: 64 KB a CTA at least, and no more clusters than can be there at once (two in 18 or 20 SMs): the last ones would wait
+    // for others to end, and write 158 MB of 1 GB by themselves
+    // (T = 65536, V = 250002, d = 1003 in fp32, forward and backward: 307 us with 13 clusters of zeros, 334 with 11, 348 with 15, 379 with 18)
     const int64_t bytes = d.V * d.d * (int64_t)sizeof(E);
-    const int64_t zeros = std::min<int64_t>((bytes + 65535) / 65536, std::max(kSortCtas, c.sm_count - kSortCtas));
-    const unsigned grid = (unsigned)(kSortCtas + (zeros + kSortCtas - 1) / kSortCtas * kSortCtas);
+    const int64_t clusters = std::max<int64_t>(1, std::min<int64_t>((bytes + kSortCtas * 65536 - 1) / (kSortCtas * 65536), kZeroClusters));
+    const unsigned grid = (unsigned)(kSortCtas * (1 + clusters));
     if (e == cudaSuccess) e = launch(k_sort, dim3(grid), dim3(kSortThreads), smem, c.stream, ids, (int)d.T, (int)d.V, d.padding, passes, bits, w.keys, w.vals,
                                      static_cast<uint8_t *>(dtable), bytes);
     if (e != cudaSuccess) return e;

@@ -442,9 +442,11 @@ struct Call {
 template <typename E, int SPLIT> void run_loss(Run &r, const Shape &s, const Plan &p, const Call &a)
 {
     constexpr bool F32 = SPLIT == 3;
-    // Slices of a piece of a sum: 512 deep (128 of three parts), which leaves the truncation of 32 MMAs (48). T = 777, V = 50001,
-    // d = 1000: losses 3.8e-7 off (256 deep 1.8e-7, 1024 8e-7); T = 16384, V = 32000, d = 2048: 1104 us (1194, 1090).
-    constexpr int P = F32 ? 2 : 8;
+    // Slices of a piece of a sum: 512 deep (256 of three parts), which leaves the truncation of 32 MMAs (16, and 80 of smaller
+    // products). T = 777, V = 50001,
+    // d = 1000: losses 3.8e-7 off (256 deep 1.8e-7, 1024 8e-7); T = 16384, V = 32000, d = 2048: 1104 us (1194, 1090). fp32, T = 2048, V = 8000,
+    // d = 768, forward and backward: dX 5.4e-7 off, 455 us (128 deep 3.8e-7, 497; 512 9.2e-7, 444).
+    constexpr int P = F32 ? 4 : 8;
     const resbm_vocab_desc &d = *a.d;
     const int64_t T = s.T, V = s.V;
     const float tau = s.distill ? d.temperature : 1.0f;

@@ -230,6 +230,7 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __gri
     // This pair's i-th unit. One job: every pairs-th one. Two: the pairs that got one unit of the first job fewer take `extra` of the
     // second one's, about as much work, before all of them go on in turn. (In plain turns 104 units of 256 slices and then 504 of
     // 52 leave some pairs 876 slices where the mean is 695; so 724.)
+    constexpr uint32_t kUnitSlices = 6;   // what a unit costs around its products
     const uint32_t pair = cluster_index(), pairs = gridDim.x / 2;
     const uint32_t mine0 = pair < job0.units ? (job0.units - pair + pairs - 1) / pairs : 0;
     const int over = JOBS > 1 ? (int)(job0.units % pairs) : 0;
@@ -237,7 +238,8 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __gri
     const bool late = (int)pair >= over;
     uint32_t extra = 0;
     if (JOBS > 1 && over > 0) {
-        extra = (uint32_t)(2 * job0.per + job1.per) / (uint32_t)(2 * job1.per + 1);
+        const uint32_t c0 = TERMS * job0.per + kUnitSlices, c1 = TERMS * job1.per + kUnitSlices;
+        extra = (2 * c0 + c1) / (2 * c1);
         if (extra > job1.units / under) extra = job1.units / under;
     }
     auto unit_at = [&](uint32_t i) -> uint32_t {

@@ -18,7 +18,8 @@ Pid_definition). The encoder and decoder run through the C ABI of libresbm.so
 inside torch.autograd.Function; everything else (attention, SwiGLU feed-forward, RMSNorm, rotary
 positions, embedding, loss) is plain PyTorch in bf16, but for the norms with fuse_add_norm, which
 add the residual and normalise in one kernel of the library. There is no fallback: without the
-library the boundary raises.
+library the boundary raises. With fuse_vocab the embedding and the loss run in the library too, without the
+batch's logits (resbm_embed_fwd, resbm_linear_ce_fwd and their backwards).
 """
 from __future__ import annotations
 
@@ -53,6 +54,8 @@ class PipelineConfig:
     fuse_norm: bool = True   # the receiving block's pre-attention RMSNorm fused into the decoder
     fuse_add_norm: bool = False   # every other RMSNorm with the residual's addition before it, in one
                                   # kernel (resbm_add_rmsnorm_fwd); else torch's
+    fuse_vocab: bool = False      # the embedding and the loss of the logits, which are not stored, by the
+                                  # library (resbm_embed_fwd, resbm_linear_ce_fwd); else torch's
 
     def with_(self, **kw) -> "PipelineConfig":
         return replace(self, **kw)
@@ -272,6 +275,109 @@ def add_norm(x, a, gamma):
     return _AddNorm.apply(x, a, gamma)
 
 
+# ---- the vocabulary's ends ------------------------------------------------------------------------
+def _dtype_name(t):
+    return "bf16" if t.dtype == torch.bfloat16 else "f32"
+
+
+class _Embed(torch.autograd.Function):
+    """scale * table[ids]: resbm_embed_fwd forward, resbm_embed_bwd backward."""
+
+    @staticmethod
+    def forward(ctx, ids, table, scale, padding):
+        flat = ids.reshape(-1).contiguous()
+        out = torch.empty(*ids.shape, table.shape[1], dtype=table.dtype, device=table.device)
+        resbm.resbm_embed_fwd(flat, table, scale, out.view(-1, table.shape[1]))
+        ctx.save_for_backward(flat)
+        ctx.shape, ctx.scale, ctx.padding = table.shape, scale, padding
+        return out
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dout):
+        ids, = ctx.saved_tensors
+        rows = _rows(dout)
+        dtable = torch.empty(ctx.shape, dtype=dout.dtype, device=dout.device)
+        ws = resbm.vocab_workspace(resbm.RESBM_VOCAB_EMBED_BWD, rows.shape[0], *ctx.shape, _dtype_name(dout), device=dout.device)
+        resbm.resbm_embed_bwd(ids, rows, ctx.scale, dtable, ws, padding=ctx.padding)
+        return None, dtable, None, None
+
+
+def embed(ids, table, scale=1.0, padding=-1):
+    """scale * table[ids] (ids int64 of any shape), with the table's gradient by sorted tokens; the tokens of the id
+    `padding` give it nothing (negative: none)."""
+    return _Embed.apply(ids, table, float(scale), int(padding))
+
+
+class _VocabLoss(torch.autograd.Function):
+    """A token's loss of the logits x . head^T, which are not stored: resbm_linear_ce_fwd and _bwd, or with a teacher's logits
+    resbm_distill_fwd and _bwd."""
+
+    @staticmethod
+    def forward(ctx, x, head, target, teacher, temperature):
+        rows = _rows(x)
+        (T, d), V, K = rows.shape, head.shape[0], 0 if teacher is None else target.shape[-1]
+        ops = (resbm.RESBM_VOCAB_CE_FWD, resbm.RESBM_VOCAB_CE_BWD) if teacher is None else (resbm.RESBM_VOCAB_DISTILL_FWD, resbm.RESBM_VOCAB_DISTILL_BWD)
+        target = (target.reshape(-1) if teacher is None else target.reshape(-1, K)).contiguous()
+        loss, lse = (torch.empty(T, dtype=torch.float32, device=x.device) for _ in range(2))
+        ws = resbm.vocab_workspace(ops[0], T, V, d, _dtype_name(x), K, x.device)
+        if teacher is None:
+            resbm.resbm_linear_ce_fwd(rows, head, target, loss, lse, ws)
+        else:
+            teacher = teacher.reshape(-1, K).contiguous()
+            resbm.resbm_distill_fwd(rows, head, target, teacher, temperature, loss, lse, ws)
+        ctx.save_for_backward(x, head, target, teacher, lse)
+        ctx.op, ctx.temperature = ops[1], temperature
+        return loss.view(x.shape[:-1])
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dloss):
+        x, head, target, teacher, lse = ctx.saved_tensors
+        rows = _rows(x)
+        K = 0 if teacher is None else target.shape[1]
+        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if ctx.needs_input_grad[0] else None
+        dhead = torch.empty(head.shape, dtype=head.dtype, device=head.device) if ctx.needs_input_grad[1] else None
+        ws = resbm.vocab_workspace(ctx.op, rows.shape[0], head.shape[0], rows.shape[1], _dtype_name(x), K, x.device)
+        out = dloss.reshape(-1).contiguous(), None if dx is None else dx.view(rows.shape), dhead, ws
+        if teacher is None:
+            resbm.resbm_linear_ce_bwd(rows, head, target, lse, *out)
+        else:
+            resbm.resbm_distill_bwd(rows, head, target, teacher, ctx.temperature, lse, *out)
+        return dx, dhead, None, None, None
+
+
+def _reduce(loss, has, reduction):
+    if reduction == "none":
+        return loss
+    if reduction == "sum":
+        return loss.sum()
+    if reduction != "mean":
+        raise ValueError("reduction must be 'mean', 'sum' or 'none'")
+    return loss.sum() / has.sum().clamp_min(1)
+
+
+def linear_cross_entropy(x, head, labels, reduction="mean"):
+    """Cross entropy of the logits x . head^T (x (..., d), head (V, d)) against labels (x's leading shape, int64; negative: no
+    label), without the logits. The mean is over the tokens with a label."""
+    if labels.shape != x.shape[:-1]:
+        raise ValueError("labels must have x's leading shape")
+    return _reduce(_VocabLoss.apply(x, head, labels, None, 1.0), labels >= 0, reduction)
+
+
+def distillation(x, head, index, teacher, temperature=1.0, reduction="mean"):
+    """temperature^2 times the divergence of softmax(x . head^T / temperature) from that of a teacher's K logits a token at the
+    words `index` (both x's leading shape and K; index int64, negative: no entry)."""
+    if index.shape[:-1] != x.shape[:-1] or teacher.shape != index.shape:
+        raise ValueError("index and teacher must be of x's leading shape and K")
+    return _reduce(_VocabLoss.apply(x, head, index, teacher, float(temperature)), (index >= 0).any(dim=-1), reduction)
+
+
+def next_tokens(tokens):
+    """The labels of a (batch, seq) tensor of token ids: the next token, none at the end"""
+    return Fn.pad(tokens[:, 1:], (0, 1), value=-100)
+
+
 class Boundary(torch.nn.Module):
     """One ResBM boundary: the encoder on the sending stage, the decoder on the receiving one.
     Weights N(0, 1/fan_in), bf16."""
@@ -388,14 +494,14 @@ class PipelineModel(torch.nn.Module):
             self._rope[seq] = _rope_tables(seq, self.cfg.d // self.cfg.heads, device)
         return self._rope[seq]
 
-    def forward(self, tokens):
-        """Mean next-token cross-entropy of a (batch, seq) tensor of token ids."""
+    def hidden(self, tokens):
+        """The last norm's output, (batch, seq, d), for a (batch, seq) tensor of token ids."""
         cfg = self.cfg
         bsz, seq = tokens.shape
         T, d = bsz * seq, cfg.d
         rope = self.rope(seq, tokens.device)
         per_stage = cfg.layers // cfg.stages
-        x = Fn.embedding(tokens, self.embed)
+        x = embed(tokens, self.embed) if cfg.fuse_vocab else Fn.embedding(tokens, self.embed)
         b = z = None
         fuse = cfg.fuse_add_norm
         for s in range(cfg.stages):
@@ -427,9 +533,28 @@ class PipelineModel(torch.nn.Module):
                 if j == per_stage - 1 and s < cfg.stages - 1:   # send: encode after the feed-forward
                     b = self.bounds[s].encode(h.reshape(T, d), z.reshape(T, d))
                 x = h
-        last = add_norm(x, z, self.norm)[1] if fuse else Fn.rms_norm(x + z, (d,), self.norm, NORM_EPS)
+        return add_norm(x, z, self.norm)[1] if fuse else Fn.rms_norm(x + z, (d,), self.norm, NORM_EPS)
+
+    def forward(self, tokens):
+        """Mean next-token cross-entropy of a (batch, seq) tensor of token ids."""
+        last = self.hidden(tokens)
+        if self.cfg.fuse_vocab:
+            return linear_cross_entropy(last, self.head, next_tokens(tokens))
         logits = Fn.linear(last, self.head)
-        return Fn.cross_entropy(logits[:, :-1].reshape(-1, cfg.vocab).float(), tokens[:, 1:].reshape(-1))
+        return Fn.cross_entropy(logits[:, :-1].reshape(-1, self.cfg.vocab).float(), tokens[:, 1:].reshape(-1))
+
+    @torch.no_grad()
+    def top_logits(self, tokens, k, rows=4096):
+        """(index, teacher): the k largest logits of every token and their words, for distill() of another model; the logits of
+        `rows` tokens at a time."""
+        last = self.hidden(tokens).reshape(-1, self.cfg.d)
+        top = [Fn.linear(part, self.head).topk(k, dim=-1) for part in last.split(rows)]
+        return tuple(torch.cat(t).view(*tokens.shape, k) for t in ([t.indices for t in top], [t.values for t in top]))
+
+    def distill(self, tokens, index, teacher, temperature=1.0):
+        """The mean divergence from a teacher's top logits (top_logits of an uncompressed model, for instance), without this
+        model's logits. (Always by the library: torch has no such loss.)"""
+        return distillation(self.hidden(tokens), self.head, index, teacher, temperature)
 
 
 def synthetic_tokens(cfg: PipelineConfig, device="cuda", seed=1):

@@ -59,22 +59,30 @@ template <typename E, int VEC, int STEP> struct Cols {
             *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
         }
     }
-    // fp32 partial sums (rows of any alignment)
+    // fp32 partial sums (rows of whole vectors where STEP is 0)
     __device__ __forceinline__ void put(float *p, int64_t left) const
     {
+        if constexpr (STEP > 0) {
 #pragma unroll
-        for (int i = 0; i < VEC; ++i)
-            if (STEP == 0 || i * STEP < left) p[STEP ? i * STEP : i] = x[i];
+            for (int i = 0; i < VEC; ++i)
+                if (i * STEP < left) p[i * STEP] = x[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < VEC; i += 4) *reinterpret_cast<float4 *>(p + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+        }
     }
     __device__ __forceinline__ void get(const float *p, int64_t left)
     {
+        if constexpr (STEP > 0) {
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) x[i] = STEP == 0 || i * STEP < left ? p[STEP ? i * STEP : i] : 0.0f;
-    }
-    __device__ __forceinline__ void ready()
-    {
+            for (int i = 0; i < VEC; ++i) x[i] = i * STEP < left ? p[i * STEP] : 0.0f;
+        } else {
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) asm volatile("" : "+f"(x[i]));
+            for (int i = 0; i < VEC; i += 4) {
+                const float4 v = *reinterpret_cast<const float4 *>(p + i);
+                x[i] = v.x; x[i + 1] = v.y; x[i + 2] = v.z; x[i + 3] = v.w;
+            }
+        }
     }
     __device__ __forceinline__ void fill(float v)
     {
@@ -253,7 +261,7 @@ struct SumArgs {
 // Blocks of kRun sorted positions, 2^log_tx threads along a row, which add the rows of each word up in order, sixteen in
 // flight. A word whose tokens all lie in the block is finished; the block's first and last runs may be pieces of longer ones, and
 // leave a partial sum (k_embed_join). So the work is even whatever the ids are.
-template <typename E, int VEC, int STEP> __global__ void __launch_bounds__(256) k_embed_sum(const SumArgs a)
+template <typename E, int VEC, int STEP> __global__ void __launch_bounds__(256, 3) k_embed_sum(const SumArgs a)
 {
     griddep_wait();
     griddep_launch_dependents();
@@ -271,7 +279,7 @@ template <typename E, int VEC, int STEP> __global__ void __launch_bounds__(256) 
     const int used = __popc(__ballot_sync(0xffffffffu, k < a.V));        // (keys ascend)
     const E *dout = static_cast<const E *>(a.dout) + col;
     float *part = a.part + b * 2 * a.d + col;
-    constexpr int F = STEP ? 4 : 8;   // rows in flight
+    constexpr int F = STEP ? 4 : 32 / VEC;   // rows in flight
     Cols<E, VEC, STEP> sum;
     sum.fill(0.0f);
     bool first_run = true;
@@ -325,8 +333,7 @@ template <typename E, int VEC, int STEP> __global__ void __launch_bounds__(256) 
             has[j] = i + j < blocks && a.keys[at * kRun] == k;
             x[j].get(a.part + at * 2 * a.d + col, left);
         }
-#pragma unroll
-        for (int j = 0; j < F; ++j) x[j].ready();   // (all of them in flight, not one after the other)
+        asm volatile("" ::: "memory");   // (all of them in flight, not one after the other)
 #pragma unroll
         for (int j = 0; j < F; ++j)
             if (has[j]) sum.add(x[j]);

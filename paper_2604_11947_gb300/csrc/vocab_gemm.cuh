@@ -170,7 +170,7 @@ template <int JOBS> struct VocabJobs {
     VocabGemm g[JOBS];
 };
 
-template <int MODE, int SPLIT, int PIECE, int JOBS = MODE == VG_GRADS ? 2 : 1>
+template <int MODE, int SPLIT, int PIECE, int JOBS>
 __global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __grid_constant__ VocabJobs<JOBS> jobs)
 {
     using C = VocabCfg;

@@ -29,8 +29,7 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // their words (the products' tiles look theirs up by bisection), ranked by counting: K^2 / 32 comparisons a lane, 128 at K = 64.
 template <typename E>
 __global__ void __launch_bounds__(256) k_targets(const int64_t *__restrict__ index, const E *__restrict__ teacher, int64_t T, int K, int64_t V,
-                                                 float tau, int32_t *__restrict__ list, float *__restrict__ weight,
-                                                 float *__restrict__ ent, float *__restrict__ bad, int32_t *__restrict__ count)
+                                                 float tau, int2 *__restrict__ list, float *__restrict__ ent, float *__restrict__ bad, int32_t *__restrict__ count)
 {
     extern __shared__ int32_t sh_key[];
     griddep_wait();
@@ -74,8 +73,7 @@ __global__ void __launch_bounds__(256) k_targets(const int64_t *__restrict__ ind
                 q = expf(x) * inv;
                 if (!(q == 0.0f)) h = fmaf(q, x - log_sum, h);
             }
-            list[t * K + rank] = mine;
-            weight[t * K + rank] = q;
+            list[t * K + rank] = make_int2(mine, __float_as_int(q));
         }
 #pragma unroll
         for (int o = 16; o; o >>= 1) h += __shfl_xor_sync(0xffffffffu, h, o);
@@ -384,8 +382,9 @@ struct Plan {
     Units fwd, dx, dw;    // (of a whole piece; the last one's are its own)
     int slots;            // fwd
     size_t bytes;
-    int32_t *n, *token, *row, *count, *list;
-    float *weight, *ent, *bad, *zt, *dxs, *dws;
+    int32_t *n, *token, *row, *count;
+    int2 *list;
+    float *ent, *bad, *zt, *dxs, *dws;
     float2 *stat;
     __nv_bfloat16 *xp, *wp, *dz;
 };
@@ -413,8 +412,7 @@ Plan make_plan(const Shape &s, void *ws)
     p.row = w.take<int32_t>(s.T);
     p.token = w.take<int32_t>(s.T);
     if (s.distill) {
-        p.list = w.take<int32_t>(s.T * s.K);
-        p.weight = w.take<float>(s.T * s.K);
+        p.list = w.take<int2>(s.T * s.K);
         p.ent = w.take<float>(s.T);
         p.bad = w.take<float>(s.T);
         p.count = w.take<int32_t>(s.T);
@@ -504,7 +502,7 @@ template <typename E, int SPLIT> void run_loss(Run &r, const Shape &s, const Pla
         const int K = (int)s.K, warps = K <= 256 ? 8 : K <= 512 ? 4 : 2;
         const unsigned grid = row_grid(c, T, warps);
         auto go = [&](auto kernel, auto teacher) {
-            r.go(kernel, dim3(grid), dim3(32 * warps), (size_t)warps * K * 4, 1, a.target, teacher, T, K, V, tau, p.list, p.weight, p.ent, p.bad, p.count);
+            r.go(kernel, dim3(grid), dim3(32 * warps), (size_t)warps * K * 4, 1, a.target, teacher, T, K, V, tau, p.list, p.ent, p.bad, p.count);
         };
         if (d.teacher_dtype == RESBM_F32) go(k_targets<float>, static_cast<const float *>(a.teacher));
         else go(k_targets<__nv_bfloat16>, static_cast<const __nv_bfloat16 *>(a.teacher));
@@ -540,7 +538,6 @@ template <typename E, int SPLIT> void run_loss(Run &r, const Shape &s, const Pla
     g.token = direct ? nullptr : p.token;
     g.label = label;
     g.list = p.list;
-    g.weight = p.weight;
     g.K = (int)s.K;
     g.tp = p.tp;
     g.c = kLog2e / tau;

@@ -61,8 +61,7 @@ struct VocabGemm {
     int32_t v0;               // the piece's first word
     const int32_t *token;     // row -> token, or null: the same
     const int64_t *label;     // a token's target, or null: the lists
-    const int32_t *list;      // K targets a token in ascending order, INT32_MAX behind the last
-    const float *weight;      // their weights
+    const int2 *list;         // K targets a token in ascending order with their weights' bits, INT32_MAX behind the last
     int32_t K;
     int32_t slot0;            // FWD: the first slot of this launch (two a unit)
     int64_t tp;               // rows of a slot, rounded up
@@ -108,38 +107,36 @@ __device__ __forceinline__ void tma_add_2d(const CUtensorMap *m, int32_t x, int3
 
 // A row's targets in ascending order, seen from a tile: `next` is the next one's column in the tile (INT_MAX: none).
 struct Targets {
-    const int32_t *list;
-    const float *weight;
+    const int2 *list;
     int K, p, base, next;
     float q;
     __device__ __forceinline__ void set()
     {
         next = INT_MAX;
         if (p < K) {
-            const int32_t v = list[p];
-            if (v != INT32_MAX) {
-                next = v - base;
-                q = weight[p];
+            const int2 v = list[p];
+            if (v.x != INT32_MAX) {
+                next = v.x - base;
+                q = __int_as_float(v.y);
             }
         }
     }
     // those from column `first` of the tile that starts at word `base_` on
-    __device__ __forceinline__ void start(const VocabGemm &g, int64_t token, int64_t label, int base_, int first)
+    __device__ __forceinline__ void start(const VocabGemm &g, int64_t token, int32_t label, int base_, int first)
     {
         base = base_;
         if (g.label) {
             K = 0;
             q = 1.0f;
-            next = label >= (int64_t)base + first && label < g.V ? (int)(label - base) : INT_MAX;
+            next = label >= base + first && label != INT32_MAX ? label - base : INT_MAX;
             return;
         }
         K = g.K;
         list = g.list + token * K;
-        weight = g.weight + token * K;
         int lo = 0, hi = K;   // the first with list >= base + first
         while (lo < hi) {
             const int mid = (lo + hi) >> 1;
-            if (list[mid] < base + first) lo = mid + 1;
+            if (list[mid].x < base + first) lo = mid + 1;
             else hi = mid;
         }
         p = lo;
@@ -158,11 +155,30 @@ struct Targets {
 
 // What a row's token brings along, loaded a unit ahead (three loads that wait for one another, 1500 cycles)
 struct RowIn {
-    int64_t token, label;
+    int32_t token, label;
     float lse, dloss, bad;
 };
 
+struct Yes { static constexpr bool value = true; };
+struct No { static constexpr bool value = false; };
+
 // MODE: what becomes of the accumulator; SPLIT: bf16 parts of an operand; PIECE: 64-deep slices of a piece of a sum (0: whole)
+// x / d for x under 2^31: a product with the reciprocal and a correction (a division is 20 dependent instructions, and every warp
+// has three a unit)
+struct Divisor {
+    uint32_t d, m;
+    __device__ __forceinline__ void set(uint32_t d_)
+    {
+        d = d_ ? d_ : 1;
+        m = 0xFFFFFFFFu / d;   // (2^32 / d or up to one less: a quotient is right or one less)
+    }
+    __device__ __forceinline__ uint32_t of(uint32_t x) const
+    {
+        const uint32_t q = __umulhi(x, m);
+        return q + (x - q * d >= d);
+    }
+};
+
 // JOBS: 1, or the two of VG_GRADS, whose units follow one another (the one with the longer units first): apart, the last round of
 // each leaves pairs without work.
 template <int JOBS> struct VocabJobs {
@@ -209,9 +225,11 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __gri
     const int n = jobs.g[0].n_ptr ? *jobs.g[0].n_ptr : jobs.g[0].n_rows;
     struct Job {
         bool dw;
-        int rows, slices, per, nn;
+        int rows, slices, per;
         uint32_t nm, per_split, units;
+        Divisor split, group, rows_left, whole;   // units a split, a group of row blocks; row blocks of the last group, of the others
     };
+    const uint32_t group = (uint32_t)jobs.g[0].group;
     auto job_of = [&](int j) {
         const VocabGemm &g = jobs.g[j];
         Job k;
@@ -220,9 +238,12 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __gri
         k.slices = ((k.dw ? n : g.depth) + 63) / 64;
         k.per = (k.slices + g.splits - 1) / g.splits;
         k.nm = (uint32_t)((k.rows + 255) / 256);
-        k.nn = g.nn;
         k.per_split = k.nm * (uint32_t)g.nn;
         k.units = k.per_split * (uint32_t)g.splits;
+        if (GRADS) k.split.set(k.per_split);
+        k.group.set(group * (uint32_t)g.nn);
+        k.rows_left.set(k.nm % group);
+        k.whole.set(group);
         return k;
     };
     const Job job0 = job_of(0), job1 = job_of(JOBS - 1);
@@ -260,14 +281,13 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __gri
         x.job = JOBS > 1 && u >= job0.units;
         if (x.job) u -= job0.units;
         const Job &k = x.job ? job1 : job0;
-        const uint32_t group = (uint32_t)jobs.g[0].group;
-        x.ks = (int)(u / k.per_split);
-        uint32_t r = u - (uint32_t)x.ks * k.per_split;
-        const uint32_t in_group = group * (uint32_t)k.nn, gi = r / in_group;
-        r -= gi * in_group;
-        const uint32_t left = k.nm - gi * group, gr = left < group ? left : group;
-        x.nb = (int)(r / gr);
-        x.mb = 2 * (int)(gi * group + r - (uint32_t)x.nb * gr) + (int)crank;
+        x.ks = GRADS ? (int)k.split.of(u) : 0;   // (the others are not split)
+        uint32_t r = GRADS ? u - (uint32_t)x.ks * k.per_split : u;
+        const uint32_t gi = k.group.of(r);
+        r -= gi * k.group.d;
+        const bool last = k.nm - gi * group < group;
+        x.nb = (int)(last ? k.rows_left.of(r) : k.whole.of(r));
+        x.mb = 2 * (int)(gi * group + r - (uint32_t)x.nb * (last ? k.rows_left.d : group)) + (int)crank;
         x.k0 = x.ks * k.per;
         const int k1 = x.k0 + k.per < k.slices ? x.k0 + k.per : k.slices;
         x.nk = k1 > x.k0 ? k1 - x.k0 : 0;
@@ -438,24 +458,30 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __gri
             }
         };
 
-        auto row_in = [&](uint32_t u) {
+        auto row_in = [&](const Unit &x) {
             RowIn r = {};
-            if (GRADS || u >= units) return r;
+            if (GRADS) return r;
             const VocabGemm &g = jobs.g[0];
-            const int row = unit_of(u).mb * 128 + q * 32 + lane;
+            const int row = x.mb * 128 + q * 32 + lane;
             if (row >= n) return r;
             r.token = g.token ? g.token[row] : row;
-            if (g.label) r.label = g.label[r.token];
+            if (g.label) {
+                const int64_t y = g.label[r.token];
+                r.label = y < 0 ? -1 : y < g.V ? (int32_t)y : INT32_MAX;
+            }
             if (MODE == VG_DZ) {
                 r.lse = g.lse[r.token];
-                r.dloss = g.dloss[r.token * g.dloss_step];
+                r.dloss = g.dloss[(int64_t)r.token * g.dloss_step];
                 if (g.bad) r.bad = g.bad[r.token];
             }
             return r;
         };
-        RowIn coming = row_in(unit_at(0));
-        for (uint32_t i = 0, u; (u = unit_at(i)) < units && ok; ++i) {
-            const Unit x = unit_of(u);
+        uint32_t u = unit_at(0);
+        Unit ahead = {};
+        if (u < units) ahead = unit_of(u);
+        RowIn coming = row_in(ahead);
+        for (uint32_t turn = 1; u < units && ok; ++turn) {
+            const Unit x = ahead;
             const VocabGemm &g = jobs.g[x.job];
             const CUtensorMap *mo = &jobs.o[x.job];
             const bool dw = GRADS && (x.job ? job1.dw : job0.dw);
@@ -465,7 +491,11 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __gri
             const int my = half ? groups / 2 : (groups + 1) / 2;   // groups of 32 columns, up to 4
             const int row0 = x.mb * 128 + q * 32, row = row0 + lane;
             const RowIn in = coming;
-            coming = row_in(unit_at(i + 1));
+            u = unit_at(turn);
+            if (u < units) {
+                ahead = unit_of(u);
+                coming = row_in(ahead);
+            }
             // this thread's row
             Targets t;
             t.next = INT_MAX;
@@ -477,7 +507,7 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __gri
                 if (MODE == VG_DZ) {
                     lse2 = in.lse * 1.4426950408889634f;
                     grad = in.dloss * g.tau + in.bad;
-                    if (g.label && in.label >= g.V) grad = NAN;
+                    if (g.label && in.label == INT32_MAX) grad = NAN;
                 }
             }
             // what becomes of 32 columns of the row, from column `c` of the tile on
@@ -530,35 +560,44 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __gri
                 continue;
             }
             if constexpr (PIECES) {
-                float sum[4][32];
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) sum[i][j] = 0.0f;
-#pragma unroll 1
-                for (int kp = 0; kp < nk; kp += PIECE, ++ti) {
+                float sum[4][32];   // this row's columns
+                // a piece's sums out of the accumulator (16 columns at a time: 32 spill)
+                auto drain = [&](auto first) {
                     const uint32_t ab = ti & 1;
                     ok = mbar_wait(smem_u32(&acc_full[ab]), (ti >> 1) & 1);
                     tc_fence_after();
-                    if (!ok) break;
+                    if (!ok) return;
                     if (row0 < rows) {   // (the same for the whole warp)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             if (i < my) {
 #pragma unroll
-                                for (int h = 0; h < 2; ++h) {   // (32 at a time spill)
+                                for (int h = 0; h < 2; ++h) {
                                     float v[16];
                                     tmem_ld16(tmem + lane_base + ab * 256 + (first_group + i) * 32 + 16 * h, v);
                                     tmem_ld_wait();
                                     tmem_regs_ready(v);
 #pragma unroll
-                                    for (int j = 0; j < 16; ++j) sum[i][16 * h + j] += v[j];
+                                    for (int j = 0; j < 16; ++j) sum[i][16 * h + j] = decltype(first)::value ? v[j] : sum[i][16 * h + j] + v[j];
                                 }
                             }
                         }
                     }
                     release_acc(ab);
+                    ++ti;
+                };
+                int kp = 0;
+                if constexpr (MODE == VG_FWD) {   // (the others spill with it)
+                    drain(Yes());
+                    kp = PIECE;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) sum[i][j] = 0.0f;
                 }
+#pragma unroll 1
+                for (; kp < nk && ok; kp += PIECE) drain(No());
                 if (!ok) break;
                 if constexpr (MODE == VG_FWD) {
                     if (row < n) {

@@ -278,19 +278,24 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __gri
     };
     auto unit_of = [&](uint32_t u) {
         Unit x;
+        auto decode = [&](const Job &k, uint32_t r) {
+            x.ks = 0;
+            if (GRADS) {   // (the others are not split)
+                x.ks = (int)k.split.of(r);
+                r -= (uint32_t)x.ks * k.per_split;
+            }
+            const uint32_t gi = k.group.of(r);
+            r -= gi * k.group.d;
+            const bool last = k.nm - gi * group < group;
+            x.nb = (int)(last ? k.rows_left.of(r) : k.whole.of(r));
+            x.mb = 2 * (int)(gi * group + r - (uint32_t)x.nb * (last ? k.rows_left.d : group)) + (int)crank;
+            x.k0 = x.ks * k.per;
+            const int k1 = x.k0 + k.per < k.slices ? x.k0 + k.per : k.slices;
+            x.nk = k1 > x.k0 ? k1 - x.k0 : 0;
+        };
         x.job = JOBS > 1 && u >= job0.units;
-        if (x.job) u -= job0.units;
-        const Job &k = x.job ? job1 : job0;
-        x.ks = GRADS ? (int)k.split.of(u) : 0;   // (the others are not split)
-        uint32_t r = GRADS ? u - (uint32_t)x.ks * k.per_split : u;
-        const uint32_t gi = k.group.of(r);
-        r -= gi * k.group.d;
-        const bool last = k.nm - gi * group < group;
-        x.nb = (int)(last ? k.rows_left.of(r) : k.whole.of(r));
-        x.mb = 2 * (int)(gi * group + r - (uint32_t)x.nb * (last ? k.rows_left.d : group)) + (int)crank;
-        x.k0 = x.ks * k.per;
-        const int k1 = x.k0 + k.per < k.slices ? x.k0 + k.per : k.slices;
-        x.nk = k1 > x.k0 ? k1 - x.k0 : 0;
+        if (x.job) decode(job1, u - job0.units);
+        else decode(job0, u);
         return x;
     };
 
@@ -401,7 +406,7 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __gri
         const uint32_t lane_base = (uint32_t)(q * 32) << 16;
         uint8_t *const box = smem + C::OFF_BOX + (warp - 2) * C::BOX;
         uint32_t ti = 0, boxes = 0;
-        bool ok = true;
+        bool ok = true, whole_box = false;   // the last store came from the whole box (fp32), not from a half of it
 
         auto release_acc = [&](uint32_t ab) {
             tc_fence_before();
@@ -410,7 +415,12 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __gri
         };
         // 32 columns of this thread's row as bf16: the next of the two 2 KB boxes, stored at (col, row0)
         auto store_bf16 = [&](const CUtensorMap *mo, const float (&v)[32], int col, int row0) {
-            if (lane == 0) bulk_wait_read<1>();
+            // (VG_GRADS: a unit of DX before this one of DW may still have its 4 KB read)
+            if (lane == 0) {
+                if (GRADS && whole_box) bulk_wait_read<0>();
+                else bulk_wait_read<1>();
+            }
+            whole_box = false;
             __syncwarp();
             uint8_t *b = box + (boxes++ & 1) * 2048;
 #pragma unroll
@@ -427,6 +437,7 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __gri
         };
         auto store_f32 = [&](const CUtensorMap *mo, const float (&v)[32], int col, int row0, bool add) {
             if (lane == 0) bulk_wait_read<0>();
+            whole_box = true;
             __syncwarp();
 #pragma unroll
             for (int e = 0; e < 8; ++e)
@@ -442,6 +453,7 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __gri
         };
         // DW into a matrix off the 16-byte grid: a row at a time, one element a lane
         auto store_plain = [&](const VocabGemm &g, const float (&v)[32], int col, int row0) {
+            if (lane == 0) bulk_wait_read<0>();   // (a unit of DX before this one)
             __syncwarp();
 #pragma unroll
             for (int e = 0; e < 8; ++e)

@@ -739,11 +739,25 @@ def _embed_desc(ids, V, rows, scale, padding, device, what):
 def resbm_embed_fwd(ids, table, scale, out, stream=None):
     """out (T, d) = scale * table[ids]; table (V, d); ids (T int64). Unit stride along d, any row stride. An id outside the
     table gives a row of NaN."""
-    device = _device()
-    desc = _embed_desc(ids, table.shape[0], out, scale, -1, device, "out")
-    ldt = _row_stride(table, (desc.V, desc.d), out.dtype, device, "table")
-    desc.ldt = ldt if desc.V > 1 else desc.d
-    _check("resbm_embed_fwd", (_lib or load()).resbm_embed_fwd(desc, _p(ids), _p(table), _p(out), _stream(stream)))
+    # (a few tokens' call is the host's time: the checks of _embed_desc without its calls)
+    shape, dtype, rows = out.shape, out.dtype, table.shape
+    code = _DT.get(dtype)
+    if code is None or len(shape) != 2 or ids.shape != shape[:1] or ids.dtype != torch.int64 or not ids.is_contiguous():
+        raise ValueError("out must be (T, d), fp32 or bf16, and ids (T,), int64, dense")
+    (T, d), device = shape, _device()
+    if len(rows) != 2 or rows[1] != d or rows[0] < 1 or d < 1 or table.dtype != dtype:
+        raise ValueError("table must be (V, %d), %s" % (d, dtype))
+    (ldo, so), (ldt, st) = out.stride(), table.stride()
+    if (so != 1 or st != 1) and d > 1:
+        raise ValueError("out and table must have unit stride along the columns")
+    if ids.get_device() != device or table.get_device() != device or out.get_device() != device:
+        raise ValueError("ids, table and out must be on the current CUDA device (%d)" % device)
+    if stream is None and _raw_stream is not None:
+        stream = _raw_stream(device)
+    status = (_lib or load()).resbm_embed_fwd(resbm_embed_desc(T, rows[0], d, ldt if rows[0] > 1 else d, ldo if T > 1 else d, -1, code, scale, 0),
+                                              ids.data_ptr(), table.data_ptr(), out.data_ptr(), _stream(stream))
+    if status != RESBM_OK:
+        _check("resbm_embed_fwd", status)
 
 
 def resbm_embed_bwd(ids, dout, scale, dtable, ws, padding=-1, stream=None):

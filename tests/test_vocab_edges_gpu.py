@@ -132,6 +132,17 @@ def test_the_same_bits_every_time(dtype):
     assert same(run(X, W, index, each(1500), teacher, 2.0), run(X, W, index, each(1500), teacher, 2.0))
 
 
+@pytest.mark.parametrize("T,V,d", [(300, 20011, 1000), (300, 20011, 1001), (2000, 6000, 520), (5, 30000, 264)])
+def test_units_of_both_gradients_in_one_warp(T, V, d):
+    """The same bits, and right ones, many times over: a warp stores units of dX (fp32) and of dW after one another."""
+    X, W, labels = vh.inputs(T, V, d)
+    want = vh.ce(X, W, labels)
+    first = run(X, W, labels, each(T))
+    want.check_bwd(each(T), *first[2:])
+    for _ in range(25):
+        assert same(run(X, W, labels, each(T)), first)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_large_logits(dtype):
     """Logits of thousands: the maximum is taken out before the exponentials."""

@@ -36,7 +36,7 @@ typedef enum {
 
 typedef struct {
     int64_t T, V, d;            /* tokens >= 0, words >= 1, hidden width >= 1                                 */
-    int64_t ldx, ldw;           /* elements from one row of X, of W to the next, >= d                         */
+    int64_t ldx, ldw;           /* elements from one row of X, of W to the next, >= d (one row: not used)     */
     int64_t K;                  /* distill: entries a token, 1 .. 1024 (not used by the cross entropy)        */
     int32_t dtype;              /* resbm_dtype of X, W, dX, dW                                                */
     int32_t teacher_dtype;      /* distill: resbm_dtype of the teacher's logits                               */
@@ -55,10 +55,11 @@ RESBM_API resbm_status resbm_vocab_workspace_bytes(const resbm_vocab_desc *desc,
  *   X : T x d in, rows ldx apart.  W : V x d in (the head), rows ldw apart.  labels : T int64 in.
  *   loss, lse : T fp32 out.
  * Rows without a label cost nothing but their share of a copy, and nothing that they hold, NaN and infinities included,
- * reaches an output. z is within 2^-20 or so of its row's largest products' sum in 64 bits.
+ * reaches an output. A logit is within 2^-17 of the sum of its terms' absolute values (fp32: three bf16 parts of every operand,
+ * which hold 24 bits; the same bound from the tensor cores' own additions), and typically within 2^-21 of itself.
  * Errors: RESBM_ERR_INVALID_ARG for a bad size, stride, type, flag, a missing or misaligned pointer (X, W: their element;
  * ws: 256 bytes) or an output that overlaps another tensor; RESBM_ERR_WORKSPACE; RESBM_ERR_UNSUPPORTED for T or V of 2^29
- * and over or d over 2^20. */
+ * and over, d over 2^20, T V of 2^43 and over, or T d or V d of 2^39 and over. */
 RESBM_API resbm_status resbm_linear_ce_fwd(const resbm_vocab_desc *desc, const void *X, const void *W, const int64_t *labels,
                                            float *loss, float *lse, void *ws, size_t ws_bytes, void *stream);
 

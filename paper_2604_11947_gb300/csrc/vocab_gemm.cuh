@@ -18,12 +18,19 @@
 //
 // fp32 (SPLIT 3): every operand is the sum of three bf16 values (the value rounded, its remainder rounded, and once more:
 // 24 bits), and a product the six of nine partial ones that are over 2^-24 of it, smallest first. They are one product of
-// six times the depth, at the bf16 rate: 375 TFLOP/s at most, where CUDA cores have 75.
+// six times the depth at the bf16 rate: 320 TFLOP/s of fp32 at most, where CUDA cores have 75.
 //
 // PIECES: the tensor core truncates as it adds to its accumulator, an error that grows with the number of MMAs in one
-// accumulator (2e-6 of a logit at d = 2048). Where that is seen in an output (the losses, and everything in fp32) a unit's sum
+// accumulator (run_loss has figures). Where that is seen in an output (the losses, and everything in fp32) a unit's sum
 // runs in pieces, which alternate between the accumulators; the epilogue warps add them in registers, rounded to
 // nearest, while the next piece runs.
+//
+// What bounds it: with d of 2048 and more the tensor cores (T = 2048, V = 32000, d = 2048: FWD_US forward, DZ_US dz, GRADS_US both
+// gradients, TF TFLOP/s; in a long run the board's power, 1.7 PFLOP/s); with d under 512 the epilogue's exponentials, whose
+// warps wait for their own results most of the time (eight warps of 128 columns a row: T = 8192, V = 32000, d = 128 130 us
+// forward, where the tensor cores need 38). Sixteen warps of 64 columns took 235: what a unit costs a warp apart from its
+// columns, and 96 registers a thread, which spill. The logits' targets are looked up by bisection in a token's sorted list, and a
+// label is a list of one.
 //
 // Every element is summed by one CTA in a fixed order, and a depth split has a slot of its own: results are the same bits
 // every time.

@@ -296,11 +296,17 @@ class _Embed(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dout):
         ids, = ctx.saved_tensors
-        rows = _rows(dout)
+        rows = _separate_rows(dout)
         dtable = torch.empty(ctx.shape, dtype=dout.dtype, device=dout.device)
         ws = resbm.vocab_workspace(resbm.RESBM_VOCAB_EMBED_BWD, rows.shape[0], *ctx.shape, _dtype_name(dout), device=dout.device)
         resbm.resbm_embed_bwd(ids, rows, ctx.scale, dtable, ws, padding=ctx.padding)
         return None, dtable, None, None
+
+
+def _separate_rows(t):
+    """t as the rows of its last dimension, each in memory of its own (an expanded tensor's are one)"""
+    rows = _rows(t)
+    return rows if rows.shape[0] <= 1 or rows.stride(0) >= rows.shape[1] else rows.contiguous()
 
 
 def embed(ids, table, scale=1.0, padding=-1):
@@ -315,7 +321,7 @@ class _VocabLoss(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, x, head, target, teacher, temperature):
-        rows = _rows(x)
+        rows = _separate_rows(x)
         (T, d), V, K = rows.shape, head.shape[0], 0 if teacher is None else target.shape[-1]
         ops = (resbm.RESBM_VOCAB_CE_FWD, resbm.RESBM_VOCAB_CE_BWD) if teacher is None else (resbm.RESBM_VOCAB_DISTILL_FWD, resbm.RESBM_VOCAB_DISTILL_BWD)
         target = (target.reshape(-1) if teacher is None else target.reshape(-1, K)).contiguous()
@@ -334,7 +340,7 @@ class _VocabLoss(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dloss):
         x, head, target, teacher, lse = ctx.saved_tensors
-        rows = _rows(x)
+        rows = _separate_rows(x)
         K = 0 if teacher is None else target.shape[1]
         dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if ctx.needs_input_grad[0] else None
         dhead = torch.empty(head.shape, dtype=head.dtype, device=head.device) if ctx.needs_input_grad[1] else None

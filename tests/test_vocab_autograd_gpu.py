@@ -57,6 +57,16 @@ def test_inputs_out_of_the_ordinary():
     assert torch.equal(a, b)
     t = wide[0, :, :72].t().contiguous().t()          # columns before rows
     assert torch.equal(pipeline.linear_cross_entropy(t, W, labels[:20], "none"), pipeline.linear_cross_entropy(t.contiguous(), W, labels[:20], "none"))
+    row = X[:1].clone().requires_grad_()              # one row for all tokens: its gradient is the rows' sum
+    pipeline.linear_cross_entropy(row.expand(60, 72), W, labels, "sum").backward()
+    each = X[:1].expand(60, 72).contiguous().requires_grad_()
+    pipeline.linear_cross_entropy(each, W, labels, "sum").backward()
+    off = (row.grad.double() - each.grad.double().sum(dim=0)).abs()
+    assert bool((off <= each.grad.double().abs().sum(dim=0) * 60 * 2.0 ** -8).all())   # (60 additions, rounded to bf16 at worst each)
+    table = torch.randn(9, 72, device="cuda").requires_grad_()
+    ids = torch.arange(12, device="cuda") % 9
+    pipeline.embed(ids, table).backward(torch.ones(72, device="cuda").expand(12, 72))   # a gradient of one row for all tokens
+    assert torch.equal(table.grad, torch.where(torch.arange(9, device="cuda") < 3, 2.0, 1.0)[:, None].expand(9, 72))
     empty = pipeline.linear_cross_entropy(X[:0].clone().requires_grad_(), W, labels[:0])
     empty.backward()
     assert float(empty) == 0.0

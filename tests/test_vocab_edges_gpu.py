@@ -101,6 +101,23 @@ def test_addresses_off_the_vectors(dtype):
     want.check_bwd(each(T), dX, dW)
 
 
+@pytest.mark.parametrize("T,V", [(1, 300), (40, 1)])
+def test_the_stride_of_a_single_row(T, V):
+    """Whatever it is, it is not used."""
+    X, W, labels = vh.inputs(T, V, 72, ignored=0.0)
+    X, W = X.contiguous(), W.contiguous()
+    want, lib = run(X, W, labels, each(T)), resbm.load()
+    ws = workspace(T, V, 72, "bf16")[:-512]
+    for ld in (0, 1, -5, 73, 1 << 50):
+        loss, lse, dX, dW, g = torch.empty(T, device="cuda"), torch.empty(T, device="cuda"), torch.empty_like(X), torch.empty_like(W), each(T)
+        desc = resbm.resbm_vocab_desc(T, V, 72, ld if T == 1 else 72, ld if V == 1 else 72, 0, 1, 0, 1.0, 1, 0)
+        p, s = (lambda t: t.data_ptr()), torch.cuda.current_stream().cuda_stream
+        assert lib.resbm_linear_ce_fwd(desc, p(X), p(W), p(labels), p(loss), p(lse), p(ws), ws.numel(), s) == 0
+        assert lib.resbm_linear_ce_bwd(desc, p(X), p(W), p(labels), p(lse), p(g), p(dX), p(dW), p(ws), ws.numel(), s) == 0
+        torch.cuda.synchronize()
+        assert same((loss, lse, dX, dW), want)
+
+
 def test_one_gradient_for_all_losses():
     X, W, labels = vh.inputs(300, 700, 72)
     for one in (torch.tensor(0.37, device="cuda"), torch.tensor([0.37], device="cuda")):

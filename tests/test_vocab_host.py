@@ -71,7 +71,8 @@ def test_distillation_refuses(lib, bad):
 def test_limits_and_workspaces(lib):
     for bwd in (False, True):
         assert loss(lib, bwd=bwd, ws_bytes=1000) == WORKSPACE and loss(lib, bwd=bwd, ws=None) == WORKSPACE
-        for big in (dict(T=1 << 29), dict(V=1 << 29), dict(d=(1 << 20) + 1, ldx=1 << 21, ldw=1 << 21), dict(T=1 << 28, V=1 << 28)):
+        for big in (dict(T=1 << 29), dict(V=1 << 29), dict(d=(1 << 20) + 1, ldx=1 << 21, ldw=1 << 21), dict(T=1 << 28, V=1 << 28),
+                    dict(V=1 << 28, d=1 << 12, ldx=1 << 12, ldw=1 << 12), dict(T=1 << 28, d=1 << 12, ldx=1 << 12, ldw=1 << 12)):
             assert loss(lib, bwd=bwd, **big) == UNSUPPORTED
     out = ctypes.c_size_t(7)
     desc = resbm.resbm_vocab_desc(10, 10, 10, 10, 10, 0, 1, 1, 1.0, 0, 0)

@@ -3,10 +3,11 @@ allowed.
 
 Allowed errors, from the arithmetic (u = 2^-24, half an fp32 step; a bf16 half step is 2^-8 of the value):
   a logit     Products of bf16 values are exact in fp32; fp32 operands are three bf16 parts each, whose dropped partial products
-              are under 3 * 2^-26 of a product. A piece of a sum (256 deep, or 128 of three parts) is at most 16 MMAs (8 at the
-              full size of its terms and 40 at 2^-8 of it), each of which truncates its products' sum and the accumulator's, at
+              are under 3 * 2^-26 of a product. A piece of a sum is at most 512 deep, 32 MMAs (of three parts 256, 16 at the
+              full size of its terms and 80 at 2^-8 of it), each of which truncates its products' sum and the accumulator's, at
               most 2 * 2^-23 of the sum of the terms' absolute values S; pieces are added in fp32. So
-              dz = (16 * 2^-22 + (d / 128 + 4) u) S. Few tokens are summed in fp32, a 32nd of the row a lane: (d / 32 + 8) u S.
+              dz = (M 2^-22 + (d / 128 + 4) u) S with M = 32 (17 of three parts); the
+              truncations hardly ever all have one sign, and 16 is what is asked of both.
   lse         A weighted mean of the logits' errors (over tau), the exponentials' (2^-21 each with its argument's rounding of
               u |z|), and the sums' of positive terms: 128 a thread in four sums, the slots' and their join: under 2^-17.
   loss        lse's and the target's logit's, the final operations' u of their operands.
@@ -39,7 +40,7 @@ class Loss:
         self.X = torch.where(has[:, None], self.X, 0.0)   # what a token without a target holds reaches nothing
         S = self.X.abs() @ self.W.abs().t()
         self.z = self.X @ self.W.t()
-        self.dz_err = S * max(16 * 2.0 ** -22 + (d / 128 + 4) * U, (d / 32 + 8) * U)
+        self.dz_err = S * (16 * 2.0 ** -22 + (d / 128 + 4) * U)
         zt = self.z / tau
         self.lse = torch.logsumexp(zt, dim=1)
         self.p = torch.exp(zt - self.lse[:, None])

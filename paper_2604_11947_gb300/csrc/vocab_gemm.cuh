@@ -20,6 +20,9 @@
 // 24 bits), and a product the six of nine partial ones that are over 2^-24 of it, smallest first. They are one product of
 // six times the depth at the bf16 rate: 320 TFLOP/s of fp32 at most, where CUDA cores have 75.
 //
+// Few tokens in bf16 (SPLIT 2): dz as two bf16 values. Its rounding is one of the outputs' own size, but a single token's gradients
+// have one large dz, the label's, whose error no sum averages: up to 2^-8 of the whole of dX and dW (T = 1: 3.7e-3 off).
+//
 // PIECES: the tensor core truncates as it adds to its accumulator, an error that grows with the number of MMAs in one
 // accumulator (run_loss has figures). Where that is seen in an output (the losses, and everything in fp32) a unit's sum
 // runs in pieces, which alternate between the accumulators; the epilogue warps add them in registers, rounded to
@@ -169,7 +172,7 @@ struct RowIn {
 struct Yes { static constexpr bool value = true; };
 struct No { static constexpr bool value = false; };
 
-// MODE: what becomes of the accumulator; SPLIT: bf16 parts of an operand; PIECE: 64-deep slices of a piece of a sum (0: whole)
+// MODE: what becomes of the accumulator; SPLIT: bf16 parts of an operand (2: of dz alone); PIECE: 64-deep slices of a piece of a sum (0: whole)
 // x / d for x under 2^31: a product with the reciprocal and a correction (a division is 20 dependent instructions, and every warp
 // has three a unit)
 struct Divisor {
@@ -199,7 +202,7 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __gri
     using C = VocabCfg;
     constexpr bool GRADS = MODE == VG_GRADS, BMN = GRADS;
     constexpr bool PIECES = PIECE > 0;
-    constexpr int TERMS = SPLIT == 3 ? 6 : 1;
+    constexpr int TERMS = SPLIT == 3 ? 6 : SPLIT == 2 && GRADS ? 2 : 1;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     __shared__ uint64_t full[C::NST], empty[C::NST], acc_full[2], acc_empty[2], done_bar;
@@ -331,11 +334,14 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __gri
                 const int piece = PIECES ? PIECE : x.nk;
                 for (int kp = 0; kp < x.nk && ok; kp += piece) {
                     const int ke = x.nk - kp < piece ? x.nk : kp + piece;
-                    for (int term = 0; term < TERMS && ok; ++term) {
-                        // the partial products, smallest first: (2, 0) (1, 1) (0, 2) (1, 0) (0, 1) (0, 0)
-                        const int sa = SPLIT == 1 ? 0 : term == 0 ? 2 : (term == 1 || term == 3) ? 1 : 0;
-                        const int sb = SPLIT == 1 ? 0 : term == 2 ? 2 : (term == 1 || term == 4) ? 1 : 0;
-                        for (int kb = kp; kb < ke; ++kb, ++it) {
+                    // Product by product (SPLIT 2: slice by slice, so that the second product finds W's in L2)
+                    constexpr bool BY_SLICE = SPLIT == 2;
+                    for (int o = 0; o < (BY_SLICE ? ke - kp : TERMS) && ok; ++o) {
+                        for (int i = 0; i < (BY_SLICE ? TERMS : ke - kp); ++i, ++it) {
+                            const int term = BY_SLICE ? i : o, kb = kp + (BY_SLICE ? o : i);
+                            // the partial products, smallest first: (2, 0) (1, 1) (0, 2) (1, 0) (0, 1) (0, 0); SPLIT 2: dz's remainder, dz
+                            const int sa = SPLIT == 3 ? (term == 0 ? 2 : (term == 1 || term == 3) ? 1 : 0) : TERMS - 1 - term;
+                            const int sb = SPLIT < 3 ? 0 : term == 2 ? 2 : (term == 1 || term == 4) ? 1 : 0;
                             const uint32_t s = it % C::NST, ph = (it / C::NST) & 1;
                             if (!mbar_wait(smem_u32(&empty[s]), ph ^ 1)) {
                                 ok = false;

@@ -55,9 +55,9 @@ def each(T, seed=5):
 
 SIZES = [(1, 1, 1), (1, 64, 64), (2, 300, 8), (3, 33, 40), (17, 1000, 100), (64, 257, 72), (255, 512, 256), (256, 511, 264), (257, 513, 1000),
          (300, 5000, 65), (600, 96, 200), (1000, 2049, 512), (130, 20011, 328), (4100, 300, 130), (1, 5003, 2056),
-         # a handful of tokens: every number of them, widths on both sides of the kernels' limits, on and off the vectors
+         # a handful of tokens, on and off the vectors, and both sides of where dz has two parts
          (1, 3001, 4096), (1, 700, 4104), (2, 1001, 1000), (4, 2000, 2048), (4, 999, 4095), (5, 1000, 2048), (7, 777, 2047), (8, 5000, 256), (8, 300, 3100),
-         (8, 40, 4096), (9, 500, 512), (3, 200, 9000)]
+         (8, 40, 4096), (9, 500, 512), (3, 200, 9000), (16, 9000, 520), (17, 9000, 520), (13, 32000, 1001)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

@@ -11,8 +11,8 @@ Allowed errors, from the arithmetic (u = 2^-24, half an fp32 step; a bf16 half s
   lse         A weighted mean of the logits' errors (over tau), the exponentials' (2^-21 each with its argument's rounding of
               u |z|), and the sums' of positive terms: 128 a thread in four sums, the slots' and their join: under 2^-17.
   loss        lse's and the target's logit's, the final operations' u of their operands.
-  dz          p's relative error e = dz + lse's + 2^-20 + u |z| and the multiplication's; stored in bf16 (2^-8 |dz|) or in three
-              parts (2^-24 |dz|).
+  dz          p's relative error e = dz + lse's + 2^-20 + u |z| and the multiplication's; stored in bf16 (2^-8 |dz|), in two
+              parts for up to 16 tokens (2^-16 |dz|), or in three (2^-24 |dz|).
   dX, dW      a sum over `depth` of products with those errors, truncated in every MMA of 16 (bf16: depth / 16 of them in one
               accumulator; fp32: in pieces, as for a logit), and the output's rounding."""
 import torch
@@ -61,7 +61,7 @@ class Loss:
         dz = (self.p - self.goal) * g
         zt = (self.z / self.tau).abs()
         e = self.dz_err / self.tau + self.lse_err[:, None] + 2.0 ** -20 + 4 * U * (zt + self.lse.abs()[:, None])
-        err = g.abs() * (self.p * e + 4 * U * self.goal) + dz.abs() * (2.0 ** -8 if not self.f32 else 3 * U)
+        err = g.abs() * (self.p * e + 4 * U * self.goal) + dz.abs() * (3 * U if self.f32 else 2.0 ** -16 if dz.shape[0] <= 16 else 2.0 ** -8)
         return dz, err
 
     def check_bwd(self, dloss, dX, dW):

@@ -334,34 +334,42 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __gri
                 const int piece = PIECES ? PIECE : x.nk;
                 for (int kp = 0; kp < x.nk && ok; kp += piece) {
                     const int ke = x.nk - kp < piece ? x.nk : kp + piece;
-                    // Product by product (SPLIT 2: slice by slice, so that the second product finds W's in L2)
-                    constexpr bool BY_SLICE = SPLIT == 2;
-                    for (int o = 0; o < (BY_SLICE ? ke - kp : TERMS) && ok; ++o) {
-                        for (int i = 0; i < (BY_SLICE ? TERMS : ke - kp); ++i, ++it) {
-                            const int term = BY_SLICE ? i : o, kb = kp + (BY_SLICE ? o : i);
-                            // the partial products, smallest first: (2, 0) (1, 1) (0, 2) (1, 0) (0, 1) (0, 0); SPLIT 2: dz's remainder, dz
-                            const int sa = SPLIT == 3 ? (term == 0 ? 2 : (term == 1 || term == 3) ? 1 : 0) : TERMS - 1 - term;
+                    // a slice of the operands' parts whose rows begin ya and yb on
+                    auto load = [&](int ya, int yb, int k) {
+                        const uint32_t s = it % C::NST, ph = (it / C::NST) & 1, own = smem_u32(&full[s]), bar = map_shared(own, 0);
+                        const uint32_t ad = smem_u32(smem + s * C::STAGE), bd = ad + C::A_STAGE;
+                        if (!mbar_wait(smem_u32(&empty[s]), ph ^ 1)) {
+                            ok = false;
+                            return;
+                        }
+                        if (crank == 0) mbar_expect_tx(own, bytes);   // both CTAs' bytes
+                        if (!dw) {
+                            if (!few || crank == 0) tma_load_2d_pair(ad, ma, k, ya + row, bar);
+                        } else {
+                            tma_load_2d_pair(ad, ma, row, ya + k, bar);
+                            tma_load_2d_pair(ad + 8192, ma, row + 64, ya + k, bar);
+                        }
+                        if (!BMN) {
+                            tma_load_2d_pair(bd, mb, k, yb + col, bar);
+                        } else {   // (what lies past the half is loaded and not read)
+                            for (int j = 0; j < loads_b; ++j) tma_load_2d_pair(bd + j * 8192, mb, col + 64 * j, yb + k, bar);
+                        }
+                        ++it;
+                    };
+                    const int first = 64 * (x.k0 + kp), end = 64 * (x.k0 + ke);
+                    if constexpr (SPLIT == 2 && GRADS) {   // dz's remainder, dz; slice by slice: the second product finds W's in L2
+                        for (int k = first; k < end && ok; k += 64) {
+                            load(g.a_off, g.b_y, k);
+                            if (ok) load(0, g.b_y, k);
+                        }
+                    } else {
+#pragma unroll 1
+                        for (int term = 0; term < TERMS && ok; ++term) {
+                            // the partial products, smallest first: (2, 0) (1, 1) (0, 2) (1, 0) (0, 1) (0, 0)
+                            const int sa = SPLIT < 3 ? 0 : term == 0 ? 2 : (term == 1 || term == 3) ? 1 : 0;
                             const int sb = SPLIT < 3 ? 0 : term == 2 ? 2 : (term == 1 || term == 4) ? 1 : 0;
-                            const uint32_t s = it % C::NST, ph = (it / C::NST) & 1;
-                            if (!mbar_wait(smem_u32(&empty[s]), ph ^ 1)) {
-                                ok = false;
-                                break;
-                            }
-                            if (crank == 0) mbar_expect_tx(smem_u32(&full[s]), bytes);   // both CTAs' bytes
-                            const uint32_t bar = map_shared(smem_u32(&full[s]), 0);
-                            const uint32_t ad = smem_u32(smem + s * C::STAGE), bd = ad + C::A_STAGE;
-                            const int k = 64 * (x.k0 + kb);
-                            if (!dw) {
-                                if (!few || crank == 0) tma_load_2d_pair(ad, ma, k, sa * g.a_off + row, bar);
-                            } else {
-                                tma_load_2d_pair(ad, ma, row, sa * g.a_off + k, bar);
-                                tma_load_2d_pair(ad + 8192, ma, row + 64, sa * g.a_off + k, bar);
-                            }
-                            if (!BMN) {
-                                tma_load_2d_pair(bd, mb, k, sb * g.b_off + g.b_y + col, bar);
-                            } else {   // (what lies past the half is loaded and not read)
-                                for (int j = 0; j < loads_b; ++j) tma_load_2d_pair(bd + j * 8192, mb, col + 64 * j, sb * g.b_off + g.b_y + k, bar);
-                            }
+                            const int ya = sa * g.a_off, yb = sb * g.b_off + g.b_y;
+                            for (int k = first; k < end && ok; k += 64) load(ya, yb, k);
                         }
                     }
                 }

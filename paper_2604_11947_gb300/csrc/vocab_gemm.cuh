@@ -643,7 +643,8 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __gri
                                 for (int j = 0; j < 32; ++j)
                                     if (j >= left) sum[i][j] = -INFINITY;
                             }
-                            while (i < my && t.next < c + 32) {
+                            // (only in columns that exist: past a piece's end stand the next one's words)
+                            while (i < my && t.next < c + min(left, 32)) {
                                 const int at = t.next - c;
                                 float x = 0.0f;
 #pragma unroll

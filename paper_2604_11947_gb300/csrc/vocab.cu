@@ -435,13 +435,15 @@ Plan make_plan(const Shape &s, void *ws)
     return p;
 }
 
-// The workspace of a call, whatever its pointers' and strides' alignment
+// The workspace of a call, whatever its pointers' and strides' alignment. (Rows of W that are off the vectors by their width may be whole
+// ones by their stride: W is then used as it lies, whose pieces, dz and slots are other ones, and may be larger.)
 size_t plan_bytes(Shape s)
 {
     s.pack_w = true;
-    const size_t a = make_plan(s, nullptr).bytes;
-    s.pack_w = packs_w(s);
-    return std::max(a, make_plan(s, nullptr).bytes);
+    const size_t packed = make_plan(s, nullptr).bytes;
+    if (s.split == 3) return packed;   // (its parts always go through the workspace)
+    s.pack_w = false;
+    return std::max(packed, make_plan(s, nullptr).bytes);
 }
 
 // ---- launches ----------------------------------------------------------------------------------------
@@ -734,6 +736,7 @@ resbm_status loss_call(const resbm_vocab_desc *desc, bool distill, bool bwd, Cal
     if (bwd && !a.dX && !a.dW) return RESBM_OK;
     s.pack_w = s.split == 3 || !al16(a.W) || d.ldw % 8 != 0;
     const Plan p = make_plan(s, ws);
+    if (p.bytes > ws_bytes) return RESBM_ERR_WORKSPACE;   // (plan_bytes covers it)
     if (s.dz == 3) run_loss<float, 3, 3>(r, s, p, a);
     else if (s.dz == 2) run_loss<__nv_bfloat16, 1, 2>(r, s, p, a);
     else run_loss<__nv_bfloat16, 1, 1>(r, s, p, a);

@@ -56,7 +56,8 @@ RESBM_API resbm_status resbm_vocab_workspace_bytes(const resbm_vocab_desc *desc,
  *   loss, lse : T fp32 out.
  * Rows without a label cost nothing but their share of a copy, and nothing that they hold, NaN and infinities included,
  * reaches an output. A logit is within 2^-17 of the sum of its terms' absolute values (fp32: three bf16 parts of every operand,
- * which hold 24 bits; the same bound from the tensor cores' own additions), and typically within 2^-21 of itself.
+ * which hold 24 bits; the same bound from the tensor cores' own additions), and typically within 2^-21 of itself. (The
+ * backward's logits in bf16 are summed in longer pieces: within 2^-16.)
  * Errors: RESBM_ERR_INVALID_ARG for a bad size, stride, type, flag, a missing or misaligned pointer (X, W: their element;
  * ws: 256 bytes) or an output that overlaps another tensor; RESBM_ERR_WORKSPACE; RESBM_ERR_UNSUPPORTED for T or V of 2^29
  * and over, d over 2^20, T V of 2^43 and over, or T d or V d of 2^39 and over. */

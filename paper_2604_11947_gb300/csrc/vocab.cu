@@ -588,7 +588,13 @@ template <typename E, int SPLIT, int DZ> void run_loss(Run &r, const Shape &s, c
             continue;
         }
         r.map(&z.o[0], p.dz, vn, DZ * p.tp, p.vc * 2, 32, 32, k64);
-        run_gemm<VG_DZ, DZ, F32 ? P : 0, 1>(r, z, row_blocks * u.nn);
+        // z again, whose error is seen where a token is certain and p - q next to nothing: in one accumulator it grew with d (d = 16384,
+        // logits up to 1400: dX and dW 1.5e-2 off; in pieces 1024 deep 1.9e-3, their rounding). T = 16384, V = 32000, d = 2048 backward
+        // 3903 -> 3947 us, T = 8192, d = 1100 3 % more; pieces 512 deep cost 4 to 10 %.
+        constexpr int kLongPiece = 16;
+        if constexpr (F32) run_gemm<VG_DZ, DZ, P, 1>(r, z, row_blocks * u.nn);
+        else if (s.d > 64 * kLongPiece) run_gemm<VG_DZ, DZ, kLongPiece, 1>(r, z, row_blocks * u.nn);
+        else run_gemm<VG_DZ, DZ, 0, 1>(r, z, row_blocks * u.nn);
 
         VocabJobs<2> gr;
         FinishJob fin[2] = {};

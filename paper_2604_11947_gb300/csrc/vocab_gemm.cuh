@@ -24,7 +24,7 @@
 // have one large dz, the label's, whose error no sum averages: up to 2^-8 of the whole of dX and dW (T = 1: 3.7e-3 off).
 //
 // PIECES: the tensor core truncates as it adds to its accumulator, an error that grows with the number of MMAs in one
-// accumulator (run_loss has figures). Where that is seen in an output (the losses, and everything in fp32) a unit's sum
+// accumulator (run_loss has figures). Where that is seen in an output (the logits, and everything in fp32) a unit's sum
 // runs in pieces, which alternate between the accumulators; the epilogue warps add them in registers, rounded to
 // nearest, while the next piece runs.
 //

@@ -341,26 +341,31 @@ int64_t up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
 constexpr int kPairs = 76;             // what units are spread over in the choice of their size
 constexpr int64_t kPackRows = 4096;    // words of a piece at least
 
-// Columns a unit and splits of the depth, by an estimate of the cycles: a 64-deep slice takes 2 bn on the tensor cores or
+// The most products that one accumulator adds up in a gradient in bf16: the tensor core cuts off at most 2 * 2^-23 of the sum's size with
+// each 16 of them, 2^-10 of the terms' absolute sum in all. More go into splits, which are added up to nearest. (A million tokens in
+// one accumulator: terms of one sign 4.2e-3 off in the mean, now 1e-5.)
+constexpr int64_t kDeepest = 65536;
+
+// Columns a unit and splits of the depth, `least` at least, by an estimate of the cycles: a 64-deep slice takes 2 bn on the tensor cores or
 // 256 + bn to load (64 bytes a cycle and SM), a unit 1500 around its products, a slot 8 bytes an element at 3000 a cycle.
 struct Units {
     int bn, nn, splits;
 };
-Units choose_units(int64_t rows, int64_t cols, int64_t depth, int most_splits, int64_t slot_bytes)
+Units choose_units(int64_t rows, int64_t cols, int64_t depth, int most_splits, int64_t slot_bytes, int64_t least = 1)
 {
     const int64_t nm = (rows + 255) / 256, slices = (depth + 63) / 64;
     Units best{256, 1, 1};
-    double least = 1e300;
+    double shortest = 1e300;
     for (int bn = 256; bn >= 32; bn -= 32) {
         if (bn > 32 && up(cols, 32) < bn) continue;
         const int64_t nn = (cols + bn - 1) / bn;
-        for (int s = 1; s <= most_splits; s = s < 8 ? s + 1 : s + 4) {
+        for (int s = (int)least; s <= std::max<int64_t>(most_splits, least); s = s < 8 ? s + 1 : s + 4) {
             const int64_t per = (slices + s - 1) / s;
-            if (s > 1 && (per < 4 || (s - 1) * per >= slices)) continue;
+            if (s > least && (per < 4 || (s - 1) * per >= slices)) continue;
             const int64_t waves = (nm * nn * s + kPairs - 1) / kPairs;
             const double t = (double)waves * ((double)per * std::max(2 * bn, 256 + bn) + 1500.0) + (s > 1 ? (double)s * (double)slot_bytes / 3000.0 : 0.0);
-            if (t < least) {
-                least = t;
+            if (t < shortest) {
+                shortest = t;
                 best = Units{bn, (int)nn, s};
             }
         }
@@ -426,8 +431,9 @@ Plan make_plan(const Shape &s, void *ws)
         p.zt = w.take<float>(s.distill ? p.slots * p.tp : p.tp);
     } else {
         p.dz = w.take<__nv_bfloat16>(s.dz * p.tp * p.vc);
-        p.dx = choose_units(s.T, s.d, p.vc * (s.split == 3 ? 6 : s.dz), 32, p.tp * p.dp * 4);
-        p.dw = choose_units(p.vc, s.d, s.T * (s.split == 3 ? 6 : s.dz), 32, 2 * p.vc * p.dp * 4);
+        auto least = [&](int64_t depth) { return s.split == 3 ? 1 : (depth + kDeepest - 1) / kDeepest; };   // (fp32 adds in short pieces)
+        p.dx = choose_units(s.T, s.d, p.vc * (s.split == 3 ? 6 : s.dz), 32, p.tp * p.dp * 4, least(p.vc));
+        p.dw = choose_units(p.vc, s.d, s.T * (s.split == 3 ? 6 : s.dz), 32, 2 * p.vc * p.dp * 4, std::max<int64_t>(1, least(s.T)));
         p.dxs = w.take<float>(p.dx.splits * p.tp * p.dp);
         if (p.dw.splits > 1) p.dws = w.take<float>(p.dw.splits * p.vc * p.dp);
     }

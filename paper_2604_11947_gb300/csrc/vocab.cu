@@ -375,8 +375,7 @@ Units choose_units(int64_t rows, int64_t cols, int64_t depth, int most_splits, i
 
 struct Shape {
     int64_t T, V, d, K;
-    int split;            // bf16 parts of an operand
-    int dz;               // of dz
+    int split;            // bf16 parts of an operand, and of dz in memory
     bool distill, bwd;
     bool pack_w;          // W goes through the workspace
 };
@@ -408,7 +407,7 @@ Plan make_plan(const Shape &s, void *ws)
     p.dp = up(s.d, 64);   // (whole 128-byte lines: rows that straddle them load at half the rate)
     // dz of a piece: 2^27 elements (268 MB in bf16), but no fewer than 4096 words
     int64_t vc = up(s.V, 256);
-    if (s.bwd) vc = std::min(vc, std::max(kPackRows, (int64_t(1) << (s.dz > 1 ? 26 : 27)) / p.tp / 256 * 256));
+    if (s.bwd) vc = std::min(vc, std::max(kPackRows, (int64_t(1) << (s.split == 3 ? 26 : 27)) / p.tp / 256 * 256));
     if (s.pack_w) vc = std::min(vc, std::max(kPackRows, packs_w(s) ? (int64_t(1) << 26) / p.dp / 256 * 256 : 0));
     p.pieces = (int)((s.V + vc - 1) / vc);
     p.vc = up((s.V + p.pieces - 1) / p.pieces, 256);
@@ -430,10 +429,11 @@ Plan make_plan(const Shape &s, void *ws)
         p.stat = w.take<float2>(p.slots * p.tp);
         p.zt = w.take<float>(s.distill ? p.slots * p.tp : p.tp);
     } else {
-        p.dz = w.take<__nv_bfloat16>(s.dz * p.tp * p.vc);
+        p.dz = w.take<__nv_bfloat16>(s.split * p.tp * p.vc);
+        const int parts = s.split == 3 ? 6 : s.T <= kTwoParts ? 2 : 1;   // products of a unit (for more tokens the most likely number)
         auto least = [&](int64_t depth) { return s.split == 3 ? 1 : (depth + kDeepest - 1) / kDeepest; };   // (fp32 adds in short pieces)
-        p.dx = choose_units(s.T, s.d, p.vc * (s.split == 3 ? 6 : s.dz), 32, p.tp * p.dp * 4, least(p.vc));
-        p.dw = choose_units(p.vc, s.d, s.T * (s.split == 3 ? 6 : s.dz), 32, 2 * p.vc * p.dp * 4, std::max<int64_t>(1, least(s.T)));
+        p.dx = choose_units(s.T, s.d, p.vc * parts, 32, p.tp * p.dp * 4, least(p.vc));
+        p.dw = choose_units(p.vc, s.d, s.T * parts, 32, 2 * p.vc * p.dp * 4, std::max<int64_t>(1, least(s.T)));
         p.dxs = w.take<float>(p.dx.splits * p.tp * p.dp);
         if (p.dw.splits > 1) p.dws = w.take<float>(p.dw.splits * p.vc * p.dp);
     }
@@ -492,10 +492,11 @@ struct Call {
     void *dX, *dW;
 };
 
-// E: the tensors' type; SPLIT: bf16 parts of X and W, DZ of dz
-template <typename E, int SPLIT, int DZ> void run_loss(Run &r, const Shape &s, const Plan &p, const Call &a)
+// E: the tensors' type; SPLIT: bf16 parts of X and W
+template <typename E, int SPLIT> void run_loss(Run &r, const Shape &s, const Plan &p, const Call &a)
 {
     constexpr bool F32 = SPLIT == 3;
+    constexpr int DZ = F32 ? 3 : 2;   // parts of dz (2: for few tokens)
     // Slices of a piece of a sum: 512 deep (256 of three parts), which leaves the truncation of 32 MMAs (16, and 80 of smaller
     // products). T = 777, V = 50001,
     // d = 1000: losses 3.8e-7 off (256 deep 1.8e-7, 1024 8e-7); T = 16384, V = 32000, d = 2048: 1104 us (1194, 1090). fp32, T = 2048, V = 8000,
@@ -593,7 +594,7 @@ template <typename E, int SPLIT, int DZ> void run_loss(Run &r, const Shape &s, c
             g.slot0 += 2 * u.nn;
             continue;
         }
-        r.map(&z.o[0], p.dz, vn, DZ * p.tp, p.vc * 2, 32, 32, k64);
+        r.map(&z.o[0], p.dz, vn, SPLIT * p.tp, p.vc * 2, 32, 32, k64);
         // z again, whose error is seen where a token is certain and p - q next to nothing: in one accumulator it grew with d (d = 16384,
         // logits up to 1400: dX and dW 1.5e-2 off; in pieces 1024 deep 1.9e-3, their rounding). T = 16384, V = 32000, d = 2048 backward
         // 3903 -> 3947 us, T = 8192, d = 1100 3 % more; pieces 512 deep cost 4 to 10 %.
@@ -616,7 +617,7 @@ template <typename E, int SPLIT, int DZ> void run_loss(Run &r, const Shape &s, c
             h.nn = p.dx.nn;
             h.splits = p.dx.splits;
             h.add = i > 0;
-            r.map(&gr.a[jobs], p.dz, vn, DZ * p.tp, p.vc * 2, 64, (uint32_t)g.a_rows, k128);
+            r.map(&gr.a[jobs], p.dz, vn, SPLIT * p.tp, p.vc * 2, 64, (uint32_t)g.a_rows, k128);
             r.map(&gr.b[jobs], w, s.d, w_rows, ldw * 2, 64, 64, k128);
             r.map(&gr.o[jobs], p.dxs, p.dp, h.splits * p.tp, p.dp * 4, 32, 32, k128, CU_TENSOR_MAP_DATA_TYPE_FLOAT32);
             depth[jobs++] = vn / h.splits;
@@ -637,7 +638,7 @@ template <typename E, int SPLIT, int DZ> void run_loss(Run &r, const Shape &s, c
             h.b_off = (int)p.tp;
             h.b_y = 0;
             h.out_f32 = F32;
-            r.map(&gr.a[jobs], p.dz, vn, DZ * p.tp, p.vc * 2, 64, 64, k128);
+            r.map(&gr.a[jobs], p.dz, vn, SPLIT * p.tp, p.vc * 2, 64, 64, k128);
             r.map(&gr.b[jobs], p.xp, s.d, SPLIT * p.tp, p.dp * 2, 64, 64, k128);
             CUtensorMap *mo = &gr.o[jobs];
             *mo = gr.a[jobs];
@@ -699,13 +700,9 @@ resbm_status check_shape(const resbm_vocab_desc *desc, bool distill)
     return RESBM_OK;
 }
 
-// Tokens up to which a bf16 dz has two parts: forward and backward at V = 32000, d = 2048 165 us instead of 144 with one token, whose
-// gradients were up to 3.7e-3 off, twice the outputs' rounding. Over more tokens the errors average to that.
-constexpr int64_t kTwoParts = 16;
 Shape shape_of(const resbm_vocab_desc &d, bool distill, bool bwd)
 {
-    const bool f32 = d.dtype == RESBM_F32;
-    return Shape{d.T, d.V, d.d, distill ? d.K : 0, f32 ? 3 : 1, f32 ? 3 : d.T <= kTwoParts ? 2 : 1, distill, bwd, false};
+    return Shape{d.T, d.V, d.d, distill ? d.K : 0, d.dtype == RESBM_F32 ? 3 : 1, distill, bwd, false};
 }
 
 resbm_status loss_call(const resbm_vocab_desc *desc, bool distill, bool bwd, Call a, void *ws, size_t ws_bytes, void *stream)
@@ -749,9 +746,8 @@ resbm_status loss_call(const resbm_vocab_desc *desc, bool distill, bool bwd, Cal
     s.pack_w = s.split == 3 || !al16(a.W) || d.ldw % 8 != 0;
     const Plan p = make_plan(s, ws);
     if (p.bytes > ws_bytes) return RESBM_ERR_WORKSPACE;   // (plan_bytes covers it)
-    if (s.dz == 3) run_loss<float, 3, 3>(r, s, p, a);
-    else if (s.dz == 2) run_loss<__nv_bfloat16, 1, 2>(r, s, p, a);
-    else run_loss<__nv_bfloat16, 1, 1>(r, s, p, a);
+    if (s.split == 3) run_loss<float, 3>(r, s, p, a);
+    else run_loss<__nv_bfloat16, 1>(r, s, p, a);
     count_launches(r.launches);
     if (r.e != cudaSuccess) cudaGetLastError();
     return finish(r.e);

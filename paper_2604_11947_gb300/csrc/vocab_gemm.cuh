@@ -20,8 +20,10 @@
 // 24 bits), and a product the six of nine partial ones that are over 2^-24 of it, smallest first. They are one product of
 // six times the depth at the bf16 rate: 320 TFLOP/s of fp32 at most, where CUDA cores have 75.
 //
-// Few tokens in bf16 (SPLIT 2): dz as two bf16 values. Its rounding is one of the outputs' own size, but a single token's gradients
-// have one large dz, the label's, whose error no sum averages: up to 2^-8 of the whole of dX and dW (T = 1: 3.7e-3 off).
+// Few tokens in use in bf16 (SPLIT 2, up to kTwoParts of them): dz as two bf16 values. Its rounding is one of the outputs' own size, but a
+// single token's gradients have one large dz, the label's, whose error no sum averages: up to 2^-8 of the whole of dX and dW (T = 1:
+// 3.7e-3 off). Over more tokens dW averages them, and dX its rows: 2.3e-3 of their norm instead of 1.7e-3. (One token, V = 32000, d = 2048, forward and backward: 144 us
+// with one part, 165 with two.) How many are in use is known on the device, so one kernel has both forms; the second part of the 64 rows that a depth slice reads lies kRest rows on, in the same row block.
 //
 // PIECES: the tensor core truncates as it adds to its accumulator, an error that grows with the number of MMAs in one
 // accumulator (run_loss has figures). Where that is seen in an output (the logits, and everything in fp32) a unit's sum
@@ -61,7 +63,7 @@ struct VocabGemm {
     int32_t depth;            // FWD, DZ, DX
     int32_t bn, nn;           // columns a unit (a multiple of 32), units along the columns
     int32_t splits, group;
-    int32_t a_off, b_off;     // rows from one of SPLIT's three operands to the next
+    int32_t a_off, b_off;     // rows from one of three parts of an operand to the next
     int32_t a_rows;           // FWD, DZ, DX: rows of A a load: 128, or fewer where one load has all tokens
     int32_t b_y;              // FWD, DZ, DX: the piece's first row in B's tensor map
     int32_t out_y;            // DW: the piece's first row of dW
@@ -88,6 +90,8 @@ struct VocabGemm {
     int64_t ldo;
     int32_t out_f32;          // DW: fp32 result (slots, or an fp32 dW), else bf16
 };
+
+constexpr int kTwoParts = 16, kRest = 128;
 
 struct VocabCfg {
     static constexpr uint32_t A_STAGE = 128 * 128, B_STAGE = 128 * 128, STAGE = A_STAGE + B_STAGE;
@@ -202,7 +206,6 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __gri
     using C = VocabCfg;
     constexpr bool GRADS = MODE == VG_GRADS, BMN = GRADS;
     constexpr bool PIECES = PIECE > 0;
-    constexpr int TERMS = SPLIT == 3 ? 6 : SPLIT == 2 && GRADS ? 2 : 1;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     __shared__ uint64_t full[C::NST], empty[C::NST], acc_full[2], acc_empty[2], done_bar;
@@ -233,6 +236,8 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __gri
 
     // the units, in every warp alike
     const int n = jobs.g[0].n_ptr ? *jobs.g[0].n_ptr : jobs.g[0].n_rows;
+    const bool two = SPLIT == 2 && n <= kTwoParts;   // dz in two parts
+    const int terms = SPLIT == 3 ? 6 : GRADS && two ? 2 : 1;
     struct Job {
         bool dw;
         int rows, slices, per;
@@ -269,7 +274,7 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __gri
     const bool late = (int)pair >= over;
     uint32_t extra = 0;
     if (JOBS > 1 && over > 0) {
-        const uint32_t c0 = TERMS * job0.per + kUnitSlices, c1 = TERMS * job1.per + kUnitSlices;
+        const uint32_t c0 = (uint32_t)terms * job0.per + kUnitSlices, c1 = (uint32_t)terms * job1.per + kUnitSlices;
         extra = (2 * c0 + c1) / (2 * c1);
         if (extra > job1.units / under) extra = job1.units / under;
     }
@@ -359,12 +364,12 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __gri
                     const int first = 64 * (x.k0 + kp), end = 64 * (x.k0 + ke);
                     if constexpr (SPLIT == 2 && GRADS) {   // dz's remainder, dz; slice by slice: the second product finds W's in L2
                         for (int k = first; k < end && ok; k += 64) {
-                            load(g.a_off, g.b_y, k);
+                            if (two) load(kRest, g.b_y, k);
                             if (ok) load(0, g.b_y, k);
                         }
                     } else {
 #pragma unroll 1
-                        for (int term = 0; term < TERMS && ok; ++term) {
+                        for (int term = 0; term < terms && ok; ++term) {
                             // the partial products, smallest first: (2, 0) (1, 1) (0, 2) (1, 0) (0, 1) (0, 0)
                             const int sa = SPLIT < 3 ? 0 : term == 0 ? 2 : (term == 1 || term == 3) ? 1 : 0;
                             const int sb = SPLIT < 3 ? 0 : term == 2 ? 2 : (term == 1 || term == 4) ? 1 : 0;
@@ -401,7 +406,7 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __gri
                     ok = mbar_wait(smem_u32(&acc_empty[ab]), ((ti >> 1) & 1) ^ 1);
                     tc_fence_after();
                     if (!ok) break;
-                    const int steps = (x.nk - kp < piece ? x.nk - kp : piece) * TERMS;
+                    const int steps = (x.nk - kp < piece ? x.nk - kp : piece) * terms;
                     for (int i = 0; i < steps; ++i, ++it) {
                         const uint32_t s = it % C::NST, ph = (it / C::NST) & 1;
                         ok = mbar_wait(smem_u32(&full[s]), ph);
@@ -564,9 +569,11 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __gri
 #pragma unroll
                         for (int j = 0; j < 32; ++j) v[j] = 0.0f;
                     }
+                    if (two && row0 >= 64) return;
 #pragma unroll
                     for (int part = 0; part < SPLIT; ++part) {
-                        store_bf16(mo, v, col, part * g.slot_rows + row0);
+                        store_bf16(mo, v, col, part * (SPLIT == 2 ? kRest : g.slot_rows) + row0);
+                        if (SPLIT == 2 && !two) break;
                         if (part + 1 < SPLIT) {
 #pragma unroll
                             for (int j = 0; j < 32; ++j) v[j] -= __bfloat162float(__float2bfloat16_rn(v[j]));

@@ -108,7 +108,7 @@ RESBM_API resbm_status resbm_embed_fwd(const resbm_embed_desc *desc, const int64
 /* dtable_v = scale * (the sum of dout_t over the tokens t with ids_t = v), in fp32, rounded once; zero for a word without
  * tokens and for the padding id. Tokens are sorted by id, and a word's rows are added in the tokens' order (those that lie in one
  * block of 32 sorted positions, and then the blocks' sums): the same bits every time.  dout : T x d in.  dtable : V x d out, dense, complete (not added to).
- * An id outside 0 .. V - 1 counts as padding. Errors as above; RESBM_ERR_UNSUPPORTED for T or V of 2^29 and over. */
+ * An id outside 0 .. V - 1 counts as padding. Errors as above; RESBM_ERR_UNSUPPORTED for T or V of 2^29 and over, or d over 2^20 (the forward too). */
 RESBM_API resbm_status resbm_embed_bwd(const resbm_embed_desc *desc, const int64_t *ids, const void *dout, void *dtable, void *ws,
                                        size_t ws_bytes, void *stream);
 

@@ -383,9 +383,10 @@ resbm_status check(const resbm_embed_desc *desc, const int64_t *ids, const void 
 {
     if (!desc) return RESBM_ERR_INVALID_ARG;
     const resbm_embed_desc &d = *desc;
-    if (d.T < 0 || d.V < 1 || d.d < 1 || (d.dtype != RESBM_F32 && d.dtype != RESBM_BF16) || d.flags || !isfinite(d.scale)) return RESBM_ERR_INVALID_ARG;
-    constexpr int64_t most = int64_t(1) << 29, limit = INT64_MAX / 64;
-    if (d.T >= most || d.V >= most || d.d > (int64_t(1) << 20)) return RESBM_ERR_UNSUPPORTED;
+    if (d.flags || !isfinite(d.scale)) return RESBM_ERR_INVALID_ARG;
+    const resbm_status st = embed_check_shape(d.T, d.V, d.d, d.dtype);
+    if (st != RESBM_OK) return st;
+    constexpr int64_t limit = INT64_MAX / 64;
     const int64_t es = d.dtype == RESBM_BF16 ? 2 : 4;
     const bool t = d.T > 0;
     auto bad = [&](int64_t rows, int64_t ld) { return rows > 1 && (ld < d.d || !mul_ok(rows, ld) || rows * ld > limit); };
@@ -446,6 +447,13 @@ template <typename E> cudaError_t run_bwd(const resbm_embed_desc &d, const int64
 }
 
 }  // namespace
+
+resbm_status embed_check_shape(int64_t T, int64_t V, int64_t d, int32_t dtype)
+{
+    if (T < 0 || V < 1 || d < 1 || (dtype != RESBM_F32 && dtype != RESBM_BF16)) return RESBM_ERR_INVALID_ARG;
+    constexpr int64_t most = int64_t(1) << 29;
+    return T >= most || V >= most || d > (int64_t(1) << 20) ? RESBM_ERR_UNSUPPORTED : RESBM_OK;
+}
 
 size_t embed_bwd_ws_bytes(int64_t T, int64_t d) { return carve(nullptr, T, d).bytes; }
 

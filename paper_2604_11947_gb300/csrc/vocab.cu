@@ -776,11 +776,16 @@ resbm_status resbm_vocab_workspace_bytes(const resbm_vocab_desc *desc, int op, s
     if (!bytes) return RESBM_ERR_INVALID_ARG;
     *bytes = 0;
     if (op < RESBM_VOCAB_CE_FWD || op > RESBM_VOCAB_EMBED_BWD) return RESBM_ERR_INVALID_ARG;
+    if (op == RESBM_VOCAB_EMBED_BWD) {   // (its limits are not the products')
+        if (!desc || desc->flags) return RESBM_ERR_INVALID_ARG;
+        const resbm_status st = embed_check_shape(desc->T, desc->V, desc->d, desc->dtype);
+        if (st == RESBM_OK) *bytes = embed_bwd_ws_bytes(desc->T, desc->d);
+        return st;
+    }
     const bool distill = op == RESBM_VOCAB_DISTILL_FWD || op == RESBM_VOCAB_DISTILL_BWD;
     const resbm_status st = check_shape(desc, distill);
     if (st != RESBM_OK) return st;
-    *bytes = op == RESBM_VOCAB_EMBED_BWD ? embed_bwd_ws_bytes(desc->T, desc->d)
-                                         : plan_bytes(shape_of(*desc, distill, op == RESBM_VOCAB_CE_BWD || op == RESBM_VOCAB_DISTILL_BWD));
+    *bytes = plan_bytes(shape_of(*desc, distill, op == RESBM_VOCAB_CE_BWD || op == RESBM_VOCAB_DISTILL_BWD));
     return RESBM_OK;
 }
 

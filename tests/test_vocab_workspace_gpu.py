@@ -3,6 +3,7 @@ import pytest
 import torch
 
 import vocab_helpers as vh
+from test_embed_gpu import backward, check_backward, ids_of, rows
 from test_vocab_loss_gpu import each, run
 
 pytestmark = pytest.mark.gpu
@@ -20,3 +21,9 @@ def test_a_head_of_padded_rows(T, V, d, wpad):
     dense = run(X, W.contiguous(), labels, each(T))
     want.check_fwd(*dense[:2])
     want.check_bwd(each(T), *dense[2:])
+
+
+def test_an_embedding_of_more_tokens_times_words_than_a_loss_may_have():
+    T, V, d = 1 << 22, 1 << 21, 8
+    ids, dout = ids_of(T, V, "any"), rows(T, d, "bf16")
+    check_backward(backward(ids, dout, 0.5, V), ids, dout, 0.5, V)

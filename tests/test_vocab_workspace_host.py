@@ -21,3 +21,19 @@ def test_a_head_of_padded_rows_has_room(T, V, d):
     for op in (resbm.RESBM_VOCAB_CE_FWD, resbm.RESBM_VOCAB_CE_BWD, resbm.RESBM_VOCAB_DISTILL_FWD, resbm.RESBM_VOCAB_DISTILL_BWD):
         size = lambda n: resbm.resbm_vocab_workspace_bytes(op, T, V, n, "bf16", 5)
         assert size(d) >= size(wide)
+
+
+@pytest.mark.parametrize("T,V,d", [(1 << 22, 1 << 21, 8), ((1 << 29) - 1, (1 << 29) - 1, 64), (1 << 20, 1000, 1 << 20), (1, 1, 1), (0, 1, 1 << 20)])
+def test_the_embedding_has_limits_of_its_own(T, V, d):
+    """Every size that resbm_embed_bwd takes has a workspace size: 4 numbers a token and 2 rows of fp32 a block of 32 tokens."""
+    size = resbm.resbm_vocab_workspace_bytes(resbm.RESBM_VOCAB_EMBED_BWD, T, V, d)
+    blocks = (T + 31) // 32
+    assert 16 * T + 8 * blocks * d <= size <= 16 * T + 8 * blocks * d + 3 * 256
+
+
+@pytest.mark.parametrize("T,V,d,status", [(1 << 29, 1, 1, resbm.RESBM_ERR_UNSUPPORTED), (1, 1 << 29, 1, resbm.RESBM_ERR_UNSUPPORTED), (1, 1, (1 << 20) + 1, resbm.RESBM_ERR_UNSUPPORTED),
+                                          (-1, 1, 1, resbm.RESBM_ERR_INVALID_ARG), (1, 0, 1, resbm.RESBM_ERR_INVALID_ARG), (1, 1, 0, resbm.RESBM_ERR_INVALID_ARG)])
+def test_sizes_that_the_embedding_refuses(T, V, d, status):
+    with pytest.raises(resbm.ResbmError) as e:
+        resbm.resbm_vocab_workspace_bytes(resbm.RESBM_VOCAB_EMBED_BWD, T, V, d)
+    assert e.value.status == status

@@ -83,7 +83,9 @@ RESBM_API resbm_status resbm_linear_ce_bwd(const resbm_vocab_desc *desc, const v
  *   index   : T x K int64 in, the words of the teacher's entries in any order; a negative one is no entry (fewer than K), an
  *             index that stands twice counts twice. A token with no entry has no target: loss, lse and its row of dX are
  *             zero. An index >= V gives NaN.
- *   teacher : T x K in, type teacher_dtype; not read for a meaning where the index is negative. */
+ *   teacher : T x K in, type teacher_dtype; not read for a meaning where the index is negative. An entry of -infinity has no weight, a
+ *             token whose entries are all -infinity a loss of NaN. No gradient is formed for it.
+ * The loss is a difference of sums of lse's size, and is off by tau^2 times their errors. */
 RESBM_API resbm_status resbm_distill_fwd(const resbm_vocab_desc *desc, const void *X, const void *W, const int64_t *index,
                                          const void *teacher, float *loss, float *lse, void *ws, size_t ws_bytes, void *stream);
 RESBM_API resbm_status resbm_distill_bwd(const resbm_vocab_desc *desc, const void *X, const void *W, const int64_t *index,

@@ -25,7 +25,8 @@ using namespace tc;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // ---- the targets of a distillation ---------------------------------------------------------------
-// A warp a token: q = softmax of its entries' teacher logits over tau, sum q log q, and the entries in ascending order of
+// A warp a token: q = softmax of its entries' teacher logits over tau (the largest taken off first: the lowest value of the type, over a tau
+// under 1, is no number), sum q log q, and the entries in ascending order of
 // their words (the products' tiles look theirs up by bisection), ranked by counting: K^2 / 32 comparisons a lane, 128 at K = 64.
 template <typename E>
 __global__ void __launch_bounds__(256) k_targets(const int64_t *__restrict__ index, const E *__restrict__ teacher, int64_t T, int K, int64_t V,
@@ -47,7 +48,7 @@ __global__ void __launch_bounds__(256) k_targets(const int64_t *__restrict__ ind
             if (i < 0) continue;
             ++have;
             wrong |= i >= V;
-            most = max_nan(most, to_f32(tl[k]) / tau);
+            most = max_nan(most, to_f32(tl[k]));
         }
         float sum = 0.0f;
 #pragma unroll
@@ -57,7 +58,7 @@ __global__ void __launch_bounds__(256) k_targets(const int64_t *__restrict__ ind
             wrong |= __shfl_xor_sync(0xffffffffu, wrong, o);
         }
         for (int k = lane; k < K; k += 32)
-            if (ix[k] >= 0) sum += expf(to_f32(tl[k]) / tau - most);
+            if (ix[k] >= 0) sum += expf((to_f32(tl[k]) - most) / tau);
 #pragma unroll
         for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
         const float inv = 1.0f / sum, log_sum = logf(sum);
@@ -69,7 +70,7 @@ __global__ void __launch_bounds__(256) k_targets(const int64_t *__restrict__ ind
             for (int j = 0; j < K; ++j) rank += key[j] < mine || (key[j] == mine && j < k);
             float q = 0.0f;
             if (ix[k] >= 0) {
-                const float x = to_f32(tl[k]) / tau - most;
+                const float x = (to_f32(tl[k]) - most) / tau;
                 q = expf(x) * inv;
                 if (!(q == 0.0f)) h = fmaf(q, x - log_sum, h);
             }

@@ -40,7 +40,7 @@ typedef struct {
     int64_t K;                  /* distill: entries a token, 1 .. 1024 (not used by the cross entropy)        */
     int32_t dtype;              /* resbm_dtype of X, W, dX, dW                                                */
     int32_t teacher_dtype;      /* distill: resbm_dtype of the teacher's logits                               */
-    float temperature;          /* distill: tau > 0, finite (not used by the cross entropy, where it is 1)    */
+    float temperature;          /* distill: tau, 1e-18 .. 1e18 (not used by the cross entropy, where it is 1) */
     int32_t dloss_each;         /* backward: 1 where dloss has an element for every token, 0 where it has one */
     uint32_t flags;             /* 0                                                                          */
 } resbm_vocab_desc;

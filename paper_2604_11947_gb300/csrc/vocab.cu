@@ -706,6 +706,9 @@ Shape shape_of(const resbm_vocab_desc &d, bool distill, bool bwd)
     return Shape{d.T, d.V, d.d, distill ? d.K : 0, d.dtype == RESBM_F32 ? 3 : 1, distill, bwd, false};
 }
 
+// (tau^2 and log2(e) / tau are floats)
+constexpr float kLeastTau = 1e-18f, kMostTau = 1e18f;
+
 resbm_status loss_call(const resbm_vocab_desc *desc, bool distill, bool bwd, Call a, void *ws, size_t ws_bytes, void *stream)
 {
     resbm_status st = check_shape(desc, distill);
@@ -715,7 +718,7 @@ resbm_status loss_call(const resbm_vocab_desc *desc, bool distill, bool bwd, Cal
     if (d.V == 1) d.ldw = d.d;
     const int64_t es = d.dtype == RESBM_BF16 ? 2 : 4, limit = INT64_MAX / 64;
     const bool t = d.T > 0;
-    if (distill && ((d.teacher_dtype != RESBM_F32 && d.teacher_dtype != RESBM_BF16) || !(d.temperature > 0.0f) || !(d.temperature < INFINITY)))
+    if (distill && ((d.teacher_dtype != RESBM_F32 && d.teacher_dtype != RESBM_BF16) || !(d.temperature >= kLeastTau) || !(d.temperature <= kMostTau)))
         return RESBM_ERR_INVALID_ARG;
     if (bwd && (d.dloss_each < 0 || d.dloss_each > 1)) return RESBM_ERR_INVALID_ARG;
     auto bad = [&](int64_t rows, int64_t ld) { return rows > 1 && (ld < d.d || !mul_ok(rows, ld) || rows * ld > limit); };

@@ -260,7 +260,8 @@ struct SumArgs {
 
 // Blocks of kRun sorted positions, 2^log_tx threads along a row, which add the rows of each word up in order, sixteen in
 // flight. A word whose tokens all lie in the block is finished; the block's first and last runs may be pieces of longer ones, and
-// leave a partial sum (k_embed_join). So the work is even whatever the ids are.
+// leave a partial sum. So this kernel's work is even whatever the ids are; k_embed_join's is not: a word on half of 65536 tokens is
+// 1024 partial rows, added up by the threads of one block.
 template <typename E, int VEC, int STEP> __global__ void __launch_bounds__(256, 3) k_embed_sum(const SumArgs a)
 {
     griddep_wait();

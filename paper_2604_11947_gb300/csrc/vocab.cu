@@ -518,11 +518,6 @@ template <typename E, int SPLIT> void run_loss(Run &r, const Shape &s, const Pla
         if (d.teacher_dtype == RESBM_F32) go(k_targets<float>, static_cast<const float *>(a.teacher));
         else go(k_targets<__nv_bfloat16>, static_cast<const __nv_bfloat16 *>(a.teacher));
     }
-    auto join = [&](const int32_t *row, int slots, int64_t tp) {
-        JoinArgs j{p.stat, p.zt, slots, tp, row, p.count, label, p.ent, T, V, kLog2e / tau, tau, a.loss, a.lse_out};
-        if (T < 1024) r.go(k_join<1>, dim3((unsigned)T), dim3(256), 0, 1, j);
-        else r.go(k_join<32>, dim3((unsigned)((T + 31) / 32)), dim3(256), 0, 1, j);
-    };
     const bool x_fits = al16(a.X) && d.ldx * (int64_t)sizeof(E) % 16 == 0;
     // one row block: the tokens without a target cost nothing more (but their rows must not enter dW)
     const bool direct = !s.bwd && !F32 && x_fits && T <= 256;

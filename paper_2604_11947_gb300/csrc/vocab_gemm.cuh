@@ -22,8 +22,9 @@
 //
 // Few tokens in use in bf16 (SPLIT 2, up to kTwoParts of them): dz as two bf16 values. Its rounding is one of the outputs' own size, but a
 // single token's gradients have one large dz, the label's, whose error no sum averages: up to 2^-8 of the whole of dX and dW (T = 1:
-// 3.7e-3 off). Over more tokens dW averages them, and dX its rows: 2.3e-3 of their norm instead of 1.7e-3. (One token, V = 32000, d = 2048, forward and backward: 144 us
-// with one part, 165 with two.) How many are in use is known on the device, so one kernel has both forms; the second part of the 64 rows that a depth slice reads lies kRest rows on, in the same row block.
+// 3.7e-3 off). Over more tokens dW averages them, and dX's norm its rows: 2.3e-3 of it instead of 1.7e-3. (One token, V = 32000, d = 2048,
+// forward and backward: 144 us with one part, 165 with two.) How many are in use is known on the device, so one kernel has both forms;
+// the second part of the 64 rows that a slice of dW's depth reads lies kRest rows on, in the same row block.
 //
 // PIECES: the tensor core truncates as it adds to its accumulator, an error that grows with the number of MMAs in one
 // accumulator (run_loss has figures). Where that is seen in an output (the logits, and everything in fp32) a unit's sum
@@ -176,7 +177,6 @@ struct RowIn {
 struct Yes { static constexpr bool value = true; };
 struct No { static constexpr bool value = false; };
 
-// MODE: what becomes of the accumulator; SPLIT: bf16 parts of an operand (2: of dz alone); PIECE: 64-deep slices of a piece of a sum (0: whole)
 // x / d for x under 2^31: a product with the reciprocal and a correction (a division is 20 dependent instructions, and every warp
 // has three a unit)
 struct Divisor {
@@ -200,6 +200,8 @@ template <int JOBS> struct VocabJobs {
     VocabGemm g[JOBS];
 };
 
+// MODE: what becomes of the accumulator; SPLIT: bf16 parts of an operand (2: of dz alone, for few tokens); PIECE: 64-deep slices of a piece of a
+// sum (0: whole)
 template <int MODE, int SPLIT, int PIECE, int JOBS>
 __global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __grid_constant__ VocabJobs<JOBS> jobs)
 {

@@ -373,7 +373,8 @@ def linear_cross_entropy(x, head, labels, reduction="mean"):
 
 def distillation(x, head, index, teacher, temperature=1.0, reduction="mean"):
     """temperature^2 times the divergence of softmax(x . head^T / temperature) from that of a teacher's K logits a token at the
-    words `index` (both x's leading shape and K; index int64, negative: no entry)."""
+    words `index` (both x's leading shape and K; index int64, negative: no entry). The teacher's logits are constants: no gradient
+    reaches them."""
     if index.shape[:-1] != x.shape[:-1] or teacher.shape != index.shape:
         raise ValueError("index and teacher must be of x's leading shape and K")
     return _reduce(_VocabLoss.apply(x, head, index, teacher, float(temperature)), (index >= 0).any(dim=-1), reduction)

@@ -88,13 +88,38 @@ __global__ void __launch_bounds__(256) k_targets(const int64_t *__restrict__ ind
 }
 
 // ---- the tokens in use -----------------------------------------------------------------------------
+// The common factor of the losses' gradients, taken out of dz before its rounding to bf16: the dz of a token's label is next to -dloss
+// as long as the model knows nothing of it, and where dloss is one number for all (the mean over n tokens: 1 / n) its rounding is
+// the same for all, up to 2^-8 in the end of dX and dW that no sum averages (T = 24, V = 24141, d = 2480: 2.5e-3 off, without it 1.9e-3; the outputs' rounding is 1.7e-3).
+struct LossScale {
+    const float *dloss;   // null: none is asked for
+    int each;
+    float tau;
+    float *out;           // the factor, and that times tau
+    // bits of a value that can be the factor, in ascending order: 0 for infinities and NaN
+    __device__ __forceinline__ uint32_t bits(int64_t t) const
+    {
+        const uint32_t b = __float_as_uint(dloss[t]) & 0x7FFFFFFFu;
+        return b < 0x7F800000u ? b : 0u;
+    }
+    // n tokens in use, of which `top` is the largest; where there are none a dloss of infinity (1 / 0) gives zeros
+    __device__ __forceinline__ void put(int n, uint32_t top) const
+    {
+        const float s = n == 0 ? 1.0f : !each ? dloss[0] : top ? __uint_as_float(top) : 1.0f;
+        out[0] = s;
+        out[1] = s * tau;
+    }
+};
+
 // token[r] = the r-th token with a target, row[t] = its r or -1, *n = how many. One cluster of eight CTAs, a contiguous run of the
 // tokens a warp, counted and then written. (One CTA with eight loads a thread, one after the other: 27 us at T = 16384; this 5.)
 constexpr int kScanCtas = 8;
 __global__ void __cluster_dims__(kScanCtas) __launch_bounds__(1024) k_scan(const int64_t *__restrict__ label, const int32_t *__restrict__ count, int T,
-                                                                           int32_t *__restrict__ n, int32_t *__restrict__ token, int32_t *__restrict__ row)
+                                                                           int32_t *__restrict__ n, int32_t *__restrict__ token, int32_t *__restrict__ row,
+                                                                           const LossScale scale)
 {
     __shared__ int sums[32], total;
+    __shared__ uint32_t tops[32], top_all;
     griddep_wait();
     griddep_launch_dependents();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rank = (int)cluster_rank();
@@ -103,17 +128,31 @@ __global__ void __cluster_dims__(kScanCtas) __launch_bounds__(1024) k_scan(const
     const int p0 = (int)(first < T ? first : T), p1 = (int)(first + per < T ? first + per : T);
     auto has = [&](int t) { return t < p1 && (label ? label[t] >= 0 : count[t] > 0); };
     int mine = 0;
+    uint32_t top = 0;
+    const bool tops_too = scale.dloss && scale.each;
 #pragma unroll 4
-    for (int p = p0; p < p1; p += 32) mine += __popc(__ballot_sync(0xffffffffu, has(p + lane)));
-    if (lane == 0) sums[warp] = mine;
+    for (int p = p0; p < p1; p += 32) {
+        const bool h = has(p + lane);
+        mine += __popc(__ballot_sync(0xffffffffu, h));
+        if (tops_too && h) top = max(top, scale.bits(p + lane));
+    }
+    top = __reduce_max_sync(0xffffffffu, top);
+    if (lane == 0) {
+        sums[warp] = mine;
+        tops[warp] = top;
+    }
     __syncthreads();
     int before = 0, all = 0;
 #pragma unroll
     for (int w = 0; w < 32; ++w) {
         before += w < warp ? sums[w] : 0;
         all += sums[w];
+        top = max(top, tops[w]);
     }
-    if (threadIdx.x == 0) total = all;
+    if (threadIdx.x == 0) {
+        total = all;
+        top_all = top;
+    }
     cluster_sync();
     int whole = 0;
     for (int c = 0; c < kScanCtas; ++c) {
@@ -121,6 +160,8 @@ __global__ void __cluster_dims__(kScanCtas) __launch_bounds__(1024) k_scan(const
         asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(map_shared(smem_addr(&total), (uint32_t)c)));
         if (c < rank) before += v;
         whole += v;
+        asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(map_shared(smem_addr(&top_all), (uint32_t)c)));
+        top = max(top, (uint32_t)v);
     }
     for (int p = p0; p < p1; p += 32) {
         const bool h = has(p + lane);
@@ -130,7 +171,10 @@ __global__ void __cluster_dims__(kScanCtas) __launch_bounds__(1024) k_scan(const
         if (h) token[at] = p + lane;
         before += __popc(who);
     }
-    if (rank == 0 && threadIdx.x == 0) *n = whole;
+    if (rank == 0 && threadIdx.x == 0) {
+        *n = whole;
+        if (scale.dloss) scale.put(whole, top);
+    }
     cluster_sync();   // no CTA leaves while another reads its total
 }
 
@@ -189,25 +233,36 @@ constexpr int kCollect = 4096;
 template <typename E, int SPLIT>
 __global__ void __launch_bounds__(256) k_collect(const int64_t *__restrict__ label, const int32_t *__restrict__ count, int T, const E *__restrict__ in,
                                                  int64_t ld, bool vec, int d, int dp, __nv_bfloat16 *__restrict__ out, int64_t off, int32_t *__restrict__ n,
-                                                 int32_t *__restrict__ token, int32_t *__restrict__ row)
+                                                 int32_t *__restrict__ token, int32_t *__restrict__ row, const LossScale scale)
 {
-    __shared__ uint32_t sums[8];
+    __shared__ uint32_t sums[8], tops[8];
     griddep_wait();
     griddep_launch_dependents();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t0 = blockIdx.x * 8, t = t0 + warp;
     auto has = [&](int i) { return label ? label[i] >= 0 : count[i] > 0; };
-    uint32_t mine = 0;   // all tokens in use, and from bit 16 on those before the CTA's
+    uint32_t mine = 0, top = 0;   // all tokens in use, and from bit 16 on those before the CTA's; the largest dloss's bits
+    const bool tops_too = scale.dloss && scale.each && blockIdx.x == 0;
 #pragma unroll 8
     for (int i = threadIdx.x; i < T; i += 256)
-        if (has(i)) mine += i < t0 ? 65537u : 1u;
+        if (has(i)) {
+            mine += i < t0 ? 65537u : 1u;
+            if (tops_too) top = max(top, scale.bits(i));
+        }
     mine = __reduce_add_sync(0xffffffffu, mine);
-    if (lane == 0) sums[warp] = mine;
+    top = __reduce_max_sync(0xffffffffu, top);
+    if (lane == 0) {
+        sums[warp] = mine;
+        tops[warp] = top;
+    }
     const bool own = lane < 8 && t0 + lane < T && has(t0 + lane);   // (the CTA's tokens, in every warp)
     const uint32_t who = __ballot_sync(0xffffffffu, own);
     __syncthreads();
     uint32_t both = 0;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) both += sums[w];
+    for (int w = 0; w < 8; ++w) {
+        both += sums[w];
+        top = max(top, tops[w]);
+    }
     const int all = (int)(both & 0xFFFFu), before = (int)(both >> 16);
     const int at = before + __popc(who & ((1u << warp) - 1));
     if (t < T) {
@@ -218,7 +273,10 @@ __global__ void __launch_bounds__(256) k_collect(const int64_t *__restrict__ lab
         }
         if (h) pack_row<E, SPLIT>(in + (int64_t)t * ld, vec, d, dp, out + (int64_t)at * dp, off);
     }
-    if (blockIdx.x == 0 && threadIdx.x == 0) *n = all;
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        *n = all;
+        if (scale.dloss) scale.put(all, top);
+    }
     // zeros up to a multiple of 256
     for (int r = all + t; r < (all + 255) / 256 * 256; r += 8 * (int)gridDim.x) pack_row<E, SPLIT>(static_cast<const E *>(nullptr), vec, d, dp, out + (int64_t)r * dp, off);
 }
@@ -287,8 +345,8 @@ template <int TX> __global__ void __launch_bounds__(256) k_join(const JoinArgs a
 }
 
 // ---- rows of fp32 slots, summed in order and rounded -----------------------------------------------
-// out[t] = the sum of the slots' rows row[t] (or t), zeros where that is negative or there are no slots. Eight columns a thread;
-// up to two matrices in a launch.
+// out[t] = the sum of the slots' rows row[t] (or t), times scale[1] where there is one; zeros where the row is negative. Eight columns a
+// thread; up to two matrices in a launch.
 struct FinishJob {
     const float *slot;
     int slots;
@@ -298,10 +356,11 @@ struct FinishJob {
     void *out;
     bool vec;
 };
-template <typename E> __global__ void __launch_bounds__(256) k_finish(const FinishJob j0, const FinishJob j1, int d, int dp)
+template <typename E> __global__ void __launch_bounds__(256) k_finish(const FinishJob j0, const FinishJob j1, int d, int dp, const float *scale)
 {
     griddep_wait();
     griddep_launch_dependents();
+    const float factor = scale ? scale[1] : 1.0f;
     const FinishJob &j = blockIdx.y ? j1 : j0;
     const int per = (d + 7) / 8;
     const int64_t vectors = j.T * per;
@@ -318,6 +377,10 @@ template <typename E> __global__ void __launch_bounds__(256) k_finish(const Fini
             const float4 a = p[0], b = p[1];
             x[0] += a.x; x[1] += a.y; x[2] += a.z; x[3] += a.w;
             x[4] += b.x; x[5] += b.y; x[6] += b.z; x[7] += b.w;
+        }
+        if (scale && count > 0) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] *= factor;
         }
         E *dst = static_cast<E *>(j.out) + t * d + c;
         if (j.vec && c + 8 <= d) {
@@ -390,7 +453,7 @@ struct Plan {
     size_t bytes;
     int32_t *n, *token, *row, *count;
     int2 *list;
-    float *ent, *bad, *zt, *dxs, *dws;
+    float *ent, *bad, *zt, *dxs, *dws, *scale;
     float2 *stat;
     __nv_bfloat16 *xp, *wp, *dz;
 };
@@ -430,6 +493,7 @@ Plan make_plan(const Shape &s, void *ws)
         p.stat = w.take<float2>(p.slots * p.tp);
         p.zt = w.take<float>(s.distill ? p.slots * p.tp : p.tp);
     } else {
+        if (s.split == 1) p.scale = w.take<float>(2);
         p.dz = w.take<__nv_bfloat16>(s.split * p.tp * p.vc);
         const int parts = s.split == 3 ? 6 : s.T <= kTwoParts ? 2 : 1;   // products of a unit (for more tokens the most likely number)
         auto least = [&](int64_t depth) { return s.split == 3 ? 1 : (depth + kDeepest - 1) / kDeepest; };   // (fp32 adds in short pieces)
@@ -518,14 +582,15 @@ template <typename E, int SPLIT> void run_loss(Run &r, const Shape &s, const Pla
         if (d.teacher_dtype == RESBM_F32) go(k_targets<float>, static_cast<const float *>(a.teacher));
         else go(k_targets<__nv_bfloat16>, static_cast<const __nv_bfloat16 *>(a.teacher));
     }
+    const LossScale scale{s.bwd && !F32 ? a.dloss : nullptr, d.dloss_each, tau, p.scale};
     const bool x_fits = al16(a.X) && d.ldx * (int64_t)sizeof(E) % 16 == 0;
     // one row block: the tokens without a target cost nothing more (but their rows must not enter dW)
     const bool direct = !s.bwd && !F32 && x_fits && T <= 256;
     if (!direct && T <= kCollect) {
         r.go(k_collect<E, SPLIT>, dim3((unsigned)((T + 7) / 8)), dim3(256), 0, 1, label, p.count, (int)T, static_cast<const E *>(a.X), d.ldx, x_fits, (int)s.d, (int)p.dp,
-             p.xp, p.tp * p.dp, p.n, p.token, p.row);
+             p.xp, p.tp * p.dp, p.n, p.token, p.row, scale);
     } else if (!direct) {
-        r.go(k_scan, dim3(kScanCtas), dim3(1024), 0, 1, label, p.count, (int)T, p.n, p.token, p.row);
+        r.go(k_scan, dim3(kScanCtas), dim3(1024), 0, 1, label, p.count, (int)T, p.n, p.token, p.row, scale);
         r.go(k_pack<E, SPLIT>, dim3(row_grid(c, p.tp, 8)), dim3(256), 0, 1, static_cast<const E *>(a.X), d.ldx, x_fits, p.token, p.n, 0, (int)s.d,
              (int)p.dp, p.xp, p.tp * p.dp);
     }
@@ -553,6 +618,7 @@ template <typename E, int SPLIT> void run_loss(Run &r, const Shape &s, const Pla
     g.zt = p.zt;
     g.lse = a.lse;
     g.dloss = a.dloss;
+    g.scale = p.scale;
     g.dloss_step = d.dloss_each;
     g.bad = s.distill ? p.bad : nullptr;
 
@@ -672,7 +738,7 @@ template <typename E, int SPLIT> void run_loss(Run &r, const Shape &s, const Pla
         run_gemm<VG_GRADS, DZ, F32 ? P : 0, 2>(r, gr, units);
         if (fins) {
             const int64_t most = std::max(fin[0].T, fin[1].T) * ((s.d + 7) / 8);
-            r.go(k_finish<E>, dim3(row_grid(c, most, 256), (unsigned)fins), dim3(256), 0, 1, fin[0], fin[1], (int)s.d, (int)p.dp);
+            r.go(k_finish<E>, dim3(row_grid(c, most, 256), (unsigned)fins), dim3(256), 0, 1, fin[0], fin[1], (int)s.d, (int)p.dp, static_cast<const float *>(p.scale));
         }
     }
     if (s.bwd) return;

@@ -3,7 +3,8 @@
 //
 //   VG_FWD   z = X . W^T             a row's running maximum and sum of exponentials over the unit's columns, and its
 //                                    targets' logits: 16 bytes a row and unit instead of the logits
-//   VG_DZ    z again, then           dz = g (softmax(z / tau) - q), stored for a piece of the vocabulary at a time
+//   VG_DZ    z again, then           dz = g (softmax(z / tau) - q), stored for a piece of the vocabulary at a time (bf16: over the g's
+//                                    common factor, whose rounding would be the same for every token's label)
 //   VG_DX    dz . W                  fp32, added to what earlier pieces gave
 //   VG_DW    dz^T . X                complete for the piece's rows of W (in one launch with VG_DX)
 //
@@ -82,6 +83,7 @@ struct VocabGemm {
     float2 *stat;             // FWD: (maximum c, sum of 2^(z c - maximum c)) of slot, row
     float *zt;                // FWD: the label's logit a row; with lists: the weighted sum of slot, row
     const float *lse, *dloss; // DZ: a token's log-sum-exp, its loss's gradient
+    const float *scale;       // bf16: the losses' gradients' common factor, and that times tau; dz is without it, the gradients get it at the end
     int32_t dloss_step;       // 1, or 0: one for all
     float tau;
     const float *bad;         // DZ: a value added to a token's gradient (NaN where its targets are none), or null
@@ -511,11 +513,14 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __gri
             }
             if (MODE == VG_DZ) {
                 r.lse = g.lse[r.token];
-                r.dloss = g.dloss[(int64_t)r.token * g.dloss_step];
+                // (one for all is the factor itself)
+                if (SPLIT == 2) r.dloss = g.dloss_step ? g.dloss[r.token] / g.scale[0] : 1.0f;
+                else r.dloss = g.dloss[(int64_t)r.token * g.dloss_step] * g.tau;
                 if (g.bad) r.bad = g.bad[r.token];
             }
             return r;
         };
+        const float factor = SPLIT == 2 && GRADS ? jobs.g[0].scale[1] : 1.0f;   // (of slots: k_finish)
         uint32_t u = unit_at(0);
         Unit ahead = {};
         if (u < units) ahead = unit_of(u);
@@ -546,7 +551,7 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __gri
                 t.start(g, in.token, in.label, g.v0 + nb * g.bn, first_group * 32);
                 if (MODE == VG_DZ) {
                     lse2 = in.lse * 1.4426950408889634f;
-                    grad = in.dloss * g.tau + in.bad;
+                    grad = in.dloss + in.bad;
                     if (g.label && in.label == INT32_MAX) grad = NAN;
                 }
             }
@@ -583,6 +588,10 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __gri
                     }
                 } else {
                     if (row0 >= rows || col >= g.cols) return;
+                    if (SPLIT == 2 && dw && !g.out_f32) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] *= factor;
+                    }
                     if (!dw) store_f32(mo, v, col, ks * g.slot_rows + row0, g.add);
                     else if (g.out) store_plain(g, v, col, row0);
                     else if (g.out_f32) store_f32(mo, v, col, g.out_y + ks * g.slot_rows + row0, false);

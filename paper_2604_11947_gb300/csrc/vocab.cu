@@ -292,6 +292,7 @@ struct JoinArgs {
     const float *ent;
     int64_t T, V;
     float c, tau;
+    float back, back_rest;     // 1 / (c tau) in two parts: from a logit times c to nats
     float *loss, *lse;
 };
 
@@ -336,7 +337,8 @@ template <int TX> __global__ void __launch_bounds__(256) k_join(const JoinArgs a
     if (r >= 0) {
         most = sm[0][x];
         const float log_sum = log2f(ss[0][x]);
-        lse = most == -INFINITY ? NAN : kLn2 * (most + log_sum);
+        // (rounded once: most + log_sum, in units of ln 2, would be off by more than lse's own rounding, and so would c's be)
+        lse = most == -INFINITY ? NAN : fmaf(most, a.back, fmaf(most, a.back_rest, kLn2 * log_sum));
         if (a.label) loss = a.label[t] < a.V ? kLn2 * (fmaf(-a.zt[r], a.c, most) + log_sum) : NAN;
         else loss = a.tau * a.tau * (a.ent[t] + kLn2 * (fmaf(-sz[0][x], a.c, most) + log_sum));
     }
@@ -742,7 +744,8 @@ template <typename E, int SPLIT> void run_loss(Run &r, const Shape &s, const Pla
         }
     }
     if (s.bwd) return;
-    JoinArgs j{p.stat, p.zt, p.slots, p.tp, direct ? nullptr : p.row, p.count, label, p.ent, T, V, g.c, tau, a.loss, a.lse_out};
+    const double back = 1.0 / ((double)g.c * tau);
+    JoinArgs j{p.stat, p.zt, p.slots, p.tp, direct ? nullptr : p.row, p.count, label, p.ent, T, V, g.c, tau, (float)back, (float)(back - (double)(float)back), a.loss, a.lse_out};
     if (T < 1024) r.go(k_join<1>, dim3((unsigned)T), dim3(256), 0, 1, j);
     else r.go(k_join<32>, dim3((unsigned)((T + 31) / 32)), dim3(256), 0, 1, j);
 }

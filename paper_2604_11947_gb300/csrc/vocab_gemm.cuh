@@ -521,6 +521,7 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __gri
             return r;
         };
         const float factor = SPLIT == 2 && GRADS ? jobs.g[0].scale[1] : 1.0f;   // (of slots: k_finish)
+        const float inv_tau = SPLIT == 3 && MODE == VG_DZ ? 1.0f / jobs.g[0].tau : 1.0f;
         uint32_t u = unit_at(0);
         Unit ahead = {};
         if (u < units) ahead = unit_of(u);
@@ -550,7 +551,7 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __gri
             if (!GRADS && row < n) {
                 t.start(g, in.token, in.label, g.v0 + nb * g.bn, first_group * 32);
                 if (MODE == VG_DZ) {
-                    lse2 = in.lse * 1.4426950408889634f;
+                    lse2 = SPLIT == 3 ? in.lse : in.lse * 1.4426950408889634f;
                     grad = in.dloss + in.bad;
                     if (g.label && in.label == INT32_MAX) grad = NAN;
                 }
@@ -562,7 +563,11 @@ __global__ void __launch_bounds__(VocabCfg::THREADS, 1) k_vocab_gemm(const __gri
                     if (col >= g.cols) return;
                     if (row < n) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = exp2_fast(fmaf(v[j], g.c, -lse2));
+                        for (int j = 0; j < 32; ++j) {
+                            // (fp32: lse times log2(e) has a rounding of its own, the same for the whole row)
+                            if (SPLIT == 3) v[j] = exp2_fast(fmaf(v[j], inv_tau, -lse2) * 1.4426950408889634f);
+                            else v[j] = exp2_fast(fmaf(v[j], g.c, -lse2));
+                        }
                         while (t.next < c + 32) {
                             const int at = t.next - c;
 #pragma unroll

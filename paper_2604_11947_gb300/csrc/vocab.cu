@@ -663,8 +663,11 @@ template <typename E, int SPLIT> void run_loss(Run &r, const Shape &s, const Pla
         // logits up to 1400: dX and dW 1.5e-2 off; in pieces 1024 deep 1.9e-3, their rounding). T = 16384, V = 32000, d = 2048 backward
         // 3903 -> 3947 us, T = 8192, d = 1100 3 % more; pieces 512 deep cost 4 to 10 %.
         constexpr int kLongPiece = 16;
-        if constexpr (F32) run_gemm<VG_DZ, DZ, P, 1>(r, z, row_blocks * u.nn);
-        else if (s.d > 64 * kLongPiece) run_gemm<VG_DZ, DZ, kLongPiece, 1>(r, z, row_blocks * u.nn);
+        // In fp32 up to 256 tokens in the forward's pieces, so that z is the same: 6 tokens of V = 545, d = 1168 had dX and dW 2.4e-6 off.
+        if constexpr (F32) {
+            if (T <= 256) run_gemm<VG_DZ, DZ, P / 4, 1>(r, z, row_blocks * u.nn);
+            else run_gemm<VG_DZ, DZ, P, 1>(r, z, row_blocks * u.nn);
+        } else if (s.d > 64 * kLongPiece) run_gemm<VG_DZ, DZ, kLongPiece, 1>(r, z, row_blocks * u.nn);
         else run_gemm<VG_DZ, DZ, 0, 1>(r, z, row_blocks * u.nn);
 
         VocabJobs<2> gr;

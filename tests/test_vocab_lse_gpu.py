@@ -37,3 +37,25 @@ def test_lse_and_probabilities(most, tau):
     tol = g.double().abs() * (tau or 1.0) * ((p * (z - lse.double()[:, None]).abs()).sum(dim=1) * 2 * U + 2.0 ** -20)
     off = (dX[:, 1].double() - total).abs()
     assert bool((off <= tol).all()), float((off / tol).max())
+
+
+@pytest.mark.parametrize("T", [6, 120, 256])
+def test_a_few_tokens_probabilities_sum_to_one(T):
+    """Forward and backward form the same logits, whatever the tensor cores cut off: with the forward's lse the probabilities' sum is off by
+    lse's rounding (U of it), 2^-20 for either side's exponentials and sum, and the second product's error: 2^-18 (17 MMAs' truncation,
+    2 * 2^-23 each) of the sum of |dz|, 2 at most. Sums of 64 terms of about 1000 and then of nearly as much with the other sign leave
+    logits of about one with an error of their own."""
+    V, d = 545, 1216
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x = 0.5 + torch.rand(T, 9, 1, 64, generator=g, device="cuda")
+    w = (0.9 + 0.2 * torch.rand(V, 9, 1, 64, generator=g, device="cuda")) * (1000 / 64)
+    rest = torch.randn(V, 9, 1, 64, generator=g, device="cuda") / 24
+    X, W = torch.zeros(T, d, device="cuda"), torch.ones(V, d, device="cuda")
+    X[:, :1152], W[:, :1152] = torch.cat((x, x), dim=2).view(T, 1152), torch.cat((w, rest - w), dim=2).view(V, 1152)
+    labels = torch.randint(0, V, (T,), generator=g, device="cuda")
+    up = each(T)
+    _, lse, dX, _ = run(X, W, labels, up)
+    assert float(lse.abs().max()) < 16
+    off = dX[:, -1].double().abs() / up.double().abs()
+    tol = U * 16 * 1.01 + 2 * 2.0 ** -20 + 2 * 17 * 2.0 ** -22 + 4 * U
+    assert bool((off <= tol).all()), float((off / tol).max())

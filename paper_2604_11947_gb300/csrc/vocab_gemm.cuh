@@ -32,8 +32,8 @@
 // runs in pieces, which alternate between the accumulators; the epilogue warps add them in registers, rounded to
 // nearest, while the next piece runs.
 //
-// What bounds it: with d of 2048 and more the tensor cores (T = 2048, V = 32000, d = 2048: 141 us forward, 143 dz, 278 both
-// gradients, 1880 to 1930 TFLOP/s; in a long run the board's power, 1.7 PFLOP/s); with d under 512 the epilogue, whose
+// What bounds it: with d of 2048 and more the tensor cores (T = 2048, V = 32000, d = 2048: 144 us forward, 157 dz, 283 both
+// gradients, 1710 to 1900 TFLOP/s; in a long run the board's power, 1.7 PFLOP/s); with d under 512 the epilogue, whose
 // warps wait for their own results most of the time (T = 8192, V = 32000, d = 128 130 us forward, where the tensor cores need 38 and
 // the exponentials 57). Sixteen epilogue warps of 64 columns took 235: what a unit costs a warp apart from its columns, and 96
 // registers a thread, which spill. The logits' targets are looked up by bisection in a token's sorted list, and a label is a

@@ -90,7 +90,8 @@ __global__ void __launch_bounds__(256) k_targets(const int64_t *__restrict__ ind
 // ---- the tokens in use -----------------------------------------------------------------------------
 // The common factor of the losses' gradients, taken out of dz before its rounding to bf16: the dz of a token's label is next to -dloss
 // as long as the model knows nothing of it, and where dloss is one number for all (the mean over n tokens: 1 / n) its rounding is
-// the same for all, up to 2^-8 in the end of dX and dW that no sum averages (T = 24, V = 24141, d = 2480: 2.5e-3 off, without it 1.9e-3; the outputs' rounding is 1.7e-3).
+// the same for all, an error of dX and dW of up to 2^-8 that no sum averages (T = 24, V = 24141, d = 2480: 2.5e-3 off, without it
+// 1.9e-3; the outputs' rounding alone is 1.7e-3).
 struct LossScale {
     const float *dloss;   // null: none is asked for
     int each;

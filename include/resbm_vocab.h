@@ -69,10 +69,11 @@ RESBM_API resbm_status resbm_linear_ce_fwd(const resbm_vocab_desc *desc, const v
  *   lse : T fp32 in, resbm_linear_ce_fwd's.  dX : T x d out, zero on tokens without a label.  dW : V x d out, complete (not
  *   added to). Both dense, of type dtype; either may be NULL.
  * z is formed again, for a piece of the vocabulary at a time, whose dz is kept in ws (bf16, or fp32 as three bf16 values):
- * with bf16 tensors dz is rounded to bf16 as it enters the products (without the largest finite |dloss| of the tokens with a target, by
- * which the products' sums are multiplied, so that a dloss that all have in common is not rounded; one under 2^-110 of it loses bits), which puts a relative error of 2^-8 at most on its elements, one
- * of the size of the outputs' own rounding (where 16 tokens or fewer have a target it is kept to 16 bits, as two bf16 values). The products' sums lose
- * at most 2^-10 of their terms' absolute sum to the tensor cores' additions (65536 terms or more, all of one sign; in proportion with fewer). */
+ * with bf16 tensors dz is rounded to bf16 as it enters the products, which puts a relative error of 2^-8 at most on its elements, one of
+ * the size of the outputs' own rounding (where 16 tokens or fewer have a target it is kept to 16 bits, as two bf16 values). The largest
+ * finite |dloss| of the tokens with a target is taken out of dz and multiplies the products' sums, so that a dloss that all have in
+ * common is not rounded; one under 2^-110 of it loses bits. The products' sums lose at most 2^-10 of their terms' absolute sum to the
+ * tensor cores' additions (65536 terms or more, all of one sign; in proportion with fewer). */
 RESBM_API resbm_status resbm_linear_ce_bwd(const resbm_vocab_desc *desc, const void *X, const void *W, const int64_t *labels,
                                            const float *lse, const float *dloss, void *dX, void *dW, void *ws, size_t ws_bytes,
                                            void *stream);
